@@ -5,8 +5,8 @@
   diff         differential attention (diff_attention), O = (softmax(s q1 k1^T) - lam_h softmax(s q2 k2^T)) v.
 
 ``call`` is "fwd" (no gradients: evaluation, serving) or "step" (outputs and the gradients of everything learned).
-With ``own`` false ``run`` computes the operators from elementary operations in 32 bits, one head at a time, rounded
-once at the end; with ``own`` true it calls the package's operators.
+With ``own`` false ``run`` computes the operators from elementary operations in 32 bits, rounded once at the end; with
+``own`` true it calls the package's operators.
 """
 import math
 
@@ -238,61 +238,62 @@ def _plain_norm_rope(s, c):
     return (yq, yk) if dq is None else [yq, yk, gq, gk, gwq, gwk]
 
 
-def _hidden(c, qlen, klen, r0, r1, dev):
-    """Pairs of the rows r0 .. r1 - 1 that the masks exclude, and the rows past their sequence."""
+def _visible_pairs(c, qlen, klen, r0, r1, dev):
+    """Pairs of the rows r0 .. r1 - 1 that the masks leave, [B or 1, 1, 1, rows, N_K]."""
     rows = torch.arange(r0, r1, device=dev)[:, None]
     cols = torch.arange(c["nk"], device=dev)[None, :]
-    nq = c["nq"] if qlen is None else qlen
-    nk = c["nk"] if klen is None else klen
-    hidden = cols >= nk
+    nq = c["nq"] if qlen is None else qlen[:, None, None]
+    nk = c["nk"] if klen is None else klen[:, None, None]
+    seen = (cols < nk) & (rows < nq)
     if c["causal"]:
-        hidden = hidden | (cols > rows + (nk - nq))
-    return hidden | (rows >= nq)
+        seen = seen & (cols <= rows + (nk - nq))
+    return seen.reshape(-1, 1, 1, r1 - r0, c["nk"])
 
 
-def _plain_map(q, k, scale, hidden):
-    z = (q @ k.T) * scale
-    z = z.masked_fill(hidden, -math.inf)
-    m = z.amax(1, keepdim=True)
+def _plain_map(q, k, seen):
+    """softmax of the visible logits of q [B, Hk, G, rows, d] (scaled) and k [B, Hk, N_K, d]; rows that see nothing: 0."""
+    z = (q.flatten(2, 3) @ k.transpose(2, 3).contiguous()).view(*q.shape[:4], -1)
+    z = z.masked_fill(~seen, -math.inf)
+    m = z.amax(-1, keepdim=True)
     e = torch.exp(z - torch.where(m == -math.inf, 0.0, m))
-    total = e.sum(1, keepdim=True)
-    return e / torch.where(total == 0, 1.0, total)
+    return e / e.sum(-1, keepdim=True).clamp_min(1e-37)
 
 
 def _plain_diff(s, c):
-    q1, k1, q2, k2, v, lam = (s[n].detach().float() for n in ("q1", "k1", "q2", "k2", "v", "lam"))
-    step, G = c["call"] == "step", c["H"] // c["Hk"]
-    out = torch.zeros(c["B"], c["H"], c["nq"], c["dv"], device=q1.device)
-    scale = 1.0 / math.sqrt(c["d"])
+    step, G, scale = c["call"] == "step", c["H"] // c["Hk"], 1.0 / math.sqrt(c["d"])
+    q1, q2 = (s[n].detach().float().unflatten(1, (c["Hk"], G)) for n in ("q1", "q2"))
+    k1, k2, v = (s[n].detach().float().contiguous() for n in ("k1", "k2", "v"))
+    lam = s["lam"].detach().view(c["Hk"], G, 1, 1)
+    out = torch.empty(*q1.shape[:4], c["dv"], device=q1.device)
     if step:
-        do = s["do"].float()
-        g1, h1, g2, h2, gv, gl = (torch.zeros_like(x) for x in (q1, k1, q2, k2, v, lam))
-    block = max(1, min(c["nq"], (1 << 28) // c["nk"]))
-    for b in range(c["B"]):
-        ql, kl = (None if s[n] is None else s[n][b] for n in ("qlen", "klen"))
-        for r0 in range(0, c["nq"], block):
-            r = slice(r0, min(c["nq"], r0 + block))
-            hidden = _hidden(c, ql, kl, r.start, r.stop, q1.device)
-            for h in range(c["H"]):
-                j = h // G
-                p1 = _plain_map(q1[b, h, r], k1[b, j], scale, hidden)
-                p2 = _plain_map(q2[b, h, r], k2[b, j], scale, hidden)
-                p = p1 - lam[h] * p2
-                out[b, h, r] = p @ v[b, j]
-                if not step:
-                    continue
-                gv[b, j] += p.T @ do[b, h, r]
-                dp = do[b, h, r] @ v[b, j].T
-                d2 = (p2 * dp).sum(1, keepdim=True)
-                gl[h] -= d2.sum()
-                ds1 = p1 * (dp - (p1 * dp).sum(1, keepdim=True)) * scale
-                ds2 = p2 * (dp - d2) * (-scale * lam[h])
-                g1[b, h, r] = ds1 @ k1[b, j]
-                g2[b, h, r] = ds2 @ k2[b, j]
-                h1[b, j] += ds1.T @ q1[b, h, r]
-                h2[b, j] += ds2.T @ q2[b, h, r]
-    out = out.bfloat16()
-    return [out, *(x.bfloat16() for x in (g1, h1, g2, h2, gv)), gl] if step else out
+        do = s["do"].float().unflatten(1, (c["Hk"], G))
+        g1, h1, g2, h2, gv = (torch.zeros_like(x) for x in (q1, k1, q2, k2, v))
+        gl = torch.zeros_like(lam)
+    # the maps of all heads at once, as many rows at a time as keep one of them within 2 GB
+    block = max(1, min(c["nq"], (1 << 29) // (c["B"] * c["H"] * c["nk"])))
+    for r0 in range(0, c["nq"], block):
+        r = slice(r0, min(c["nq"], r0 + block))
+        seen = _visible_pairs(c, s["qlen"], s["klen"], r.start, r.stop, q1.device)
+        p1, p2 = (_plain_map(q[:, :, :, r] * scale, k, seen) for q, k in ((q1, k1), (q2, k2)))
+        p = (p1 - lam * p2).flatten(2, 3)
+        out[:, :, :, r] = (p @ v).unflatten(2, (G, -1))
+        if not step:
+            continue
+        dor = do[:, :, :, r].flatten(2, 3)
+        gv += p.transpose(2, 3).contiguous() @ dor
+        dp = (dor @ v.transpose(2, 3).contiguous()).view(p1.shape)
+        d2 = (p2 * dp).sum(-1, keepdim=True)
+        gl -= d2.sum((0, 3), keepdim=True)[0]
+        ds1 = (p1 * (dp - (p1 * dp).sum(-1, keepdim=True)) * scale).flatten(2, 3)
+        ds2 = (p2 * (dp - d2) * (-scale * lam)).flatten(2, 3)
+        g1[:, :, :, r] = (ds1 @ k1).unflatten(2, (G, -1))
+        g2[:, :, :, r] = (ds2 @ k2).unflatten(2, (G, -1))
+        h1 += ds1.transpose(2, 3).contiguous() @ q1[:, :, :, r].flatten(2, 3)
+        h2 += ds2.transpose(2, 3).contiguous() @ q2[:, :, :, r].flatten(2, 3)
+    out = out.flatten(1, 2).bfloat16()
+    if not step:
+        return out
+    return [out, *(x.bfloat16() for x in (g1.flatten(1, 2), h1, g2.flatten(1, 2), h2, gv)), gl.flatten()]
 
 
 # --- what a pass cannot do without ------------------------------------------------------------------------------------
