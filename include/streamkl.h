@@ -330,6 +330,171 @@ size_t streamkl_fwd_split_workspace_bytes(int B, int H, int N_Q, int splits);
  */
 int streamkl_fwd_split_count(int B, int H, int N_Q, int N_K, int d1, int d2);
 
+/*
+ * The operators around the divergence
+ * -----------------------------------
+ * What stands before and beside the two maps that the calls above compare:
+ * the norm and rotation that make a layer's queries and keys
+ * (streamkl_qk_norm_rope_*), and attention by the difference of two maps
+ * (streamkl_diff_*). The conventions above hold: device pointers of the
+ * caller, nothing allocated, checks before anything is enqueued, work on
+ * `stream`, which belongs to the current device. All of these calls launch
+ * kernels only and record into a HIP graph, and their results are
+ * reproducible bit for bit (no atomics).
+ */
+
+/* Element types. */
+typedef enum {
+  STREAMKL_BF16 = 0,
+  STREAMKL_F16 = 1,
+  STREAMKL_F32 = 2
+} streamkl_dtype;
+
+/*
+ * A [batch, head, row] arrangement of contiguous rows in memory: row n of
+ * head h of batch b begins at data + b sb + h sh + n sn (in elements). data
+ * is 16-byte aligned, the strides are >= 0 and whole 16-byte steps. Strides of
+ * extents of 1 must satisfy this too (0 will do). The struct itself lies in
+ * host memory and is read before the call returns.
+ */
+typedef struct {
+  const void* data;
+  long long sb, sh, sn;
+} streamkl_rows;
+
+/*
+ * Norms of queries and keys per head, with the position rotation in the same
+ * pass. For every head x[0..d) of a token, with its learned weight w and the
+ * cosines c and sines s of the token's position:
+ *     n_j = x_j w_j / sqrt(mean_i x_i^2 + eps)
+ *     y_a = n_a c - n_b s,  y_b = n_b c + n_a s   for every rotated pair (a, b)
+ *     y_j = n_j                                   for the columns j >= rot
+ *   q         [B, N_Q, H, d]: rows as a projection leaves them, or in any
+ *             arrangement streamkl_rows can express. NULL: no queries.
+ *   k         [B, N_K, HK, d], the same; NULL: no keys.
+ *   d         a multiple of 32, 32 to 256.
+ *   dtype     element type of q and k (streamkl_dtype).
+ *   wq, wk    float32 [d], 16-byte aligned; NULL: ones.
+ *   eps       finite, > 0.
+ *   table     float32 [n_pos, rot], 16-byte aligned: for every position the
+ *             rot/2 cosines, then the rot/2 sines. Not read when rot = 0.
+ *   rot       columns that are rotated: a multiple of 16, at most d (0: the
+ *             norm alone). interleaved = 0 pairs (j, j + rot/2), 1 pairs
+ *             (2 j, 2 j + 1).
+ *   q_pos, k_pos  positions, int32 (pos64 = 0) or int64 (pos64 = 1):
+ *             contiguous [N] shared by all sequences (*_pos_shared = 1) or
+ *             [B, N]. NULL: keys stand at 0 .. N_K - 1 and queries are the
+ *             last N_Q of these places (bottom-right alignment; N_Q <= N_K
+ *             then, and N_Q = places 0 .. N_Q - 1 without keys). A position
+ *             outside the table gives NaN in the rotated columns of its rows;
+ *             nothing is read there.
+ *   k_copies  every key head is written this often in a row: yk has
+ *             HK k_copies heads. With k_copies = H / HK it has one per query
+ *             head, as streamkl_fwd reads them.
+ *   yq, yk    bf16, contiguous [B, H, N_Q, d] and [B, HK k_copies, N_K, d],
+ *             16-byte aligned. Sums and products are float32, rounded once.
+ * At most 2^31 - 1 heads of tokens (B N H) a tensor, else
+ * STREAMKL_ERR_UNSUPPORTED.
+ */
+int streamkl_qk_norm_rope_fwd(const streamkl_rows* q, const streamkl_rows* k, int B, int H, int HK, int N_Q, int N_K,
+                              int d, int dtype, const float* wq, const float* wk, float eps,
+                              const float* table, int n_pos, int rot, int interleaved,
+                              const void* q_pos, const void* k_pos, int pos64, int q_pos_shared, int k_pos_shared,
+                              int k_copies, void* yq, void* yk, hipStream_t stream);
+
+/*
+ * Gradients of streamkl_qk_norm_rope_fwd, from its inputs alone.
+ *   dyq, dyk  upstream gradients in the layout of yq, yk, bf16 or float32
+ *             (dy_dtype); the gradients of a key head's copies are added.
+ *   dxq, dxk  contiguous [B, N_Q, H, d] and [B, N_K, HK, d] in the inputs'
+ *             type, 16-byte aligned.
+ *   dwq, dwk  float32 [d]; NULL: not wanted.
+ *   workspace device memory, 4-byte aligned, at least
+ *             streamkl_qk_norm_rope_bwd_workspace_bytes bytes (not needed
+ *             where neither dwq nor dwk is wanted); calls that may overlap
+ *             need one each, as do two captured graphs that may.
+ */
+int streamkl_qk_norm_rope_bwd(const streamkl_rows* q, const streamkl_rows* k, int B, int H, int HK, int N_Q, int N_K,
+                              int d, int dtype, const float* wq, const float* wk, float eps,
+                              const float* table, int n_pos, int rot, int interleaved,
+                              const void* q_pos, const void* k_pos, int pos64, int q_pos_shared, int k_pos_shared,
+                              int k_copies, const void* dyq, const void* dyk, int dy_dtype,
+                              void* workspace, size_t workspace_bytes,
+                              void* dxq, void* dxk, float* dwq, float* dwk, hipStream_t stream);
+
+/* Workspace bytes of streamkl_qk_norm_rope_bwd with both weight gradients; 0 for invalid extents. */
+size_t streamkl_qk_norm_rope_bwd_workspace_bytes(int B, int H, int HK, int N_Q, int N_K, int d);
+
+/*
+ * Differential attention: attention by the difference of two softmax maps,
+ *     S_t = scale * Q_t[b,h,i] K_t[b,hk]^T,  P_t = softmax(S_t) over the keys row i may attend,
+ *     O = (P_1 - lam_h P_2) V[b,hk],         hk = h / (H / HK)
+ * in one pass over the keys that materialises neither map.
+ *   q1, q2    bf16 [B, H, N_Q, d];  k1, k2 [B, HK, N_K, d];  v [B, HK, N_K, dv], each in any arrangement
+ *             that streamkl_rows can express with row strides below 2^25 elements (rows of a head may span
+ *             more than 4 GiB). H is a multiple of HK: groups of H / HK consecutive query heads share a key
+ *             head, and their keys and values are streamed once for the group.
+ *   d         a multiple of 32, 32 to 128;  dv a multiple of 32, 32 to 256. The kernels are built for 64 and 128
+ *             (and 256 for dv); others run the next one up with the missing columns read as zeros.
+ *   scale     2^-64 to 2^64 (usual: 1/sqrt(d)); the scaled logits must stay in the float32 range.
+ *   lam       float32 [H] on the device, any sign.
+ *   q_len, kv_len  int32 [B] on the device, or NULL: sequence b has its first q_len[b] rows and kv_len[b] keys
+ *             (values outside 0 .. N are clamped). Keys behind kv_len are not read, whatever they hold.
+ *             Rows behind q_len give O = 0, LSE = -inf and zero gradients, and take no part in any other.
+ *   causal    1: row i sees the keys j <= kv_len[b] - q_len[b] + i (bottom-right alignment). Rows that see no
+ *             key give O = 0, LSE = -inf and zero gradients.
+ *   splits    1: one pass. 2 to 256: the keys are cut into this many ranges of whole 32-key tiles, streamed by
+ *             workgroups of their own and joined by a second kernel: for few rows against many keys.
+ *             streamkl_diff_fwd_split_count gives the library's choice.
+ *   workspace for splits > 1: device memory, 16-byte aligned, at least streamkl_diff_fwd_workspace_bytes bytes,
+ *             contents ignored on entry and unspecified on return. Calls that may overlap need one each, and
+ *             so do captured graphs whose replays may overlap.
+ *   out       bf16 [B, H, N_Q, dv], contiguous, 16-byte aligned.
+ *   out2, lse1, lse2  what the backward pass needs: O_2 = P_2 V (layout of out) and the natural-log
+ *             log-sum-exps [B, H, N_Q] of the two maps; each may be NULL.
+ * Sums, maxima and accumulators are float32; P_t is rounded to bf16 as an operand of the product with V, O once at
+ * the end. Keys that a row may see are expected finite, as are the rows: a non-finite value in a key row that the
+ * causal mask hides from row i can reach it where both fall into one 32-key tile (0 x inf), never through kv_len
+ * or q_len.
+ */
+int streamkl_diff_fwd(const streamkl_rows* q1, const streamkl_rows* k1, const streamkl_rows* q2,
+                      const streamkl_rows* k2, const streamkl_rows* v,
+                      int B, int H, int HK, int N_Q, int N_K, int d, int dv, float scale, int causal,
+                      const float* lam, const int* q_len, const int* kv_len,
+                      int splits, void* workspace, size_t workspace_bytes,
+                      void* out, void* out2, float* lse1, float* lse2, hipStream_t stream);
+
+/* Split count of the library for these extents: as many as give one round of resident workgroups, four tiles each at
+   least; 1 where the single pass fills the chip. 0 for invalid or unsupported arguments. */
+int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int N_K, int d, int dv);
+
+/* Workspace bytes of streamkl_diff_fwd: 8 * splits * B * H * N_Q * (dv + 2) when splits > 1, else 0. */
+size_t streamkl_diff_fwd_workspace_bytes(int B, int H, int N_Q, int dv, int splits);
+
+/*
+ * Gradients of streamkl_diff_fwd's output, recomputed tile by tile from out, out2, lse1 and lse2 of a forward call
+ * with the same inputs. With dP = dO V^T and D_t = dO . O_t:
+ *     dS_1 = P_1 (dP - D_1),  dS_2 = -lam P_2 (dP - D_2),  dQ_t = scale dS_t K_t,  dK_t = scale dS_t^T Q_t,
+ *     dV = (P_1 - lam P_2)^T dO,  dlam_h = -sum over its rows and keys of P_2 dP
+ * (dK_t, dV summed over the query heads of the group, dlam over the batch).
+ *   dout      bf16 [B, H, N_Q, dv], contiguous, 16-byte aligned; rows behind q_len are not read.
+ *   workspace device memory, 16-byte aligned, at least streamkl_diff_bwd_workspace_bytes bytes; as above.
+ *   dq1, dq2  [B, H, N_Q, d];  dk1, dk2 [B, HK, N_K, d];  dvalues [B, HK, N_K, dv], contiguous: float32, or bf16
+ *             with bf16_grads = 1 (4-byte aligned, each value rounded once). dlam float32 [H]. Each may be
+ *             NULL (not wanted), not all of them; no kernel runs for outputs that are all NULL.
+ */
+int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k1, const streamkl_rows* q2,
+                      const streamkl_rows* k2, const streamkl_rows* v,
+                      int B, int H, int HK, int N_Q, int N_K, int d, int dv, float scale, int causal,
+                      const float* lam, const int* q_len, const int* kv_len,
+                      const void* dout, const void* out, const void* out2, const float* lse1, const float* lse2,
+                      void* workspace, size_t workspace_bytes,
+                      void* dq1, void* dk1, void* dq2, void* dk2, void* dvalues, float* dlam,
+                      int bf16_grads, hipStream_t stream);
+
+/* Workspace bytes of streamkl_diff_bwd; 0 for negative extents. */
+size_t streamkl_diff_bwd_workspace_bytes(int B, int H, int N_Q);
+
 /* Static description of a status code. Never NULL. */
 const char* streamkl_strerror(int status);
 

@@ -1,0 +1,185 @@
+// C ABI of differential attention: argument checks and dispatch. Every check
+// happens before anything is enqueued.
+#include <cmath>
+#include <cstdint>
+
+#include "diff_launch.hpp"
+#include "streamkl.h"
+
+namespace {
+
+using streamkl::DiffArgs;
+using streamkl::DiffRows;
+
+constexpr long long kMaxInt = 0x7fffffffLL;
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Rows of one input; `used`: it has elements that a kernel may read.
+int check_rows(const streamkl_rows* x, bool used) {
+  if (!x) return STREAMKL_ERR_INVALID_ARG;
+  if (!used) return STREAMKL_OK;
+  if (!x->data || !aligned(x->data, 16)) return STREAMKL_ERR_INVALID_ARG;
+  if (x->sb < 0 || x->sh < 0 || x->sn < 0 || x->sb % 8 || x->sh % 8 || x->sn % 8) return STREAMKL_ERR_INVALID_ARG;
+  // a tile of 32 rows is addressed with 31-bit byte offsets
+  if (x->sn >= 1LL << 25) return STREAMKL_ERR_UNSUPPORTED;
+  return STREAMKL_OK;
+}
+
+int check_extents(int B, int H, int HK, int N_Q, int N_K, int d, int dv) {
+  if (B < 0 || H < 0 || HK < 0 || N_Q < 0 || N_K < 0) return STREAMKL_ERR_INVALID_ARG;
+  if (H > 0 && (HK == 0 || H % HK != 0)) return STREAMKL_ERR_INVALID_ARG;
+  if (H == 0 && HK != 0) return STREAMKL_ERR_INVALID_ARG;
+  if (!streamkl::diff_dims(d, dv)) return STREAMKL_ERR_UNSUPPORTED;
+  const long long bh = (long long)B * H;
+  // rows and 128-row blocks are counted in 31 bits
+  if (bh > kMaxInt || (H && (long long)N_Q * (H / HK) > kMaxInt - 256) || (bh && N_Q > (kMaxInt - 256) / bh))
+    return STREAMKL_ERR_UNSUPPORTED;
+  if (N_K > kMaxInt - 256 || (HK && B && (N_K + 127LL) / 128 > kMaxInt / ((long long)B * HK))) return STREAMKL_ERR_UNSUPPORTED;
+  return STREAMKL_OK;
+}
+
+bool scale_ok(float s) { return std::isfinite(s) && s >= 0x1p-64f && s <= 0x1p64f; }
+
+DiffRows rows_of(const streamkl_rows* x) {
+  return DiffRows{static_cast<const uint16_t*>(x->data), x->sb, x->sh, x->sn};
+}
+
+int check_inputs(const streamkl_rows* q1, const streamkl_rows* k1, const streamkl_rows* q2, const streamkl_rows* k2,
+                 const streamkl_rows* v, int B, int H, int HK, int N_Q, int N_K, int d, int dv, float scale, int causal,
+                 const float* lam, const int* q_len, const int* kv_len, hipStream_t stream, DiffArgs* a) {
+  if (causal != 0 && causal != 1) return STREAMKL_ERR_INVALID_ARG;
+  int st = check_extents(B, H, HK, N_Q, N_K, d, dv);
+  if (st != STREAMKL_OK) return st;
+  if (!scale_ok(scale)) return STREAMKL_ERR_INVALID_ARG;
+  const bool rows = (long long)B * H * N_Q != 0, keys = (long long)B * HK * N_K != 0;
+  const streamkl_rows* in[] = {q1, q2, k1, k2, v};
+  for (int i = 0; i < 5; ++i) {
+    st = check_rows(in[i], i < 2 ? rows : keys);
+    if (st != STREAMKL_OK) return st;
+  }
+  if (H > 0 && (!lam || !aligned(lam, 4))) return STREAMKL_ERR_INVALID_ARG;
+  if ((q_len && !aligned(q_len, 4)) || (kv_len && !aligned(kv_len, 4))) return STREAMKL_ERR_INVALID_ARG;
+  *a = DiffArgs{};
+  a->q1 = rows_of(q1);
+  a->k1 = rows_of(k1);
+  a->q2 = rows_of(q2);
+  a->k2 = rows_of(k2);
+  a->v = rows_of(v);
+  a->B = B;
+  a->H = H;
+  a->HK = HK;
+  a->NQ = N_Q;
+  a->NK = N_K;
+  a->d = d;
+  a->dv = dv;
+  a->scale = scale;
+  a->causal = causal;
+  a->lam = lam;
+  a->q_len = q_len;
+  a->kv_len = kv_len;
+  a->splits = 1;
+  a->stream = stream;
+  return STREAMKL_OK;
+}
+
+int hip_status(hipError_t e) { return e == hipSuccess ? STREAMKL_OK : STREAMKL_ERR_HIP; }
+
+}  // namespace
+
+extern "C" int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int N_K, int d, int dv) {
+  if (check_extents(B, H, HK, N_Q, N_K, d, dv) != STREAMKL_OK) return 0;
+  if ((long long)B * H * N_Q == 0) return 1;
+  const long long R = (long long)N_Q * (H / HK);
+  const int rows = streamkl::diff_fwd_rows(d, dv, R);
+  const long long base = (long long)B * HK * ((R + rows - 1) / rows), resident = streamkl::diff_fwd_resident(d, dv, R);
+  const long long tiles = (N_K + 31LL) / 32;
+  long long s = resident / base;   // one round of workgroups
+  if (s > tiles / 4) s = tiles / 4;   // each of them streams a few tiles
+  if (s > streamkl::kDiffMaxSplits) s = streamkl::kDiffMaxSplits;
+  return s < 2 ? 1 : (int)s;
+}
+
+extern "C" size_t streamkl_diff_fwd_workspace_bytes(int B, int H, int N_Q, int dv, int splits) {
+  if (B < 0 || H < 0 || N_Q < 0 || dv < 0 || splits <= 1 || splits > streamkl::kDiffMaxSplits) return 0;
+  return (size_t)B * H * N_Q * splits * 2 * (dv + 2) * sizeof(float);
+}
+
+extern "C" int streamkl_diff_fwd(const streamkl_rows* q1, const streamkl_rows* k1, const streamkl_rows* q2,
+                                 const streamkl_rows* k2, const streamkl_rows* v, int B, int H, int HK, int N_Q,
+                                 int N_K, int d, int dv, float scale, int causal, const float* lam, const int* q_len,
+                                 const int* kv_len, int splits, void* workspace, size_t workspace_bytes, void* out,
+                                 void* out2, float* lse1, float* lse2, hipStream_t stream) {
+  DiffArgs a;
+  const int st = check_inputs(q1, k1, q2, k2, v, B, H, HK, N_Q, N_K, d, dv, scale, causal, lam, q_len, kv_len, stream,
+                              &a);
+  if (st != STREAMKL_OK) return st;
+  if (splits < 1) return STREAMKL_ERR_INVALID_ARG;
+  if (splits > streamkl::kDiffMaxSplits) return STREAMKL_ERR_UNSUPPORTED;
+  if ((long long)B * H * N_Q == 0) return STREAMKL_OK;
+  if (splits > 1 && (!workspace || !aligned(workspace, 16) ||
+                     workspace_bytes < streamkl_diff_fwd_workspace_bytes(B, H, N_Q, dv, splits)))
+    return STREAMKL_ERR_INVALID_ARG;
+  if (!out || !aligned(out, 16) || (out2 && !aligned(out2, 16))) return STREAMKL_ERR_INVALID_ARG;
+  if ((lse1 && !aligned(lse1, 4)) || (lse2 && !aligned(lse2, 4))) return STREAMKL_ERR_INVALID_ARG;
+  a.splits = splits;
+  a.part = static_cast<float*>(workspace);
+  a.out = static_cast<uint16_t*>(out);
+  a.out2 = static_cast<uint16_t*>(out2);
+  a.lse1 = lse1;
+  a.lse2 = lse2;
+  hipError_t e = streamkl::launch_diff_fwd(a);
+  if (e == hipSuccess && splits > 1) e = streamkl::launch_diff_merge(a);
+  return hip_status(e);
+}
+
+extern "C" size_t streamkl_diff_bwd_workspace_bytes(int B, int H, int N_Q) {
+  if (B < 0 || H < 0 || N_Q < 0) return 0;
+  return (streamkl::diff_bwd_stats_floats(B, H, N_Q) + streamkl::diff_bwd_dlam_floats(B, H, N_Q)) * sizeof(float);
+}
+
+extern "C" int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k1, const streamkl_rows* q2,
+                                 const streamkl_rows* k2, const streamkl_rows* v, int B, int H, int HK, int N_Q,
+                                 int N_K, int d, int dv, float scale, int causal, const float* lam, const int* q_len,
+                                 const int* kv_len, const void* dout, const void* out, const void* out2,
+                                 const float* lse1, const float* lse2, void* workspace, size_t workspace_bytes,
+                                 void* dq1, void* dk1, void* dq2, void* dk2, void* dvalues, float* dlam,
+                                 int bf16_grads, hipStream_t stream) {
+  DiffArgs a;
+  const int st = check_inputs(q1, k1, q2, k2, v, B, H, HK, N_Q, N_K, d, dv, scale, causal, lam, q_len, kv_len, stream,
+                              &a);
+  if (st != STREAMKL_OK) return st;
+  if (bf16_grads != 0 && bf16_grads != 1) return STREAMKL_ERR_INVALID_ARG;
+  if (!dq1 && !dk1 && !dq2 && !dk2 && !dvalues && !dlam) return STREAMKL_ERR_INVALID_ARG;
+  const bool rows = (long long)B * H * N_Q != 0, keys = (long long)B * HK * N_K != 0;
+  const bool of_rows = dq1 || dq2 || dlam, of_keys = dk1 || dk2 || dvalues;
+  const void* f32[] = {lse1, lse2, dlam, dq1, dk1, dq2, dk2, dvalues};
+  for (const void* p : f32)
+    if (p && !aligned(p, 4)) return STREAMKL_ERR_INVALID_ARG;
+  if (rows) {
+    if (!dout || !out || !out2 || !lse1 || !lse2) return STREAMKL_ERR_INVALID_ARG;
+    if (!aligned(dout, 16) || !aligned(out, 16) || !aligned(out2, 16)) return STREAMKL_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16) || workspace_bytes < streamkl_diff_bwd_workspace_bytes(B, H, N_Q))
+      return STREAMKL_ERR_INVALID_ARG;
+  }
+  a.dout = static_cast<const uint16_t*>(dout);
+  a.out = static_cast<uint16_t*>(const_cast<void*>(out));     // read only here
+  a.out2 = static_cast<uint16_t*>(const_cast<void*>(out2));
+  a.lse1 = const_cast<float*>(lse1);
+  a.lse2 = const_cast<float*>(lse2);
+  a.stats = static_cast<float*>(workspace);
+  a.dlam_part = a.stats ? a.stats + streamkl::diff_bwd_stats_floats(B, H, N_Q) : nullptr;
+  a.dq1 = dq1;
+  a.dk1 = dk1;
+  a.dq2 = dq2;
+  a.dk2 = dk2;
+  a.dv_out = dvalues;
+  a.dlam = dlam;
+  a.bf16_grads = bf16_grads;
+  hipError_t e = hipSuccess;
+  if (rows) e = streamkl::launch_diff_bwd_prep(a);
+  if (e == hipSuccess && keys && of_keys) e = streamkl::launch_diff_bwd_dkv(a);   // without rows: zeros
+  if (e == hipSuccess && rows && of_rows) e = streamkl::launch_diff_bwd_dq(a);
+  if (e == hipSuccess && dlam && H > 0) e = streamkl::launch_diff_bwd_dlam(a);
+  return hip_status(e);
+}

@@ -1,0 +1,151 @@
+// Shared parts of the differential-attention kernels: arguments, tile
+// staging from strided rows, operand addressing.
+//
+//   S_t = s Q_t K_t^T (masked), P_t = softmax(S_t), O_t = P_t V,
+//   O = O_1 - lam_h O_2,   t = 1, 2
+//
+// Query heads share keys and values in groups of G = H / HK consecutive
+// heads. Sequence b has q_len[b] rows and kv_len[b] keys (all of them without
+// lengths); row i of it sees the keys j < kv_len[b] and, under the causal
+// mask, j <= kv_len[b] - q_len[b] + i.
+#pragma once
+
+#include "kl_common.hpp"
+
+namespace streamkl {
+
+constexpr int kDiffTile = 32;   // streamed rows per tile: one 32 x 32 MFMA block
+
+// Rows [batch, head, row] with element strides; see streamkl_rows.
+struct DiffRows {
+  const uint16_t* p;
+  long long sb, sh, sn;
+};
+
+struct DiffArgs {
+  DiffRows q1, k1, q2, k2, v;
+  int B, H, HK, NQ, NK, d, dv;
+  float scale;
+  int causal;
+  const float* lam;          // [H]
+  const int *q_len, *kv_len; // [B] or null
+  // forward
+  uint16_t *out, *out2;      // [B, H, NQ, dv]; out2 (O_2) may be null
+  float *lse1, *lse2;        // [B, H, NQ], may be null
+  int splits;
+  float* part;               // splits > 1: see diff_fwd.hpp
+  // backward
+  const uint16_t* dout;      // [B, H, NQ, dv]
+  float* stats;              // prepared row statistics, see diff_bwd.hpp
+  float* dlam_part;          // partial sums of dlam
+  void *dq1, *dk1, *dq2, *dk2, *dv_out;
+  float* dlam;
+  int bf16_grads;
+  hipStream_t stream;
+};
+
+__device__ __forceinline__ int clamp_len(const int* len, int b, int n) {
+  return len ? min(max(len[b], 0), n) : n;
+}
+
+// Byte offset, from the first row of a tile, of logical chunk c of row r, or
+// kOutOfSlab for a chunk past the row's real length (a padded head dim).
+__device__ __forceinline__ uint32_t row_chunk_offset(int r, int c, int creal, uint32_t row_bytes) {
+  return c < creal ? (uint32_t)r * row_bytes + (uint32_t)c * 16u : kOutOfSlab;
+}
+
+// Resource over rows row0 .. row0 + kDiffTile - 1 of a head, of which `rows`
+// exist: the base is the tile's first row (64-bit), so a head may span more
+// than 4 GiB, and reads past the last row that exists return zeros. base is
+// the head's first row; every row is dreal elements, row_bytes apart.
+__device__ __forceinline__ rsrc_t tile_rsrc(const uint16_t* base, int row0, int n_rows, uint32_t row_bytes, int dreal) {
+  const int rows = min(max(n_rows - row0, 0), kDiffTile);
+  const uint32_t bytes = rows > 0 ? (uint32_t)(rows - 1) * row_bytes + (uint32_t)dreal * 2u : 0u;
+  return make_rsrc(reinterpret_cast<const char*>(base) + (long long)(rows > 0 ? row0 : 0) * row_bytes, bytes);
+}
+
+// Staging of a tile of three matrices A, B (DA columns each) and C (DC
+// columns), 32 rows each, by direct-to-LDS loads of NT threads: stage layout
+// [A | B | C], every matrix in the swizzled layout of kl_common.hpp. Pieces
+// of 64 chunks (one load instruction of a wave) never straddle matrices.
+template <int DA, int DC, int NT>
+struct DiffDma {
+  static constexpr int CA = DA / 8, CC = DC / 8;
+  static constexpr int CHUNKS = kDiffTile * (2 * CA + CC);
+  static constexpr int NCH = CHUNKS / NT;
+  static_assert(CHUNKS % NT == 0, "staging split");
+  uint32_t voff[NCH];
+
+  // which matrix chunk p of the stage belongs to
+  __device__ __forceinline__ static int matrix(int p) {
+    return p < kDiffTile * CA ? 0 : p < 2 * kDiffTile * CA ? 1 : 2;
+  }
+
+  __device__ __forceinline__ DiffDma(int tid, int da_real, int dc_real, uint32_t ba, uint32_t bb, uint32_t bc) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int p = tid + NT * i, m = matrix(p);
+      if (m < 2) {
+        const int pp = p - m * kDiffTile * CA;
+        const int r = pp / CA, c = (pp - r * CA) ^ swz<CA>(r);
+        voff[i] = row_chunk_offset(r, c, da_real / 8, m == 0 ? ba : bb);
+      } else {
+        const int pp = p - 2 * kDiffTile * CA;
+        const int r = pp / CC, c = (pp - r * CC) ^ swz<CC>(r);
+        voff[i] = row_chunk_offset(r, c, dc_real / 8, bc);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void issue(rsrc_t ra, rsrc_t rb, rsrc_t rc, u32x4* stage, int wave) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int m = matrix(NT * i + 64 * wave);   // uniform
+      const rsrc_t r = m == 0 ? ra : m == 1 ? rb : rc;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(stage + NT * i + 64 * wave), 16, voff[i], 0, 0, 0);
+    }
+#endif
+  }
+};
+
+// Byte offsets within a matrix of D columns of the transpose reads that
+// deliver, for 16-row block s, the 32 columns 32 nb + l % 32 of rows
+// 4 half + 0..3 (h = 0) and 8 + 4 half + 0..3 (h = 1): offset(nb, h) + 256 D / 8 s.
+// Computed once and hidden from the optimizer (see TrOffsets in kl_bwd.hpp).
+template <int D>
+struct TrCols {
+  static constexpr int CPR = D / 8, NB = D / 32;
+  int o[NB][2];
+  __device__ __forceinline__ explicit TrCols(int lane) {
+    const int half = lane >> 5;
+    const int row = 4 * half + ((lane & 15) >> 2);
+    const int col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const int e = 32 * nb + col;
+        o[nb][h] = opaque(chunk_slot<CPR>(row + 8 * h, e >> 3) * 16 + ((e >> 2) & 1) * 8);
+      }
+  }
+  // base: byte offset of the matrix in buf
+  __device__ __forceinline__ bf16x8 read(const void* buf, int base, int nb, int s) const {
+    return cat8(lds_tr4_at(buf, o[nb][0] + base + 256 * CPR * s), lds_tr4_at(buf, o[nb][1] + base + 256 * CPR * s));
+  }
+};
+
+// 16-byte chunks 2 ks + half of a row as MFMA operands; zeros past its end or
+// where the row does not exist.
+template <int D>
+__device__ __forceinline__ void load_row_operand(bf16x8 (&op)[D / 16], const uint16_t* row, bool ok, int half,
+                                                 int dreal) {
+  const u32x4* p = reinterpret_cast<const u32x4*>(row);
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) {
+    const int c = 2 * ks + half;
+    op[ks] = __builtin_bit_cast(bf16x8, ok && 8 * c < dreal ? p[c] : u32x4{0u, 0u, 0u, 0u});
+  }
+}
+
+}  // namespace streamkl

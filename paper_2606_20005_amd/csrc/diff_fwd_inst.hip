@@ -1,0 +1,145 @@
+// Instantiations of the differential-attention forward, the rule that picks
+// among them, and the kernel that joins split partials.
+#include "diff_fwd.hpp"
+#include "diff_launch.hpp"
+
+namespace streamkl {
+
+namespace {
+
+// Joins the partials of one output row (see diff_fwd.hpp). A quarter-column
+// group of four floats per lane; the groups of lanes share the splits.
+__global__ void __launch_bounds__(kThreads) diff_merge_kernel(const DiffArgs a) {
+  __shared__ float w[2][kDiffMaxSplits];
+  __shared__ float top[2], total[2];
+  __shared__ f32x4 acc[2][kThreads];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const long long row = blockIdx.x;
+  const int bh = (int)(row / a.NQ), i = (int)(row - (long long)bh * a.NQ), b = bh / a.H, h = bh - b * a.H;
+  const bool ok = i < clamp_len(a.q_len, b, a.NQ);
+  const int S = a.splits, cols = a.dv / 4;   // 8 to 64, a multiple of 8
+  const long long rows = (long long)a.B * a.H * a.NQ;
+  const float* po = a.part + row * S * 2 * a.dv;
+  const float* pm = a.part + rows * S * 2 * a.dv + row * S * 4;
+  if (wave < 2) {   // wave m: the joint reference and sum of map m
+    float t = kNegInf;
+    if (ok)
+      for (int s = lane; s < S; s += 64) t = fmaxf(t, pm[(s * 2 + wave) * 2]);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) t = fmaxf(t, __shfl_xor(t, x));
+    float sum = 0.f;
+    for (int s = lane; s < S; s += 64) {
+      float f = 0.f;
+      if (ok) {
+        const float r = pm[(s * 2 + wave) * 2];
+        f = r == kNegInf ? 0.f : exp2_fast(r - t);
+        sum = __builtin_fmaf(f, pm[(s * 2 + wave) * 2 + 1], sum);
+      }
+      w[wave][s] = f;
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+    if (lane == 0) {
+      top[wave] = t;
+      total[wave] = sum;
+    }
+  }
+  __syncthreads();
+  const int groups = kThreads / cols, grp = tid / cols, col = tid - grp * cols;
+  f32x4 o1 = {0.f, 0.f, 0.f, 0.f}, o2 = o1;
+  if (ok && grp < groups) {
+    for (int s = grp; s < S; s += groups) {
+      const f32x4* p = reinterpret_cast<const f32x4*>(po + (long long)s * 2 * a.dv);
+      o1 += p[col] * w[0][s];
+      o2 += p[cols + col] * w[1][s];
+    }
+  }
+  acc[0][tid] = o1;
+  acc[1][tid] = o2;
+  __syncthreads();
+  if (tid < cols) {
+    for (int g = 1; g < groups; ++g) {
+      o1 += acc[0][g * cols + tid];
+      o2 += acc[1][g * cols + tid];
+    }
+    auto inverse = [](float l) { return l > 0.f || l != l ? 1.f / l : 0.f; };
+    const float f1 = ok ? inverse(total[0]) : 0.f, f2 = ok ? inverse(total[1]) : 0.f, lam = a.lam[h];
+    bf16x4 r, r2;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float v2 = ok ? o2[j] * f2 : 0.f;
+      r2[j] = (__bf16)v2;
+      r[j] = (__bf16)(ok ? __builtin_fmaf(-lam, v2, o1[j] * f1) : 0.f);
+    }
+    *reinterpret_cast<bf16x4*>(a.out + row * a.dv + 4 * tid) = r;
+    if (a.out2) *reinterpret_cast<bf16x4*>(a.out2 + row * a.dv + 4 * tid) = r2;
+  }
+  if (tid < 2) {
+    float* lse = tid ? a.lse2 : a.lse1;
+    if (lse) lse[row] = !ok || top[tid] == kNegInf ? kNegInf : (log2f(total[tid]) + top[tid]) * kLn2;
+  }
+}
+
+template <int D, int DV, int RB, int NW>
+struct FwdPick {
+  using C = DiffFwdCfg<D, DV, RB, NW>;
+  static constexpr int rows() { return C::ROWS; }
+  static constexpr int resident() {
+    constexpr int lds = (C::STAGE + (C::STAGE > C::XCHG ? C::STAGE : C::XCHG)) * 16;
+    constexpr int by_lds = 160 * 1024 / lds, by_waves = 4 * C::WAVES / NW;
+    return kCus * (by_lds < by_waves ? by_lds : by_waves);
+  }
+  static hipError_t launch(const DiffArgs& a) {
+    const long long R = (long long)a.NQ * (a.H / a.HK);
+    const unsigned grid = (unsigned)((long long)a.B * a.HK * ((R + C::ROWS - 1) / C::ROWS));
+    hipLaunchKernelGGL((diff_fwd_kernel<D, DV, RB, NW>), dim3(grid, (unsigned)a.splits), dim3(C::NT), 0, a.stream, a);
+    return hipGetLastError();
+  }
+};
+
+// Rows of one pair of waves where there are few (a whole block would be
+// mostly padding, and short blocks leave more of them resident), 128-row
+// blocks otherwise.
+template <typename F>
+auto pick(int d, int dv, long long rows, F f) {
+  auto by_rows = [&](auto kd, auto kv) {
+    constexpr int D = kd.value, DV = kv.value;
+    if constexpr (DV == 256) {
+      if (rows <= 32) return f(FwdPick<D, DV, 1, 2>{});
+      return f(FwdPick<D, DV, 1, 4>{});
+    } else {
+    if (rows <= 32) return f(FwdPick<D, DV, 1, 2>{});
+    if (rows <= 64) return f(FwdPick<D, DV, 2, 2>{});
+    return f(FwdPick<D, DV, 2, 4>{});
+    }
+  };
+  auto by_dv = [&](auto kd) {
+    switch (diff_value_dim(dv)) {
+      case 64: return by_rows(kd, std::integral_constant<int, 64>{});
+      case 128: return by_rows(kd, std::integral_constant<int, 128>{});
+      default: return by_rows(kd, std::integral_constant<int, 256>{});
+    }
+  };
+  return diff_key_dim(d) == 64 ? by_dv(std::integral_constant<int, 64>{}) : by_dv(std::integral_constant<int, 128>{});
+}
+
+}  // namespace
+
+int diff_fwd_rows(int d, int dv, long long rows) {
+  return pick(d, dv, rows, [](auto p) { return p.rows(); });
+}
+
+int diff_fwd_resident(int d, int dv, long long rows) {
+  return pick(d, dv, rows, [](auto p) { return p.resident(); });
+}
+
+hipError_t launch_diff_fwd(const DiffArgs& a) {
+  return pick(a.d, a.dv, (long long)a.NQ * (a.H / a.HK), [&](auto p) { return p.launch(a); });
+}
+
+hipError_t launch_diff_merge(const DiffArgs& a) {
+  hipLaunchKernelGGL(diff_merge_kernel, dim3((unsigned)((long long)a.B * a.H * a.NQ)), dim3(kThreads), 0, a.stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace streamkl

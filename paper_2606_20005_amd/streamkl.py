@@ -29,7 +29,16 @@ ACT_SOFTMAX, ACT_SIGMOID = 0, 1
 ENTRY_POINTS = ("streamkl_fwd", "streamkl_bwd", "streamkl_bwd_ex", "streamkl_bwd_choose", "streamkl_fwd_split",
                 "streamkl_fwd_split_noalloc", "streamkl_fwd_split_workspace_bytes", "streamkl_fwd_split_count",
                 "streamkl_fwd_act", "streamkl_bwd_act", "streamkl_bwd_grads", "streamkl_strerror", "streamkl_version",
-                "streamkl_supported_head_dim")
+                "streamkl_supported_head_dim", "streamkl_qk_norm_rope_fwd", "streamkl_qk_norm_rope_bwd",
+                "streamkl_qk_norm_rope_bwd_workspace_bytes", "streamkl_diff_fwd", "streamkl_diff_fwd_split_count",
+                "streamkl_diff_fwd_workspace_bytes", "streamkl_diff_bwd", "streamkl_diff_bwd_workspace_bytes")
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class _Rows(ctypes.Structure):
+    """streamkl_rows: a [batch, head, row] arrangement of contiguous rows."""
+    _fields_ = [("data", ctypes.c_void_p), ("sb", ctypes.c_longlong), ("sh", ctypes.c_longlong),
+                ("sn", ctypes.c_longlong)]
 
 
 def _load():
@@ -64,6 +73,27 @@ def _load():
     lib.streamkl_fwd_split_workspace_bytes.restype = sz
     lib.streamkl_fwd_split_count.argtypes = [i, i, i, i, i, i]
     lib.streamkl_fwd_split_count.restype = i
+    rows = ctypes.POINTER(_Rows)
+    lib.streamkl_qk_norm_rope_fwd.argtypes = [rows, rows, i, i, i, i, i, i, i, vp, vp, f, vp, i, i, i, vp, vp, i, i, i,
+                                              i, vp, vp, vp]
+    lib.streamkl_qk_norm_rope_fwd.restype = i
+    lib.streamkl_qk_norm_rope_bwd.argtypes = [rows, rows, i, i, i, i, i, i, i, vp, vp, f, vp, i, i, i, vp, vp, i, i, i,
+                                              i, vp, vp, i, vp, sz, vp, vp, vp, vp, vp]
+    lib.streamkl_qk_norm_rope_bwd.restype = i
+    lib.streamkl_qk_norm_rope_bwd_workspace_bytes.argtypes = [i, i, i, i, i, i]
+    lib.streamkl_qk_norm_rope_bwd_workspace_bytes.restype = sz
+    lib.streamkl_diff_fwd.argtypes = [rows, rows, rows, rows, rows, i, i, i, i, i, i, i, f, i, vp, vp, vp, i, vp, sz,
+                                      vp, vp, vp, vp, vp]
+    lib.streamkl_diff_fwd.restype = i
+    lib.streamkl_diff_fwd_split_count.argtypes = [i, i, i, i, i, i, i]
+    lib.streamkl_diff_fwd_split_count.restype = i
+    lib.streamkl_diff_fwd_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.streamkl_diff_fwd_workspace_bytes.restype = sz
+    lib.streamkl_diff_bwd.argtypes = [rows, rows, rows, rows, rows, i, i, i, i, i, i, i, f, i, vp, vp, vp, vp, vp, vp,
+                                      vp, vp, vp, sz, vp, vp, vp, vp, vp, vp, i, vp]
+    lib.streamkl_diff_bwd.restype = i
+    lib.streamkl_diff_bwd_workspace_bytes.argtypes = [i, i, i]
+    lib.streamkl_diff_bwd_workspace_bytes.restype = sz
     lib.streamkl_strerror.argtypes = [i]
     lib.streamkl_strerror.restype = ctypes.c_char_p
     lib.streamkl_version.argtypes = []
@@ -411,3 +441,380 @@ def attention_kl(q1, k1, q2, k2, *, s1=None, s2=None, causal=False, direction="f
     kl, st1, st2 = _AttentionKL.apply(q1, k1, q2, k2, s1, s2, bool(causal), _direction(direction), bwd_strategy,
                                       _activation(activation))
     return (kl, st1, st2) if return_lse else kl
+
+
+# --- norms of queries and keys with the position rotation -------------------------------------------------------------
+
+
+def rope_table(n_pos, rot_dim, base=10000.0, device="cuda"):
+    """Cosines and sines of the positions 0 .. n_pos - 1 for qk_norm_rope: float32 [n_pos, rot_dim], the rot_dim/2
+    cosines of a position, then its sines. Pair i turns by p * base^(-2 i / rot_dim). The angles are formed in
+    64 bits (at position 100000 a float32 angle is off by up to 4e-3) and the values rounded once. A program lays this
+    out once."""
+    if rot_dim <= 0 or rot_dim % 16 != 0:
+        raise ValueError(f"rot_dim must be a positive multiple of 16, got {rot_dim}")
+    pos = torch.arange(int(n_pos), device=device, dtype=torch.float64)
+    freq = float(base) ** (torch.arange(0, rot_dim, 2, device=device, dtype=torch.float64) / -rot_dim)
+    angle = pos[:, None] * freq[None, :]
+    return torch.cat((angle.cos(), angle.sin()), 1).float().contiguous()
+
+
+def _rows(t, name, batch=0, head=1, row=2):
+    """A tensor with contiguous 16-byte aligned rows as a streamkl_rows; batch, head and row are its axes."""
+    es, shape, stride = t.element_size(), t.shape, t.stride()
+    if stride[3] != 1 and shape[3] != 1:
+        raise ValueError(f"{name} must be contiguous along its last axis")
+    ptr = t.data_ptr()
+    st = [0 if shape[a] <= 1 else stride[a] for a in (batch, head, row)]   # the stride of one element says nothing
+    if ptr % 16 or any(x * es % 16 for x in st):
+        raise ValueError(f"the rows of {name} must begin at multiples of 16 bytes")
+    return _Rows(ptr, *st)
+
+
+def _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k):
+    """Checked arguments of the norm-and-rotation calls: (device, B, H, HK, N_Q, N_K, d, n_pos, rot, copies)."""
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q and k are both None")
+    for n, t in (("q", q), ("k", k)):
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError(f"{n} must be a GPU tensor")
+        if t.dtype not in DTYPES:
+            raise ValueError(f"{n} must be bfloat16, float16 or float32, got {t.dtype}")
+        if t.dim() != 4:
+            raise ValueError(f"{n} must be a [B, N, H, d] tensor")
+        if t.dtype != first.dtype or t.device != first.device or t.shape[0] != first.shape[0] or \
+                t.shape[3] != first.shape[3]:
+            raise ValueError("q and k must have one type, device, batch and head dim")
+    dev, d = first.device, first.shape[3]
+    for n, w in (("wq", wq), ("wk", wk)):
+        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous() or
+                              w.device != dev):
+            raise ValueError(f"{n} must be a contiguous float32 tensor of shape {(d,)} on {dev}")
+    n_pos = rot = 0
+    if table is not None:
+        if table.dtype != torch.float32 or table.dim() != 2 or not table.is_contiguous() or table.device != dev:
+            raise ValueError(f"table must be a contiguous float32 [positions, rot_dim] tensor on {dev}")
+        n_pos, rot = table.shape
+        if rot <= 0 or rot > d or rot % 16:
+            raise ValueError(f"the table's rot_dim must be a multiple of 16 up to the head dim {d}, got {rot}")
+    B = first.shape[0]
+    NQ, H = (q.shape[1], q.shape[2]) if q is not None else (0, 0)
+    NK, HK = (k.shape[1], k.shape[2]) if k is not None else (0, 0)
+    for n, p, t, rows in (("q_positions", q_positions, q, NQ), ("k_positions", k_positions, k, NK)):
+        if p is None:
+            continue
+        if t is None:
+            raise ValueError(f"{n} given without {n[0]}")
+        if p.dtype not in (torch.int32, torch.int64) or tuple(p.shape) not in ((rows,), (B, rows)) or \
+                not p.is_contiguous() or p.device != dev:
+            raise ValueError(f"{n} must be a contiguous int32 or int64 tensor of shape {(rows,)} or {(B, rows)} on "
+                             f"{dev}")
+    if q_positions is not None and k_positions is not None and q_positions.dtype != k_positions.dtype:
+        raise ValueError("q_positions and k_positions must have one type")
+    if table is not None and q is not None and k is not None and q_positions is None and NQ > NK:
+        raise ValueError("more queries than keys: their positions have to be given")
+    copies = 1
+    if expand_k:
+        if q is None or k is None or HK == 0 or H % HK:
+            raise ValueError("expand_k needs q and k, with whole groups of query heads per key head")
+        copies = H // HK
+    return dev, B, H, HK, NQ, NK, d, n_pos, rot, copies
+
+
+def _prep_args(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, cfg):
+    """The arguments that the forward and backward calls share."""
+    _, B, H, HK, NQ, NK, d, n_pos, rot, copies = cfg
+    pos = q_positions if q_positions is not None else k_positions
+    return (None if q is None else _rows(q, "q", 0, 2, 1), None if k is None else _rows(k, "k", 0, 2, 1), B, H, HK, NQ,
+            NK, d, DTYPES[(q if q is not None else k).dtype], _p(wq), _p(wk), float(eps), _p(table), n_pos, rot,
+            int(bool(interleaved)), _p(q_positions), _p(k_positions),
+            int(pos is not None and pos.dtype == torch.int64), int(q_positions is not None and q_positions.dim() == 1),
+            int(k_positions is not None and k_positions.dim() == 1), copies)
+
+
+def qk_norm_rope_fwd(q, k, wq=None, wk=None, table=None, eps=1e-6, q_positions=None, k_positions=None,
+                     interleaved=False, expand_k=False, out=None):
+    """streamkl_qk_norm_rope_fwd: (yq, yk), bf16 [B, H, N, d]; None for a side that is None. See qk_norm_rope.
+    ``out`` may hold the two outputs, preallocated."""
+    cfg = _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k)
+    dev, B, H, HK, NQ, NK, d, _, _, copies = cfg
+    shapes = (None if q is None else (B, H, NQ, d), None if k is None else (B, HK * copies, NK, d))
+    ys = []
+    for n, shape, t in zip(("yq", "yk"), shapes, out or (None, None)):
+        if shape is not None and t is not None and (t.dtype != torch.bfloat16 or tuple(t.shape) != shape or
+                                                    not t.is_contiguous() or t.device != dev):
+            raise ValueError(f"{n} must be a contiguous bfloat16 tensor of shape {shape} on {dev}")
+        ys.append(None if shape is None else t if t is not None else torch.empty(shape, dtype=torch.bfloat16,
+                                                                                 device=dev))
+    args = _prep_args(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, cfg)
+    with _on(dev):
+        st = lib.streamkl_qk_norm_rope_fwd(*args, _p(ys[0]), _p(ys[1]), _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_qk_norm_rope_fwd")
+    return tuple(ys)
+
+
+def qk_norm_rope_bwd(q, k, dyq, dyk, wq=None, wk=None, table=None, eps=1e-6, q_positions=None, k_positions=None,
+                     interleaved=False, expand_k=False, want_w=True, workspace=None):
+    """streamkl_qk_norm_rope_bwd: (dq, dk, dwq, dwk) from the upstream gradients dyq, dyk (contiguous, both bf16 or both
+    float32, in the layout of the outputs); dq and dk in the inputs' type, dwq and dwk float32 (None unless
+    ``want_w``). The workspace is allocated here unless given."""
+    cfg = _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k)
+    dev, B, H, HK, NQ, NK, d, _, _, copies = cfg
+    shapes = (None if q is None else (B, H, NQ, d), None if k is None else (B, HK * copies, NK, d))
+    kind = (dyq if q is not None else dyk).dtype
+    for n, shape, t in zip(("dyq", "dyk"), shapes, (dyq, dyk)):
+        if (shape is None) != (t is None):
+            raise ValueError(f"{n} must be given exactly where {n[-1]} is")
+        if t is not None and (t.dtype not in (torch.bfloat16, torch.float32) or t.dtype != kind or
+                              tuple(t.shape) != shape or not t.is_contiguous() or t.device != dev):
+            raise ValueError(f"{n} must be a contiguous bfloat16 or float32 tensor of shape {shape} on {dev}, of one "
+                             "type with the other")
+    dx = [None if t is None else torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k)]
+    dw = [None if t is None or not want_w else torch.empty(d, dtype=torch.float32, device=dev) for t in (q, k)]
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+    elif want_w:
+        ws_bytes = lib.streamkl_qk_norm_rope_bwd_workspace_bytes(B, H, HK, NQ, NK, d)
+        workspace = torch.empty(max(ws_bytes, 4), dtype=torch.uint8, device=dev)
+    args = _prep_args(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, cfg)
+    with _on(dev):
+        st = lib.streamkl_qk_norm_rope_bwd(*args, _p(dyq), _p(dyk), DTYPES[kind], _p(workspace), ws_bytes, _p(dx[0]),
+                                           _p(dx[1]), _p(dw[0]), _p(dw[1]), _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_qk_norm_rope_bwd")
+    return dx[0], dx[1], dw[0], dw[1]
+
+
+class _QKNormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k):
+        ctx.save_for_backward(q, k, wq, wk, table, q_positions, k_positions)
+        ctx.cfg = (eps, interleaved, expand_k)
+        ctx.set_materialize_grads(False)
+        return qk_norm_rope_fwd(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k)
+
+    @staticmethod
+    def backward(ctx, gq, gk):
+        q, k, wq, wk, table, q_positions, k_positions = ctx.saved_tensors
+        eps, interleaved, expand_k = ctx.cfg
+        need = ctx.needs_input_grad
+        # an output that the loss does not reach has no gradient; the positions of the other do not change by that
+        if gq is not None:
+            gq = gq.contiguous()
+        if gk is not None:
+            gk = gk.contiguous()
+        if gq is not None and gk is not None and gq.dtype != gk.dtype:
+            gq, gk = gq.float(), gk.float()
+        if gq is None and gk is None:
+            return (None,) * 10
+        if (gq is None or gk is None) and q is not None and k is not None:
+            return (*_one_side(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k),
+                    *(None,) * 6)
+        dq, dk, dwq, dwk = qk_norm_rope_bwd(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved,
+                                            expand_k, want_w=need[2] or need[3])
+        return (dq if need[0] else None, dk if need[1] else None, dwq if need[2] else None, dwk if need[3] else None,
+                *(None,) * 6)
+
+
+def _one_side(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k):
+    """Gradients where only one of the two outputs has an upstream gradient: the other's is zero."""
+    if gq is None:
+        gq = torch.zeros((q.shape[0], q.shape[2], q.shape[1], q.shape[3]), dtype=gk.dtype, device=q.device)
+    else:
+        heads = q.shape[2] if expand_k else k.shape[2]
+        gk = torch.zeros((k.shape[0], heads, k.shape[1], k.shape[3]), dtype=gq.dtype, device=k.device)
+    dq, dk, dwq, dwk = qk_norm_rope_bwd(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved,
+                                        expand_k)
+    return dq, dk, None if wq is None else dwq, None if wk is None else dwk
+
+
+def qk_norm_rope(q, k, wq=None, wk=None, table=None, *, eps=1e-6, q_positions=None, k_positions=None,
+                 interleaved=False, expand_k=False):
+    """Norm of every query and key head and the rotation by its position, differentiable; one kernel.
+
+    q [B, N_Q, H, d] and k [B, N_K, HK, d] as their projections leave them (bfloat16, float16 or float32; any strides
+    with a contiguous last axis), either may be None. Returns yq [B, H, N_Q, d] and yk [B, HK, N_K, d] in bf16,
+    contiguous, as attention_kl and diff_attention read them:
+        n = x / sqrt(mean(x^2) + eps) * w,   then the pairs of the first rot_dim columns turned by the token's position.
+
+    wq, wk: float32 [d] or None (ones). table: rope_table(...), or None for the norm alone. q_positions, k_positions:
+    int32 or int64 [N] or [B, N]; by default keys stand at 0 .. N_K - 1 and queries are the last N_Q of these places,
+    as everywhere in this library. A position outside the table gives NaN rows. interleaved: pairs (2j, 2j + 1) instead
+    of (j, j + rot_dim/2). expand_k: write every key head once per query head of its group, so that yk has H heads (the
+    gradients of the copies are added).
+    """
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, wq, wk)):
+        return _QKNormRope.apply(q, k, wq, wk, table, float(eps), q_positions, k_positions, bool(interleaved),
+                                 bool(expand_k))
+    return qk_norm_rope_fwd(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k)
+
+
+# --- differential attention -------------------------------------------------------------------------------------------
+
+
+def _diff_inputs(q1, k1, q2, k2, v, lam, q_len, kv_len):
+    """Checked extents of the differential-attention calls: (device, (B, H, HK, N_Q, N_K, d, dv))."""
+    for n, t in (("q1", q1), ("k1", k1), ("q2", q2), ("k2", k2), ("v", v)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError(f"{n} must be a GPU tensor")
+        if t.dtype != torch.bfloat16:
+            raise ValueError(f"{n} must be bfloat16, got {t.dtype}")
+        if t.dim() != 4:
+            raise ValueError(f"{n} must be a [B, H, N, d] tensor")
+    B, H, NQ, d = q1.shape
+    HK, NK = k1.shape[1:3]
+    dv = v.shape[3]
+    if q2.shape != q1.shape or k2.shape != k1.shape or k1.shape[0] != B or k1.shape[3] != d or \
+            tuple(v.shape) != (B, HK, NK, dv):
+        raise ValueError(f"inconsistent shapes q1{tuple(q1.shape)} k1{tuple(k1.shape)} q2{tuple(q2.shape)} "
+                         f"k2{tuple(k2.shape)} v{tuple(v.shape)}")
+    if (HK == 0) != (H == 0) or (HK and H % HK):
+        raise ValueError(f"{H} query heads do not share {HK} key heads evenly")
+    dev = q1.device
+    if any(t.device != dev for t in (k1, q2, k2, v)):
+        raise ValueError("all inputs must be on one device")
+    _f32_rows(lam, (H,), dev, "lam")
+    for n, t in (("q_len", q_len), ("kv_len", kv_len)):
+        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_contiguous() or
+                              t.device != dev):
+            raise ValueError(f"{n} must be a contiguous int32 tensor of shape {(B,)} on {dev}")
+    return dev, (B, H, HK, NQ, NK, d, dv)
+
+
+def _diff_scale(scale, d):
+    return 1.0 / math.sqrt(d) if scale is None else float(scale)
+
+
+def diff_split_count(B, H, HK, n_q, n_k, d, dv) -> int:
+    """streamkl_diff_fwd_split_count (0 for invalid arguments)."""
+    return int(lib.streamkl_diff_fwd_split_count(int(B), int(H), int(HK), int(n_q), int(n_k), int(d), int(dv)))
+
+
+def diff_workspace_bytes(B, H, n_q, dv, splits) -> int:
+    """streamkl_diff_fwd_workspace_bytes: workspace of the split forward."""
+    return int(lib.streamkl_diff_fwd_workspace_bytes(int(B), int(H), int(n_q), int(dv), int(splits)))
+
+
+def diff_bwd_workspace_bytes(B, H, n_q) -> int:
+    """streamkl_diff_bwd_workspace_bytes: workspace of the backward."""
+    return int(lib.streamkl_diff_bwd_workspace_bytes(int(B), int(H), int(n_q)))
+
+
+def _bf16_out(t, shape, dev, name):
+    if t is None:
+        return torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name} must be a contiguous bfloat16 tensor of shape {shape} on {dev}")
+    return t
+
+
+def diff_fwd(q1, k1, q2, k2, v, lam, scale=None, causal=False, q_len=None, kv_len=None, splits="auto", save=False,
+             out=None, workspace=None):
+    """streamkl_diff_fwd: the output, bf16 [B, H, N_Q, dv], or with ``save`` (out, out2, lse1, lse2), what diff_bwd
+    needs. See diff_attention. splits: an int >= 1 or "auto" (diff_split_count). ``out`` may be a preallocated output;
+    the split workspace is allocated here unless ``workspace`` (diff_workspace_bytes) is given."""
+    dev, ext = _diff_inputs(q1, k1, q2, k2, v, lam, q_len, kv_len)
+    B, H, HK, NQ, NK, d, dv = ext
+    n = lib.streamkl_diff_fwd_split_count(*ext) or 1 if splits == "auto" else int(splits)
+    out = _bf16_out(out, (B, H, NQ, dv), dev, "out")
+    out2 = lse1 = lse2 = None
+    if save:
+        out2 = torch.empty((B, H, NQ, dv), dtype=torch.bfloat16, device=dev)
+        lse1, lse2 = torch.empty((2, B, H, NQ), dtype=torch.float32, device=dev).unbind(0)
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+    elif n > 1:
+        ws_bytes = lib.streamkl_diff_fwd_workspace_bytes(B, H, NQ, dv, n)
+        workspace = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=dev)
+    with _on(dev):
+        st = lib.streamkl_diff_fwd(_rows(q1, "q1"), _rows(k1, "k1"), _rows(q2, "q2"), _rows(k2, "k2"), _rows(v, "v"),
+                                   *ext, _diff_scale(scale, d), int(bool(causal)), _p(lam), _p(q_len), _p(kv_len), n,
+                                   _p(workspace), ws_bytes, _p(out), _p(out2), _p(lse1), _p(lse2), _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_diff_fwd")
+    return (out, out2, lse1, lse2) if save else out
+
+
+DIFF_GRADS = ("dq1", "dk1", "dq2", "dk2", "dv", "dlam")
+
+
+def diff_bwd(q1, k1, q2, k2, v, lam, dout, out, out2, lse1, lse2, scale=None, causal=False, q_len=None, kv_len=None,
+             want=DIFF_GRADS, grad_dtype=torch.float32, workspace=None):
+    """streamkl_diff_bwd: (dq1, dk1, dq2, dk2, dv, dlam), None where not in ``want``; from dout (bf16, contiguous) and
+    the results of diff_fwd(..., save=True). grad_dtype: float32 or bfloat16 (dlam is float32 always)."""
+    dev, ext = _diff_inputs(q1, k1, q2, k2, v, lam, q_len, kv_len)
+    B, H, HK, NQ, NK, d, dv = ext
+    unknown = set(want) - set(DIFF_GRADS)
+    if unknown or not want:
+        raise ValueError(f"want must name some of {DIFF_GRADS}, got {sorted(want)}")
+    if grad_dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"grad_dtype must be float32 or bfloat16, got {grad_dtype}")
+    for n, t in (("dout", dout), ("out", out), ("out2", out2)):
+        if t is None:
+            raise ValueError(f"{n} is missing")
+        _bf16_out(t, (B, H, NQ, dv), dev, n)
+    for n, t in (("lse1", lse1), ("lse2", lse2)):
+        if t is None:
+            raise ValueError(f"{n} is missing")
+        _f32_rows(t, (B, H, NQ), dev, n)
+    shapes = {"dq1": (B, H, NQ, d), "dk1": (B, HK, NK, d), "dq2": (B, H, NQ, d), "dk2": (B, HK, NK, d),
+              "dv": (B, HK, NK, dv), "dlam": (H,)}
+    g = {n: torch.empty(s, dtype=torch.float32 if n == "dlam" else grad_dtype, device=dev) if n in want else None
+         for n, s in shapes.items()}
+    if workspace is None:
+        ws_bytes = lib.streamkl_diff_bwd_workspace_bytes(B, H, NQ)
+        workspace = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=dev)
+    else:
+        ws_bytes = workspace.numel() * workspace.element_size()
+    with _on(dev):
+        st = lib.streamkl_diff_bwd(_rows(q1, "q1"), _rows(k1, "k1"), _rows(q2, "q2"), _rows(k2, "k2"), _rows(v, "v"),
+                                   *ext, _diff_scale(scale, d), int(bool(causal)), _p(lam), _p(q_len), _p(kv_len),
+                                   _p(dout), _p(out), _p(out2), _p(lse1), _p(lse2), _p(workspace), ws_bytes,
+                                   *(_p(g[n]) for n in DIFF_GRADS), int(grad_dtype == torch.bfloat16), _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_diff_bwd")
+    return tuple(g[n] for n in DIFF_GRADS)
+
+
+class _DiffAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q1, k1, q2, k2, v, lam, scale, causal, q_len, kv_len):
+        saved = diff_fwd(q1, k1, q2, k2, v, lam, scale, causal, q_len, kv_len, save=True)
+        ctx.save_for_backward(q1, k1, q2, k2, v, lam, q_len, kv_len, *saved)
+        ctx.cfg = (scale, causal)
+        return saved[0]
+
+    @staticmethod
+    def backward(ctx, dout):
+        q1, k1, q2, k2, v, lam, q_len, kv_len, *saved = ctx.saved_tensors
+        scale, causal = ctx.cfg
+        want = tuple(n for n, need in zip(DIFF_GRADS, ctx.needs_input_grad) if need)
+        if not want:
+            return (None,) * 10
+        grads = diff_bwd(q1, k1, q2, k2, v, lam, dout.to(torch.bfloat16).contiguous(), *saved, scale, causal, q_len,
+                         kv_len, want=want, grad_dtype=torch.bfloat16)
+        return (*grads, None, None, None, None)
+
+
+def diff_attention(q1, k1, q2, k2, v, lam, *, scale=None, causal=False, q_len=None, kv_len=None):
+    """Differential attention, (softmax(scale q1 k1^T) - lam_h softmax(scale q2 k2^T)) v, differentiable.
+
+    q1, q2 [B, H, N_Q, d], k1, k2 [B, HK, N_K, d], v [B, HK, N_K, dv], bf16 with contiguous 16-byte aligned rows in any
+    arrangement (halves of one projection, values as their projection leaves them, the filled part of a cache). H is a
+    multiple of HK: groups of H / HK query heads share keys and values. lam float32 [H]. Returns bf16 [B, H, N_Q, dv],
+    contiguous; gradients come in the inputs' types.
+
+    causal: bottom-right alignment, as everywhere in this library. q_len, kv_len: int32 [B] on the device; sequence b
+    has its first q_len[b] rows and kv_len[b] keys (a right-padded batch, caches filled to different lengths). Rows
+    behind q_len and rows that see no key give 0. scale defaults to 1/sqrt(d).
+    """
+    scale = _diff_scale(scale, q1.shape[-1])
+    if torch.is_grad_enabled() and any(t.requires_grad for t in (q1, k1, q2, k2, v, lam)):
+        return _DiffAttention.apply(q1, k1, q2, k2, v, lam, scale, bool(causal), q_len, kv_len)
+    return diff_fwd(q1, k1, q2, k2, v, lam, scale, causal, q_len, kv_len)
