@@ -492,8 +492,9 @@ int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k1, const st
                       void* dq1, void* dk1, void* dq2, void* dk2, void* dvalues, float* dlam,
                       int bf16_grads, hipStream_t stream);
 
-/* Workspace bytes of streamkl_diff_bwd; 0 for negative extents. */
-size_t streamkl_diff_bwd_workspace_bytes(int B, int H, int N_Q);
+/* Workspace bytes of streamkl_diff_bwd (row statistics, and partial gradients where the library cuts the streamed
+   axis into ranges to fill the chip); 0 for invalid or unsupported extents. */
+size_t streamkl_diff_bwd_workspace_bytes(int B, int H, int HK, int N_Q, int N_K, int d, int dv, int causal);
 
 /* Static description of a status code. Never NULL. */
 const char* streamkl_strerror(int status);

@@ -38,7 +38,8 @@ CFLAGS = [
 # The pipelined backward keeps one wave per SIMD with all 512 registers, where the compiler by default lets every MFMA
 # write the upper half, which vector instructions cannot read: each logit would be copied down first. This form keeps
 # the logits in the lower half and leaves the resident rows to the upper one.
-UNIT_FLAGS = {"kl_bwd_pipe_": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+_VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+UNIT_FLAGS = {p: _VGPR_FORM for p in ("kl_bwd_pipe_", "diff_fwd_", "diff_bwd_dq_", "diff_bwd_dkv_")}
 
 
 def unit_flags(src: str) -> list[str]:

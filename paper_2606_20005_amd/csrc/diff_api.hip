@@ -83,6 +83,52 @@ int check_inputs(const streamkl_rows* q1, const streamkl_rows* k1, const streamk
   return STREAMKL_OK;
 }
 
+// Ranges of the streamed axis in the backward kernels. A kernel's blocks own
+// 128 rows (keys) and walk over all keys (rows) of their head; where that
+// leaves the chip unevenly filled, the walk is cut into ranges whose partial
+// float32 gradients a further kernel adds up. The number of ranges is the one
+// with the least estimated time: rounds of resident workgroups times steps,
+// about 0.042 us an MFMA and resident wave of a SIMD (measured 0.038 to 0.048), and the
+// partials written and read back at 4 TB/s. Measured (us, split against not):
+// see diff_bwd.hpp.
+struct GradSplits {
+  int q, k;
+  size_t part_floats;
+};
+
+int grad_splits(long long blocks, int waves, long long steps, bool causal, int mfmas, double bytes) {
+  const double slots = 256.0 * waves, us = 0.042 * mfmas * waves;
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= streamkl::kDiffMaxGradSplits; ++s) {
+    if (s > 1 && steps < 4LL * s) break;
+    const double rounds = (double)blocks * s / slots, each = (double)steps / s;
+    // causal blocks are handed out longest first and are half as long on average
+    const double filled = std::ceil(rounds) * each, even = 0.5 * rounds * each;
+    double t = (causal ? (even > each ? even : each) : rounds > 8 ? rounds * each : filled) * us;
+    if (s > 1) t += (s + 1) * bytes / 4e6 + 8.0;
+    if (s == 1 || t < 0.95 * least) {
+      best = s;
+      least = t;
+    }
+  }
+  return best;
+}
+
+GradSplits bwd_splits(int B, int H, int HK, int N_Q, int N_K, int d, int dv, int causal) {
+  GradSplits g = {1, 1, 0};
+  if ((long long)B * H * N_Q == 0 || (long long)B * HK * N_K == 0) return g;
+  const int kd = d <= 64 ? 64 : 128, kv = (dv + 63) / 64 * 64;
+  const long long q_floats = 2LL * B * H * N_Q * d, k_floats = (long long)B * HK * N_K * (2 * d + dv);
+  g.q = grad_splits((long long)B * H * streamkl::diff_row_blocks(N_Q), streamkl::diff_bwd_dq_waves(d, dv),
+                    (N_K + 31LL) / 32, causal != 0, kd / 4 + kv / 16, 4.0 * q_floats);
+  g.k = grad_splits((long long)B * HK * streamkl::diff_row_blocks(N_K), streamkl::diff_bwd_dkv_waves(d, dv),
+                    (long long)(H / HK) * ((N_Q + 31LL) / 32), causal != 0, kd / 4 + kv / 8, 4.0 * k_floats);
+  const long long q_part = g.q > 1 ? g.q * q_floats : 0, k_part = g.k > 1 ? g.k * k_floats : 0;
+  g.part_floats = (size_t)(q_part > k_part ? q_part : k_part);
+  return g;
+}
+
 int hip_status(hipError_t e) { return e == hipSuccess ? STREAMKL_OK : STREAMKL_ERR_HIP; }
 
 }  // namespace
@@ -133,9 +179,11 @@ extern "C" int streamkl_diff_fwd(const streamkl_rows* q1, const streamkl_rows* k
   return hip_status(e);
 }
 
-extern "C" size_t streamkl_diff_bwd_workspace_bytes(int B, int H, int N_Q) {
-  if (B < 0 || H < 0 || N_Q < 0) return 0;
-  return (streamkl::diff_bwd_stats_floats(B, H, N_Q) + streamkl::diff_bwd_dlam_floats(B, H, N_Q)) * sizeof(float);
+extern "C" size_t streamkl_diff_bwd_workspace_bytes(int B, int H, int HK, int N_Q, int N_K, int d, int dv, int causal) {
+  if (check_extents(B, H, HK, N_Q, N_K, d, dv) != STREAMKL_OK) return 0;
+  const GradSplits g = bwd_splits(B, H, HK, N_Q, N_K, d, dv, causal);
+  return (streamkl::diff_bwd_stats_floats(B, H, N_Q) + streamkl::diff_bwd_dlam_floats(B, H, N_Q, g.q) + g.part_floats) *
+         sizeof(float);
 }
 
 extern "C" int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k1, const streamkl_rows* q2,
@@ -159,7 +207,8 @@ extern "C" int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k
   if (rows) {
     if (!dout || !out || !out2 || !lse1 || !lse2) return STREAMKL_ERR_INVALID_ARG;
     if (!aligned(dout, 16) || !aligned(out, 16) || !aligned(out2, 16)) return STREAMKL_ERR_INVALID_ARG;
-    if (!workspace || !aligned(workspace, 16) || workspace_bytes < streamkl_diff_bwd_workspace_bytes(B, H, N_Q))
+    if (!workspace || !aligned(workspace, 16) || 
+        workspace_bytes < streamkl_diff_bwd_workspace_bytes(B, H, HK, N_Q, N_K, d, dv, causal))
       return STREAMKL_ERR_INVALID_ARG;
   }
   a.dout = static_cast<const uint16_t*>(dout);
@@ -168,7 +217,13 @@ extern "C" int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k
   a.lse1 = const_cast<float*>(lse1);
   a.lse2 = const_cast<float*>(lse2);
   a.stats = static_cast<float*>(workspace);
-  a.dlam_part = a.stats ? a.stats + streamkl::diff_bwd_stats_floats(B, H, N_Q) : nullptr;
+  const GradSplits g = bwd_splits(B, H, HK, N_Q, N_K, d, dv, causal);
+  a.q_splits = g.q;
+  a.k_splits = g.k;
+  if (a.stats) {
+    a.dlam_part = a.stats + streamkl::diff_bwd_stats_floats(B, H, N_Q);
+    a.grad_part = a.dlam_part + streamkl::diff_bwd_dlam_floats(B, H, N_Q, g.q);
+  }
   a.dq1 = dq1;
   a.dk1 = dk1;
   a.dq2 = dq2;
@@ -179,7 +234,9 @@ extern "C" int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k
   hipError_t e = hipSuccess;
   if (rows) e = streamkl::launch_diff_bwd_prep(a);
   if (e == hipSuccess && keys && of_keys) e = streamkl::launch_diff_bwd_dkv(a);   // without rows: zeros
+  if (e == hipSuccess && keys && of_keys && g.k > 1) e = streamkl::launch_diff_bwd_join_k(a);
   if (e == hipSuccess && rows && of_rows) e = streamkl::launch_diff_bwd_dq(a);
+  if (e == hipSuccess && rows && of_rows && g.q > 1) e = streamkl::launch_diff_bwd_join_q(a);
   if (e == hipSuccess && dlam && H > 0) e = streamkl::launch_diff_bwd_dlam(a);
   return hip_status(e);
 }

@@ -34,15 +34,20 @@ namespace streamkl {
 
 constexpr int kDiffStatsTile = 4 * kDiffTile;   // floats per tile
 
-template <int D, int DV>
+template <int D, int DV, int PART = 3>
 struct DiffBwdCfg {
   static constexpr int NW = 4, NT = 64 * NW, ROWS = 32 * NW;
   static constexpr int CD = D / 8, CV = DV / 8;
   static constexpr int STAGE = DiffDma<D, DV, NT>::CHUNKS;
+  static constexpr int STATS = kDiffStatsTile / 4;   // chunks of prepared statistics behind a stage (dK, dV)
   // registers: gradients, resident rows, three logit tiles, about 64 for the rest
   static constexpr int REGS_Q = D + (2 * D + DV) / 4 + 48 + 64;
-  static constexpr int REGS_K = D + DV / 2 + (2 * D + DV) / 4 + 48 + 64;
+  static constexpr int REGS_K = (PART & 1 ? D + DV / 4 + 16 : 0) + (PART & 2 ? DV / 2 : 0) + D / 2 + 32 + 64;
   static constexpr int WAVES_Q = REGS_Q <= 256 ? 2 : 1, WAVES_K = REGS_K <= 256 ? 2 : 1;
+  static constexpr int LA_Q = WAVES_Q == 1 ? 4 : 3, LA_K = WAVES_K == 1 ? 4 : 2;   // operand reads in flight
+  // three stages where the workgroups that the registers leave room for have room for them too
+  static constexpr int STAGES_Q = 3 * STAGE * 16 * WAVES_Q <= 158 * 1024 ? 3 : 2;
+  static constexpr int STAGES_K = 3 * (STAGE + STATS) * 16 * WAVES_K <= 158 * 1024 ? 3 : 2;
 };
 
 // One 32 x 32 block of raw products streamed x resident: A = rows of the
@@ -62,8 +67,10 @@ __device__ __forceinline__ f32x16 diff_product(const u32x4* tile, const bf16x8 (
 template <int D, int DV>
 __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_bwd_dq_kernel(const DiffArgs a) {
   using C = DiffBwdCfg<D, DV>;
+  constexpr int KD = D / 16, KV = DV / 16, ND = D / 32;
   __shared__ u32x4 st0[C::STAGE];
   __shared__ u32x4 st1[C::STAGE];
+  __shared__ u32x4 st2[C::STAGES_Q == 3 ? C::STAGE : 1];
   __shared__ float red[C::NW];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -83,7 +90,12 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
   const float c = a.scale * kLog2e;
   auto limit_of = [&](int i) { return a.causal ? min(max(off + i + 1, 0), klen) : klen; };
   const int r0 = blk * C::ROWS, rw = r0 + 32 * wave, row = rw + (lane & 31);
-  const int t_end = r0 < qlen ? (limit_of(min(r0 + C::ROWS, qlen) - 1) + kDiffTile - 1) / kDiffTile : 0;
+  int t_end = r0 < qlen ? (limit_of(min(r0 + C::ROWS, qlen) - 1) + kDiffTile - 1) / kDiffTile : 0, t_begin = 0;
+  if (a.q_splits > 1) {
+    const int each = (t_end + a.q_splits - 1) / a.q_splits;
+    t_begin = min(t_end, (int)blockIdx.y * each);
+    t_end = min(t_end, t_begin + each);
+  }
   const int wave_min = limit_of(rw), wave_max = rw < qlen ? limit_of(min(rw + 32, qlen) - 1) : 0;
 
   const bool ok = row < qlen;
@@ -123,68 +135,112 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
   const uint16_t* vv = a.v.p + (long long)b * a.v.sb + (long long)hk * a.v.sh;
   const DiffDma<D, DV, C::NT> dma(tid, a.d, a.dv, bk1, bk2, bv);
   const TrCols<D> tr(lane);
+  TileRows r1(k1, bk1, a.d), r2(k2, bk2, a.d), r3(vv, bv, a.dv);
+  r1.skip(t_begin);
+  r2.skip(t_begin);
+  r3.skip(t_begin);
   auto load = [&](int t, u32x4* stage) {
-    dma.issue(tile_rsrc(k1, t * kDiffTile, klen, bk1, a.d), tile_rsrc(k2, t * kDiffTile, klen, bk2, a.d),
-              tile_rsrc(vv, t * kDiffTile, klen, bv, a.dv), stage, wave);
+    const int rows = klen - t * kDiffTile;
+    dma.issue(r1.next(rows), r2.next(rows), r3.next(rows), stage, wave);
   };
 
-  auto tile = [&](const u32x4* stage, int t) {
+  auto tile = [&](int t, const u32x4* stage) {
     const int k0 = t * kDiffTile;
     if (k0 >= wave_max) return;
-    f32x16 s1 = diff_product<D>(stage, q1, lane);
-    f32x16 s2 = diff_product<D>(stage + kDiffTile * C::CD, q2, lane);
-    const f32x16 dp = diff_product<DV>(stage + 2 * kDiffTile * C::CD, go, lane);
-    if (k0 + kDiffTile > wave_min) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const bool seen = k0 + 8 * (i >> 2) + 4 * half + (i & 3) < limit;
-        s1[i] = seen ? s1[i] : kNegInf;
-        s2[i] = seen ? s2[i] : kNegInf;
-      }
-    }
+    constexpr int J1 = KD, J2 = J1 + KD, J3 = J2 + KV, J4 = J3 + 4 * ND, LA = C::LA_Q;
+    bf16x8 buf[J4];   // streamed operands, read LA of them ahead of their MFMAs
+    auto rd = [&](int j) {
+      if (j < J2) buf[j] = lds_row8<C::CD>(stage + j / KD * kDiffTile * C::CD, lane & 31, 2 * (j % KD) + half);
+      else if (j < J3) buf[j] = lds_row8<C::CV>(stage + 2 * kDiffTile * C::CD, lane & 31, 2 * (j - J2) + half);
+      else if (j < J4)   // [k-block][map][columns]
+        buf[j] = tr.read(stage, (j - J3) / ND % 2 * kDiffTile * C::CD * 16, (j - J3) % ND, (j - J3) / (2 * ND));
+    };
+    f32x16 s1 = zero16(), s2 = zero16(), dp = zero16();
     float e1[16], e2[16];
+    const bool mask = k0 + kDiffTile > wave_min;
+    auto hide = [&](f32x16& s) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float p1 = exp2_fast(__builtin_fmaf(s1[i], c, -ls1)), p2 = exp2_fast(__builtin_fmaf(s2[i], c, -ls2));
-      e1[i] = p1 * (dp[i] - d1);
-      e2[i] = p2 * (dp[i] - d2);
-      dl = __builtin_fmaf(p2, dp[i], dl);
+      for (int i = 0; i < 16; ++i) s[i] = k0 + 8 * (i >> 2) + 4 * half + (i & 3) < limit ? s[i] : kNegInf;
+    };
+    diff_pin();
+#pragma unroll
+    for (int j = 0; j < LA; ++j) rd(j);
+    diff_pin();
+#pragma unroll
+    for (int j = 0; j < J1; ++j) {
+      rd(j + LA);
+      s1 = mfma32(buf[j], q1[j], s1);
+      diff_pin();
     }
+    if (mask) hide(s1);
+    diff_pin();
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const bf16x8 a1 = pack8(e1 + 8 * u), a2 = pack8(e2 + 8 * u);
+    for (int j = J1; j < J2; ++j) {
+      rd(j + LA);
+      s2 = mfma32(buf[j], q2[j - J1], s2);
 #pragma unroll
-      for (int n = 0; n < D / 32; ++n) g1[n] = mfma32(a1, tr.read(stage, 0, n, u), g1[n]);
+      for (int i = 16 * (j - J1) / KD; i < 16 * (j - J1 + 1) / KD; ++i)
+        e1[i] = exp2_fast(__builtin_fmaf(s1[i], c, -ls1));
+      diff_pin();
+    }
+    if (mask) hide(s2);
+    diff_pin();
 #pragma unroll
-      for (int n = 0; n < D / 32; ++n) g2[n] = mfma32(a2, tr.read(stage, kDiffTile * C::CD * 16, n, u), g2[n]);
+    for (int j = J2; j < J3; ++j) {
+      rd(j + LA);
+      dp = mfma32(buf[j], go[j - J2], dp);
+#pragma unroll
+      for (int i = 16 * (j - J2) / KV; i < 16 * (j - J2 + 1) / KV; ++i)
+        e2[i] = exp2_fast(__builtin_fmaf(s2[i], c, -ls2));
+      diff_pin();
+    }
+    bf16x8 a1[2], a2[2];
+    auto grad = [&](int i) {
+      e1[i] *= dp[i] - d1;
+      dl = __builtin_fmaf(e2[i], dp[i], dl);
+      e2[i] *= dp[i] - d2;
+      if (i % 8 == 7) {
+        a1[i / 8] = pack8(e1 + i - 7);
+        a2[i / 8] = pack8(e2 + i - 7);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) grad(i);
+    diff_pin();
+#pragma unroll
+    for (int j = J3; j < J4; ++j) {
+      rd(j + LA);
+      const int x = j - J3, u = x / (2 * ND), n = x % ND;
+      if (x / ND % 2 == 0) g1[n] = mfma32(a1[u], buf[j], g1[n]);
+      else g2[n] = mfma32(a2[u], buf[j], g2[n]);
+      if (u == 0) {
+#pragma unroll
+        for (int i = 8 * x / (2 * ND); i < 8 * (x + 1) / (2 * ND); ++i) grad(8 + i);
+      }
+      diff_pin();
     }
   };
 
-  if (t_end > 0) load(0, st0);
-  wait_vmem();
-  barrier_no_fence();
-  auto step = [&](const u32x4* cur, u32x4* nxt, int t) {
-    if (t + 1 < t_end) load(t + 1, nxt);
-    tile(cur, t);
-    wait_vmem();
-    wait_lds();
-    barrier_no_fence();
-  };
-  for (int t = 0; t < t_end; t += 2) {
-    step(st0, st1, t);
-    if (t + 1 < t_end) step(st1, st0, t + 1);
-  }
+  stream_tiles<C::STAGES_Q, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
 
   const size_t rows = (size_t)bh * a.NQ;
-  if (a.dq1) write_grad<D>(a.dq1, a.bf16_grads != 0, g1, rows, rw, a.NQ, a.scale, lane, a.d);
-  if (a.dq2) write_grad<D>(a.dq2, a.bf16_grads != 0, g2, rows, rw, a.NQ, -a.scale * lam, lane, a.d);
+  void *o1 = a.dq1, *o2 = a.dq2;
+  bool as_bf16 = a.bf16_grads != 0;
+  if (a.q_splits > 1) {
+    const long long each = (long long)a.B * a.H * a.NQ * a.d;
+    as_bf16 = false;
+    if (o1) o1 = a.grad_part + (2 * (long long)blockIdx.y) * each;
+    if (o2) o2 = a.grad_part + (2 * (long long)blockIdx.y + 1) * each;
+  }
+  if (o1) write_grad<D>(o1, as_bf16, g1, rows, rw, a.NQ, a.scale, lane, a.d);
+  if (o2) write_grad<D>(o2, as_bf16, g2, rows, rw, a.NQ, -a.scale * lam, lane, a.d);
   if (a.dlam) {
     if (!ok) dl = 0.f;
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) dl += __shfl_xor(dl, x);
     if (lane == 0) red[wave] = dl;
     __syncthreads();
-    if (tid == 0) a.dlam_part[(long long)bh * T + blk] = (red[0] + red[1]) + (red[2] + red[3]);
+    if (tid == 0) a.dlam_part[((long long)bh * T + blk) * a.q_splits + blockIdx.y] = (red[0] + red[1]) + (red[2] + red[3]);
   }
 }
 
@@ -193,12 +249,14 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
 // of 32 rows, one query head of the group after the other, with their
 // prepared statistics.
 // ---------------------------------------------------------------------------
-template <int D, int DV>
-__global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_K)) diff_bwd_dkv_kernel(const DiffArgs a) {
-  using C = DiffBwdCfg<D, DV>;
-  __shared__ u32x4 st0[C::STAGE];
-  __shared__ u32x4 st1[C::STAGE];
-  __shared__ f32x4 stat[2][4][kDiffTile / 4];
+template <int D, int DV, int PART>
+__global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) diff_bwd_dkv_kernel(const DiffArgs a) {
+  using C = DiffBwdCfg<D, DV, PART>;
+  constexpr bool WANT_K = (PART & 1) != 0, WANT_V = (PART & 2) != 0;
+  constexpr int KD = D / 16, KV = DV / 16, ND = D / 32, NV = DV / 32;
+  __shared__ u32x4 st0[C::STAGE + C::STATS];
+  __shared__ u32x4 st1[C::STAGE + C::STATS];
+  __shared__ u32x4 st2[C::STAGES_K == 3 ? C::STAGE + C::STATS : 1];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int T = (a.NK + C::ROWS - 1) / C::ROWS, G = a.H / a.HK;
@@ -219,7 +277,14 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_K)) diff_b
   // row tiles that see a key of the block, for every head of the group
   const int t_all = (qlen + kDiffTile - 1) / kDiffTile;
   const int t_first = !a.causal ? 0 : min(max(kb0 - off, 0) / kDiffTile, t_all);
-  const int per = kb0 < klen ? t_all - t_first : 0, t_end = per * G;
+  const int per = kb0 < klen ? t_all - t_first : 0;
+  int s_end = per * G, s_begin = 0;   // steps: one row tile of one head each
+  if (a.k_splits > 1) {
+    const int each = (s_end + a.k_splits - 1) / a.k_splits;
+    s_begin = min(s_end, (int)blockIdx.y * each);
+    s_end = min(s_end, s_begin + each);
+  }
+  const int g_begin = per ? s_begin / per : 0, t_begin = s_begin - g_begin * per;
 
   const bool ok = key < klen;
   bf16x8 k1[D / 16], k2[D / 16], vv[DV / 16];
@@ -228,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_K)) diff_b
   };
   load_row_operand<D>(k1, row_of(a.k1), ok, half, a.d);
   load_row_operand<D>(k2, row_of(a.k2), ok, half, a.d);
-  load_row_operand<DV>(vv, row_of(a.v), ok, half, a.dv);
+  if constexpr (WANT_K) load_row_operand<DV>(vv, row_of(a.v), ok, half, a.dv);
   wait_vmem();   // before the tile loop: a first use inside it would wait on every trip
 
   f32x16 g1[D / 32], g2[D / 32], gv[DV / 32];
@@ -245,101 +310,189 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_K)) diff_b
   const TrCols<D> trd(lane);
   const TrCols<DV> trv(lane);
   const int ntq = (a.NQ + kDiffTile - 1) / kDiffTile;
-  // step u: head hk G + u / per, row tile t_first + u % per. The loads run one
-  // step ahead, so each side keeps its own place.
-  int lg = 0, lt = 0;
-  auto load = [&](u32x4* stage, int buf) {
-    const int h = hk * G + lg, row0 = (t_first + lt) * kDiffTile;
+  // step u: head hk G + u / per, row tile t_first + u % per. The loads run
+  // ahead, so each side keeps its own place.
+  int lg = g_begin, lt = t_begin;
+  TileRows r1(nullptr, bq1, a.d), r2(nullptr, bq2, a.d), r3(nullptr, bo, a.dv);
+  const float* ps = nullptr;
+  auto begin_head = [&](int h, int t0) {
     const long long bh = (long long)b * a.H + h;
-    dma.issue(tile_rsrc(a.q1.p + (long long)b * a.q1.sb + (long long)h * a.q1.sh, row0, qlen, bq1, a.d),
-              tile_rsrc(a.q2.p + (long long)b * a.q2.sb + (long long)h * a.q2.sh, row0, qlen, bq2, a.d),
-              tile_rsrc(a.dout + bh * a.NQ * a.dv, row0, qlen, bo, a.dv), stage, wave);
+    r1.p = reinterpret_cast<const char*>(a.q1.p + (long long)b * a.q1.sb + (long long)h * a.q1.sh);
+    r2.p = reinterpret_cast<const char*>(a.q2.p + (long long)b * a.q2.sb + (long long)h * a.q2.sh);
+    r3.p = reinterpret_cast<const char*>(a.dout + bh * a.NQ * a.dv);
+    r1.skip(t_first + t0);
+    r2.skip(t_first + t0);
+    r3.skip(t_first + t0);
+    ps = a.stats + (bh * ntq + t_first + t0) * kDiffStatsTile;
+  };
+  begin_head(hk * G + (g_begin < G ? g_begin : 0), t_begin);
+  auto load = [&](int, u32x4* stage) {
+    const int rows = qlen - (t_first + lt) * kDiffTile;
+    dma.issue(r1.next(rows), r2.next(rows), r3.next(rows), stage, wave);
 #if defined(__HIP_DEVICE_COMPILE__)
-    if (wave == 0) {
-      const rsrc_t rs = make_rsrc(a.stats + (bh * ntq + t_first + lt) * kDiffStatsTile, kDiffStatsTile * 4u);
-      float* dst = reinterpret_cast<float*>(&stat[buf][0][0]);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 4, 4u * lane, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(dst + 64), 4, 4u * lane + 256u, 0, 0, 0);
-    }
+    // every wave loads a quarter of the statistics: one instruction each, half of its lanes
+    const rsrc_t rs = make_rsrc(ps, kDiffStatsTile * 4u);
+    if (lane < 32)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(reinterpret_cast<float*>(stage + C::STAGE) + 32 * wave),
+                                               4, 4u * lane + 128u * wave, 0, 0, 0);
 #endif
+    ps += kDiffStatsTile;
     if (++lt == per) {
       lt = 0;
-      ++lg;
+      if (++lg < G) begin_head(hk * G + lg, 0);
     }
   };
 
-  int cg = 0, ct = 0;
-  float nsign = a.lam[hk * G] < 0.f ? 1.f : -1.f;   // -sign(lam) of the current head
-  auto tile = [&](const u32x4* stage, int buf) {
+  int cg = g_begin, ct = t_begin;
+  float nsign = a.lam[hk * G + (g_begin < G ? g_begin : 0)] < 0.f ? 1.f : -1.f;   // -sign(lam) of the current head
+  auto products = [&](const u32x4* stage, int r0) {
+    constexpr int J1 = KD, J2 = J1 + KD, J3 = J2 + (WANT_K ? KV : 0), J4 = J3 + (WANT_V ? 2 * NV : 0);
+    constexpr int J5 = J4 + (WANT_K ? 4 * ND : 0), LA = C::LA_K;
+    bf16x8 buf[J5];   // streamed operands, read LA of them ahead of their MFMAs
+    auto rd = [&](int j) {
+      if (j < J2) buf[j] = lds_row8<C::CD>(stage + j / KD * kDiffTile * C::CD, lane & 31, 2 * (j % KD) + half);
+      else if (j < J3) buf[j] = lds_row8<C::CV>(stage + 2 * kDiffTile * C::CD, lane & 31, 2 * (j - J2) + half);
+      else if (j < J4) buf[j] = trv.read(stage, 2 * kDiffTile * C::CD * 16, (j - J3) % NV, (j - J3) / NV);
+      else if (j < J5)   // [map][k-block][columns]
+        buf[j] = trd.read(stage, (j - J4) / (2 * ND) * kDiffTile * C::CD * 16, (j - J4) % ND, (j - J4) / ND % 2);
+    };
+    const f32x4* st = reinterpret_cast<const f32x4*>(stage + C::STAGE);
+    f32x4 ga[4], gb[4];   // statistics of four elements, read one such group ahead of their use
+    auto rd_st = [&](f32x4 (&g)[4], int which, int i) {
+      if (i < 16) g[i >> 2] = st[8 * which + 2 * (i >> 2) + half];
+    };
+    f32x16 s1 = zero16(), s2 = zero16(), dp = zero16();
+    float e1[16], e2[16], p[16];
+    const bool mask = (a.causal && kw + 31 > r0 + off) || kw + 32 > klen;
+    auto hide = [&](f32x16& s) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const bool seen = ok && (!a.causal || key <= r0 + 8 * (i >> 2) + 4 * half + (i & 3) + off);
+        s[i] = seen ? s[i] : kNegInf;
+      }
+    };
+    diff_pin();
+#pragma unroll
+    for (int j = 0; j < LA; ++j) rd(j);
+    diff_pin();
+#pragma unroll
+    for (int j = 0; j < J1; ++j) {
+      rd(j + LA);
+      s1 = mfma32(buf[j], k1[j], s1);
+      diff_pin();
+    }
+    rd_st(ga, 0, 0);
+    if (mask) hide(s1);
+    diff_pin();
+#pragma unroll
+    for (int j = J1; j < J2; ++j) {
+      rd(j + LA);
+      s2 = mfma32(buf[j], k2[j - J1], s2);
+#pragma unroll
+      for (int i = 16 * (j - J1) / KD; i < 16 * (j - J1 + 1) / KD; ++i) {
+        if (i % 4 == 0) rd_st(ga, 0, i + 4);
+        e1[i] = exp2_fast(__builtin_fmaf(s1[i], c, -ga[i >> 2][i & 3]));   // P_1
+      }
+      diff_pin();
+    }
+    rd_st(gb, 1, 0);
+    if (mask) hide(s2);
+    diff_pin();
+    bf16x8 ap[2];
+    auto second = [&](int i) {
+      if (i % 4 == 0) rd_st(gb, 1, i + 4);
+      e2[i] = exp2_fast(__builtin_fmaf(s2[i], c, -gb[i >> 2][i & 3]));   // |lam| P_2
+      if constexpr (WANT_V) {
+        p[i] = __builtin_fmaf(nsign, e2[i], e1[i]);
+        if (i % 8 == 7) ap[i / 8] = pack8(p + i - 7);
+      }
+    };
+    if constexpr (!WANT_K) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) second(i);
+      diff_pin();
+    }
+#pragma unroll
+    for (int j = J2; j < J3; ++j) {
+      rd(j + LA);
+      dp = mfma32(buf[j], vv[j - J2], dp);
+#pragma unroll
+      for (int i = 16 * (j - J2) / KV; i < 16 * (j - J2 + 1) / KV; ++i) second(i);
+      diff_pin();
+    }
+    bf16x8 a1[2], a2[2];
+    auto grad = [&](int i) {
+      if (i % 4 == 0) {
+        rd_st(ga, 2, i + 4);
+        rd_st(gb, 3, i + 4);
+      }
+      e1[i] *= dp[i] - ga[i >> 2][i & 3];
+      e2[i] *= __builtin_fmaf(nsign, dp[i], gb[i >> 2][i & 3]);
+      if (i % 8 == 7) {
+        a1[i / 8] = pack8(e1 + i - 7);
+        a2[i / 8] = pack8(e2 + i - 7);
+      }
+    };
+    if constexpr (WANT_K) {
+      rd_st(ga, 2, 0);
+      rd_st(gb, 3, 0);
+      diff_pin();
+      if constexpr (!WANT_V) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) grad(i);
+        diff_pin();
+      }
+    }
+#pragma unroll
+    for (int j = J3; j < J4; ++j) {
+      rd(j + LA);
+      const int x = j - J3;
+      gv[x % NV] = mfma32(ap[x / NV], buf[j], gv[x % NV]);
+      if constexpr (WANT_K) {
+#pragma unroll
+        for (int i = 16 * x / (2 * NV); i < 16 * (x + 1) / (2 * NV); ++i) grad(i);
+      } else if (x < NV) {
+#pragma unroll
+        for (int i = 8 * x / NV; i < 8 * (x + 1) / NV; ++i) second(8 + i);
+      }
+      diff_pin();
+    }
+#pragma unroll
+    for (int j = J4; j < J5; ++j) {
+      rd(j + LA);
+      const int x = j - J4, u = x / ND % 2, n = x % ND;
+      if (x < 2 * ND) g1[n] = mfma32(a1[u], buf[j], g1[n]);
+      else g2[n] = mfma32(a2[u], buf[j], g2[n]);
+      diff_pin();
+    }
+  };
+  auto tile = [&](int, const u32x4* stage) {
     const int r0 = (t_first + ct) * kDiffTile;
     const int rlast = min(r0 + kDiffTile, qlen) - 1;
     const bool active = kw < klen && (!a.causal || rlast + off >= kw);
-    if (active) {
-      const u32x4* to = stage + 2 * kDiffTile * C::CD;
-      f32x16 s1 = diff_product<D>(stage, k1, lane);
-      f32x16 s2 = diff_product<D>(stage + kDiffTile * C::CD, k2, lane);
-      const f32x16 dp = diff_product<DV>(to, vv, lane);
-      if ((a.causal && kw + 31 > r0 + off) || kw + 32 > klen) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const bool seen = ok && (!a.causal || key <= r0 + 8 * (i >> 2) + 4 * half + (i & 3) + off);
-          s1[i] = seen ? s1[i] : kNegInf;
-          s2[i] = seen ? s2[i] : kNegInf;
-        }
-      }
-      float p[16], e1[16], e2[16];
-#pragma unroll
-      for (int qd = 0; qd < 4; ++qd) {
-        const f32x4 l1 = stat[buf][0][2 * qd + half], l2 = stat[buf][1][2 * qd + half];
-        const f32x4 d1 = stat[buf][2][2 * qd + half], d2 = stat[buf][3][2 * qd + half];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = 4 * qd + j;
-          const float p1 = exp2_fast(__builtin_fmaf(s1[i], c, -l1[j]));
-          const float p2 = exp2_fast(__builtin_fmaf(s2[i], c, -l2[j]));   // |lam| P_2
-          p[i] = __builtin_fmaf(nsign, p2, p1);
-          e1[i] = p1 * (dp[i] - d1[j]);
-          e2[i] = p2 * __builtin_fmaf(nsign, dp[i], d2[j]);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bf16x8 ap = pack8(p + 8 * u), a1 = pack8(e1 + 8 * u), a2 = pack8(e2 + 8 * u);
-#pragma unroll
-        for (int n = 0; n < DV / 32; ++n)
-          gv[n] = mfma32(ap, trv.read(stage, 2 * kDiffTile * C::CD * 16, n, u), gv[n]);
-#pragma unroll
-        for (int n = 0; n < D / 32; ++n) g1[n] = mfma32(a1, trd.read(stage, 0, n, u), g1[n]);
-#pragma unroll
-        for (int n = 0; n < D / 32; ++n) g2[n] = mfma32(a2, trd.read(stage, kDiffTile * C::CD * 16, n, u), g2[n]);
-      }
-    }
+    if (active) products(stage, r0);
     if (++ct == per) {
       ct = 0;
       if (++cg < G) nsign = a.lam[hk * G + cg] < 0.f ? 1.f : -1.f;
     }
   };
 
-  if (t_end > 0) load(st0, 0);
-  wait_vmem();
-  barrier_no_fence();
-  auto step = [&](const u32x4* cur, u32x4* nxt, int t, int buf) {
-    if (t + 1 < t_end) load(nxt, buf ^ 1);
-    tile(cur, buf);
-    wait_vmem();
-    wait_lds();
-    barrier_no_fence();
-  };
-  for (int t = 0; t < t_end; t += 2) {
-    step(st0, st1, t, 0);
-    if (t + 1 < t_end) step(st1, st0, t + 1, 1);
-  }
+  stream_tiles<C::STAGES_K, DiffDma<D, DV, C::NT>::NCH + 1>(st0, st1, st2, s_begin, s_end, load, tile);
 
   const size_t rows = (size_t)bk * a.NK;
-  const bool half_type = a.bf16_grads != 0;
-  if (a.dk1) write_grad<D>(a.dk1, half_type, g1, rows, kw, a.NK, a.scale, lane, a.d);
-  if (a.dk2) write_grad<D>(a.dk2, half_type, g2, rows, kw, a.NK, a.scale, lane, a.d);
-  if (a.dv_out) write_grad<DV>(a.dv_out, half_type, gv, rows, kw, a.NK, 1.f, lane, a.dv);
+  void *o1 = a.dk1, *o2 = a.dk2, *o3 = a.dv_out;
+  bool as_bf16 = a.bf16_grads != 0;
+  if (a.k_splits > 1) {
+    const long long keys = (long long)a.B * a.HK * a.NK;
+    float* part = a.grad_part + blockIdx.y * keys * (2 * a.d + a.dv);
+    as_bf16 = false;
+    if (o1) o1 = part;
+    if (o2) o2 = part + keys * a.d;
+    if (o3) o3 = part + keys * 2 * a.d;
+  }
+  if (WANT_K && o1) write_grad<D>(o1, as_bf16, g1, rows, kw, a.NK, a.scale, lane, a.d);
+  if (WANT_K && o2) write_grad<D>(o2, as_bf16, g2, rows, kw, a.NK, a.scale, lane, a.d);
+  if (WANT_V && o3) write_grad<DV>(o3, as_bf16, gv, rows, kw, a.NK, 1.f, lane, a.dv);
 }
 
 }  // namespace streamkl

@@ -1,5 +1,5 @@
-// Instantiations of the differential-attention backward, the kernel that
-// prepares the row statistics and the one that sums dlam.
+// The small kernels of the differential-attention backward: row statistics,
+// the sum of dlam, the sum of partial gradients.
 #include "diff_bwd.hpp"
 #include "diff_launch.hpp"
 
@@ -72,18 +72,40 @@ __global__ void __launch_bounds__(kThreads) diff_bwd_dlam_kernel(const DiffArgs 
   if (tid == 0) a.dlam[h] = -((red[0] + red[1]) + (red[2] + red[3]));
 }
 
-int row_blocks(int NQ) { return (NQ + DiffBwdCfg<64, 64>::ROWS - 1) / DiffBwdCfg<64, 64>::ROWS; }
-
-template <typename F>
-hipError_t by_dims(int d, int dv, F f) {
-  auto by_dv = [&](auto kd) {
-    switch (diff_value_dim(dv)) {
-      case 64: return f(kd, std::integral_constant<int, 64>{});
-      case 128: return f(kd, std::integral_constant<int, 128>{});
-      default: return f(kd, std::integral_constant<int, 256>{});
+// Sum of n partial arrays in their order, `each` floats apart: `count` values
+// of one gradient, a multiple of 4.
+template <bool BF16>
+__global__ void __launch_bounds__(kThreads) diff_bwd_join_kernel(const float* __restrict__ part, long long each, int n,
+                                                                 void* __restrict__ out, long long count) {
+  for (long long i = ((long long)blockIdx.x * kThreads + threadIdx.x) * 4; i < count;
+       i += (long long)gridDim.x * kThreads * 4) {
+    f32x4 s = *reinterpret_cast<const f32x4*>(part + i);
+    for (int j = 1; j < n; ++j) s += *reinterpret_cast<const f32x4*>(part + j * each + i);
+    if (BF16) {
+      bf16x4 r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = (__bf16)s[e];
+      uint32_t* o = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(out) + i);   // 4-byte aligned
+      const uint64_t bits = __builtin_bit_cast(uint64_t, r);
+      o[0] = (uint32_t)bits;
+      o[1] = (uint32_t)(bits >> 32);
+    } else {
+      float* o = static_cast<float*>(out) + i;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = s[e];
     }
-  };
-  return diff_key_dim(d) == 64 ? by_dv(std::integral_constant<int, 64>{}) : by_dv(std::integral_constant<int, 128>{});
+  }
+}
+
+hipError_t join(const float* part, long long each, int n, void* out, long long count, bool bf16, hipStream_t st) {
+  if (!out || count == 0) return hipSuccess;
+  const long long blocks = (count / 4 + kThreads - 1) / kThreads;
+  const dim3 grid((unsigned)(blocks < 16 * kCus ? blocks : 16 * kCus));
+  if (bf16)
+    hipLaunchKernelGGL(diff_bwd_join_kernel<true>, grid, dim3(kThreads), 0, st, part, each, n, out, count);
+  else
+    hipLaunchKernelGGL(diff_bwd_join_kernel<false>, grid, dim3(kThreads), 0, st, part, each, n, out, count);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -92,7 +114,9 @@ size_t diff_bwd_stats_floats(int B, int H, int NQ) {
   return (size_t)B * H * ((NQ + kDiffTile - 1) / kDiffTile) * kDiffStatsTile;
 }
 
-size_t diff_bwd_dlam_floats(int B, int H, int NQ) { return (size_t)B * H * row_blocks(NQ); }
+size_t diff_bwd_dlam_floats(int B, int H, int NQ, int q_splits) {
+  return ((size_t)B * H * diff_row_blocks(NQ) * q_splits + 3) / 4 * 4;
+}
 
 hipError_t launch_diff_bwd_prep(const DiffArgs& a) {
   const int ntq = (a.NQ + kDiffTile - 1) / kDiffTile;
@@ -103,25 +127,27 @@ hipError_t launch_diff_bwd_prep(const DiffArgs& a) {
   return hipGetLastError();
 }
 
-hipError_t launch_diff_bwd_dq(const DiffArgs& a) {
-  return by_dims(a.d, a.dv, [&](auto kd, auto kv) {
-    hipLaunchKernelGGL((diff_bwd_dq_kernel<kd.value, kv.value>),
-                       dim3((unsigned)((long long)a.B * a.H * row_blocks(a.NQ))), dim3(kThreads), 0, a.stream, a);
-    return hipGetLastError();
-  });
-}
-
-hipError_t launch_diff_bwd_dkv(const DiffArgs& a) {
-  return by_dims(a.d, a.dv, [&](auto kd, auto kv) {
-    hipLaunchKernelGGL((diff_bwd_dkv_kernel<kd.value, kv.value>),
-                       dim3((unsigned)((long long)a.B * a.HK * row_blocks(a.NK))), dim3(kThreads), 0, a.stream, a);
-    return hipGetLastError();
-  });
-}
-
 hipError_t launch_diff_bwd_dlam(const DiffArgs& a) {
-  hipLaunchKernelGGL(diff_bwd_dlam_kernel, dim3((unsigned)a.H), dim3(kThreads), 0, a.stream, a, row_blocks(a.NQ));
+  hipLaunchKernelGGL(diff_bwd_dlam_kernel, dim3((unsigned)a.H), dim3(kThreads), 0, a.stream, a,
+                     diff_row_blocks(a.NQ) * a.q_splits);
   return hipGetLastError();
+}
+
+hipError_t launch_diff_bwd_join_q(const DiffArgs& a) {
+  const long long each = (long long)a.B * a.H * a.NQ * a.d;
+  const bool half = a.bf16_grads != 0;
+  hipError_t e = join(a.grad_part, 2 * each, a.q_splits, a.dq1, each, half, a.stream);
+  if (e == hipSuccess) e = join(a.grad_part + each, 2 * each, a.q_splits, a.dq2, each, half, a.stream);
+  return e;
+}
+
+hipError_t launch_diff_bwd_join_k(const DiffArgs& a) {
+  const long long keys = (long long)a.B * a.HK * a.NK, each = keys * (2 * a.d + a.dv);
+  const bool half = a.bf16_grads != 0;
+  hipError_t e = join(a.grad_part, each, a.k_splits, a.dk1, keys * a.d, half, a.stream);
+  if (e == hipSuccess) e = join(a.grad_part + keys * a.d, each, a.k_splits, a.dk2, keys * a.d, half, a.stream);
+  if (e == hipSuccess) e = join(a.grad_part + keys * 2 * a.d, each, a.k_splits, a.dv_out, keys * a.dv, half, a.stream);
+  return e;
 }
 
 }  // namespace streamkl

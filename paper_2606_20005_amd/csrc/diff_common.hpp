@@ -38,11 +38,16 @@ struct DiffArgs {
   const uint16_t* dout;      // [B, H, NQ, dv]
   float* stats;              // prepared row statistics, see diff_bwd.hpp
   float* dlam_part;          // partial sums of dlam
+  int q_splits, k_splits;    // ranges of the streamed axis in the query- and the key-owned kernel
+  float* grad_part;          // their partial gradients where there is more than one
   void *dq1, *dk1, *dq2, *dk2, *dv_out;
   float* dlam;
   int bf16_grads;
   hipStream_t stream;
 };
+
+// Nothing moves across: the order of loads, MFMAs and vector work around it is the one written.
+__device__ __forceinline__ void diff_pin() { __builtin_amdgcn_sched_barrier(0); }
 
 __device__ __forceinline__ int clamp_len(const int* len, int b, int n) {
   return len ? min(max(len[b], 0), n) : n;
@@ -54,30 +59,43 @@ __device__ __forceinline__ uint32_t row_chunk_offset(int r, int c, int creal, ui
   return c < creal ? (uint32_t)r * row_bytes + (uint32_t)c * 16u : kOutOfSlab;
 }
 
-// Resource over rows row0 .. row0 + kDiffTile - 1 of a head, of which `rows`
-// exist: the base is the tile's first row (64-bit), so a head may span more
-// than 4 GiB, and reads past the last row that exists return zeros. base is
-// the head's first row; every row is dreal elements, row_bytes apart.
-__device__ __forceinline__ rsrc_t tile_rsrc(const uint16_t* base, int row0, int n_rows, uint32_t row_bytes, int dreal) {
-  const int rows = min(max(n_rows - row0, 0), kDiffTile);
-  const uint32_t bytes = rows > 0 ? (uint32_t)(rows - 1) * row_bytes + (uint32_t)dreal * 2u : 0u;
-  return make_rsrc(reinterpret_cast<const char*>(base) + (long long)(rows > 0 ? row0 : 0) * row_bytes, bytes);
-}
+// The rows of one head, tile after tile. The resource of a tile begins at its
+// first row (a 64-bit address, so a head may span more than 4 GiB) and ends
+// with the last row that exists: reads past it return zeros. A step costs a
+// few scalar instructions: with the tile's address and extent formed anew
+// every time, the kernels spent as many issue cycles on scalar as on vector
+// instructions.
+struct TileRows {
+  const char* p;
+  uint32_t row_bytes, full, last;   // bytes per row, of a whole tile up to the end of its last row, of a row's data
+  __device__ __forceinline__ TileRows(const uint16_t* first, uint32_t rb, int dreal)
+      : p(reinterpret_cast<const char*>(first)), row_bytes(rb), full((kDiffTile - 1) * rb + (uint32_t)dreal * 2u),
+        last((uint32_t)dreal * 2u) {}
+  __device__ __forceinline__ void skip(int tiles) { p += (long long)tiles * kDiffTile * row_bytes; }
+  // the current tile, of which `rows` >= 1 rows exist; moves on to the next
+  __device__ __forceinline__ rsrc_t next(int rows) {
+    const rsrc_t r = make_rsrc(p, rows >= kDiffTile ? full : (uint32_t)(rows - 1) * row_bytes + last);
+    p += (unsigned long long)(kDiffTile * row_bytes);
+    return r;
+  }
+};
 
 // Staging of a tile of three matrices A, B (DA columns each) and C (DC
 // columns), 32 rows each, by direct-to-LDS loads of NT threads: stage layout
-// [A | B | C], every matrix in the swizzled layout of kl_common.hpp. Pieces
-// of 64 chunks (one load instruction of a wave) never straddle matrices.
+// [A | B | C], every matrix in the swizzled layout of kl_common.hpp.
 template <int DA, int DC, int NT>
 struct DiffDma {
   static constexpr int CA = DA / 8, CC = DC / 8;
   static constexpr int CHUNKS = kDiffTile * (2 * CA + CC);
   static constexpr int NCH = CHUNKS / NT;
+  // every load instruction of a wave (64 chunks) serves one matrix; which one is known at compile time unless the
+  // instruction of the whole workgroup straddles two
+  static constexpr bool WHOLE = (kDiffTile * CA) % NT == 0;
   static_assert(CHUNKS % NT == 0, "staging split");
   uint32_t voff[NCH];
 
   // which matrix chunk p of the stage belongs to
-  __device__ __forceinline__ static int matrix(int p) {
+  __device__ __forceinline__ static constexpr int matrix(int p) {
     return p < kDiffTile * CA ? 0 : p < 2 * kDiffTile * CA ? 1 : 2;
   }
 
@@ -101,13 +119,47 @@ struct DiffDma {
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int m = matrix(NT * i + 64 * wave);   // uniform
+      const int m = matrix(NT * i + (WHOLE ? 0 : 64 * wave));
       const rsrc_t r = m == 0 ? ra : m == 1 ? rb : rc;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(stage + NT * i + 64 * wave), 16, voff[i], 0, 0, 0);
     }
 #endif
   }
 };
+
+// Streams tiles t0 .. t1 - 1 through STAGES (2 or 3) LDS stages: while a tile is
+// worked on, the loads of the next one or two are in flight. load(t, stage)
+// starts the loads of a tile, NLOAD instructions of this wave; tile(t, stage)
+// works on it. The stages are separate arrays, named explicitly, so that the
+// compiler can tell reads of one from loads into another. With two, s2 is unused.
+template <int STAGES, int NLOAD, typename Load, typename Tile>
+__device__ __forceinline__ void stream_tiles(u32x4* s0, u32x4* s1, u32x4* s2, int t0, int t1, Load load, Tile tile) {
+  static_assert(STAGES == 2 || STAGES == 3, "two or three stages");
+  if (t0 < t1) load(t0, s0);
+  if (STAGES == 3 && t0 + 1 < t1) {
+    load(t0 + 1, s1);
+    wait_vmem_le<NLOAD>();
+  } else {
+    wait_vmem();
+  }
+  barrier_no_fence();
+  auto step = [&](u32x4* cur, u32x4* ahead, int t) {
+    const bool more = t + STAGES - 1 < t1;
+    if (more) load(t + STAGES - 1, ahead);
+    tile(t, cur);
+    if (STAGES == 3 && more) wait_vmem_le<NLOAD>();
+    else wait_vmem();
+    wait_lds();
+    barrier_no_fence();
+  };
+  for (int t = t0; t < t1; t += STAGES) {
+    step(s0, STAGES == 3 ? s2 : s1, t);
+    if (t + 1 < t1) step(s1, s0, t + 1);
+    if constexpr (STAGES == 3) {
+      if (t + 2 < t1) step(s2, s1, t + 2);
+    }
+  }
+}
 
 // Byte offsets within a matrix of D columns of the transpose reads that
 // deliver, for 16-row block s, the 32 columns 32 nb + l % 32 of rows

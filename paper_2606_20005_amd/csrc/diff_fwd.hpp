@@ -51,7 +51,12 @@ struct DiffFwdCfg {
   static constexpr int XCHG = GROUPS * 256;           // chunks of the exchange of one 32 x 32 block per pair
   // registers: accumulators, resident rows, logits, about 64 for the rest
   static constexpr int REGS = RB * (DV / 2 + D / 4 + 16) + 64;
-  static constexpr int WAVES = REGS <= 256 ? 2 : 1;   // waves per SIMD
+  static constexpr int WAVES = REGS <= 168 ? 3 : REGS <= 256 ? 2 : 1;   // waves per SIMD
+  static constexpr int LA = WAVES == 1 ? 4 : REGS > 248 ? 2 : 3;   // operand reads in flight ahead of their MFMAs
+  // three stages where the workgroups that the registers leave room for have room for them too
+  static constexpr int LDS2 = (STAGE + (STAGE > XCHG ? STAGE : XCHG)) * 16;
+  static constexpr int STAGES = (LDS2 + STAGE * 16) * (4 * WAVES / NW) <= 160 * 1024 ? 3 : 2;
+  static constexpr int LDS = LDS2 + (STAGES - 2) * STAGE * 16;
 };
 
 template <int D, int DV, int RB, int NW>
@@ -61,6 +66,7 @@ diff_fwd_kernel(const DiffArgs a) {
   constexpr int KS = D / 16, NB = DV / 32;
   __shared__ u32x4 st0[C::STAGE > C::XCHG ? C::STAGE : C::XCHG];
   __shared__ u32x4 st1[C::STAGE];
+  __shared__ u32x4 st2[C::STAGES == 3 ? C::STAGE : 1];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), map = wave & 1, group = wave >> 1;
   const int G = a.H / a.HK, R = a.NQ * G, T = (R + C::ROWS - 1) / C::ROWS;
@@ -92,21 +98,26 @@ diff_fwd_kernel(const DiffArgs a) {
   const bool live = rw < R && i0w < qlen;   // some row of the wave exists
   const int wave_min = limit_of(i0w), wave_max = live ? limit_of(i1w) : 0;
 
-  // resident rows
-  int limit[RB], row_i[RB], row_h[RB];
-  bool row_ok[RB];
+  // Packed row r of this lane in block x: query i of head h. Formed from `at`,
+  // which the epilogue hides from the optimizer: kept through the loop, these
+  // would take registers that it has none to spare of.
+  struct Row {
+    int i, h;
+    bool in, ok;   // inside the tensor; and inside its sequence
+  };
+  auto row_of = [&](int x, int at) {
+    const int r = rw + 32 * x + at, i = r / G;
+    return Row{i, hk * G + (r - i * G), r < R, r < R && i < qlen};
+  };
+  int limit[RB];
   bf16x8 q[RB][KS];
   const DiffRows& qv = map ? a.q2 : a.q1;
 #pragma unroll
   for (int x = 0; x < RB; ++x) {
-    const int r = rw + 32 * x + (lane & 31);
-    row_i[x] = r / G;
-    row_h[x] = hk * G + (r - row_i[x] * G);
-    row_ok[x] = r < R && row_i[x] < qlen;
-    limit[x] = row_ok[x] ? limit_of(row_i[x]) : klen;   // rows that do not exist take part unmasked, nothing reads them
-    const uint16_t* p = qv.p + (row_ok[x] ? (long long)b * qv.sb + (long long)row_h[x] * qv.sh +
-                                                (long long)row_i[x] * qv.sn : 0);
-    load_row_operand<D>(q[x], p, row_ok[x], half, a.d);
+    const Row w = row_of(x, lane & 31);
+    limit[x] = w.ok ? limit_of(w.i) : klen;   // rows that do not exist take part unmasked, nothing reads them
+    const uint16_t* p = qv.p + (w.ok ? (long long)b * qv.sb + (long long)w.h * qv.sh + (long long)w.i * qv.sn : 0);
+    load_row_operand<D>(q[x], p, w.ok, half, a.d);
   }
   wait_vmem();   // before the tile loop: a first use inside it would wait on every trip
 
@@ -128,23 +139,38 @@ diff_fwd_kernel(const DiffArgs a) {
   const uint16_t* vv = a.v.p + (long long)b * a.v.sb + (long long)hk * a.v.sh;
   const DiffDma<D, DV, C::NT> dma(tid, a.d, a.dv, bk1, bk2, bv);
   const TrCols<DV> tr(lane);
+  TileRows r1(k1, bk1, a.d), r2(k2, bk2, a.d), r3(vv, bv, a.dv);
+  r1.skip(t_begin);
+  r2.skip(t_begin);
+  r3.skip(t_begin);
   auto load = [&](int t, u32x4* stage) {
-    dma.issue(tile_rsrc(k1, t * kDiffTile, klen, bk1, a.d), tile_rsrc(k2, t * kDiffTile, klen, bk2, a.d),
-              tile_rsrc(vv, t * kDiffTile, klen, bv, a.dv), stage, wave);
+    const int rows = klen - t * kDiffTile;
+    dma.issue(r1.next(rows), r2.next(rows), r3.next(rows), stage, wave);
   };
 
-  auto tile = [&](const u32x4* stage, int t) {
+  auto tile = [&](int t, const u32x4* stage) {
     const int k0 = t * kDiffTile;
     if (k0 >= wave_max) return;
     const u32x4* kt = stage + map * kDiffTile * (D / 8);
+    constexpr int vbase = 2 * kDiffTile * (D / 8) * 16, NR = KS + 2 * NB, LA = C::LA;
+    bf16x8 buf[NR];   // streamed operands: key chunks, then value blocks; read LA of them ahead of their MFMAs
+    auto rd = [&](int j) {
+      if (j < KS) buf[j] = lds_row8<D / 8>(kt, lane & 31, 2 * j + half);
+      else if (j < NR) buf[j] = tr.read(stage, vbase, (j - KS) % NB, (j - KS) / NB);
+    };
     f32x16 s[RB];
 #pragma unroll
     for (int x = 0; x < RB; ++x) s[x] = zero16();
+    diff_pin();
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8 k = lds_row8<D / 8>(kt, lane & 31, 2 * ks + half);
+    for (int j = 0; j < LA; ++j) rd(j);
+    diff_pin();
 #pragma unroll
-      for (int x = 0; x < RB; ++x) s[x] = mfma32(k, q[x][ks], s[x]);
+    for (int j = 0; j < KS; ++j) {
+      rd(j + LA);
+#pragma unroll
+      for (int x = 0; x < RB; ++x) s[x] = mfma32(buf[j], q[x][j], s[x]);
+      diff_pin();
     }
     if (k0 + kDiffTile > wave_min) {
 #pragma unroll
@@ -175,54 +201,52 @@ diff_fwd_kernel(const DiffArgs a) {
         }
       }
     }
+    diff_pin();
+    float e[RB][16];
     bf16x8 p[RB][2];
+    auto prob = [&](int x, int i) {
+      e[x][i] = exp2_fast(__builtin_fmaf(s[x][i], c, nu[x]));
+      l[x] += e[x][i];
+      if (i % 8 == 7) p[x][i / 8] = pack8(e[x] + i - 7);
+    };
 #pragma unroll
-    for (int x = 0; x < RB; ++x) {
-      float e[16], sum = 0.f;
+    for (int x = 0; x < RB; ++x)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        e[i] = exp2_fast(__builtin_fmaf(s[x][i], c, nu[x]));
-        sum += e[i];
-      }
-      l[x] += sum;
-      p[x][0] = pack8(e);
-      p[x][1] = pack8(e + 8);
+      for (int i = 0; i < 8; ++i) prob(x, i);
+    diff_pin();
+    // the second half of the exponentials beside the products of the first
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      rd(KS + nb + LA);
+#pragma unroll
+      for (int x = 0; x < RB; ++x) o[x][nb] = mfma32(buf[KS + nb], p[x][0], o[x][nb]);
+#pragma unroll
+      for (int y = 8 * RB * nb / NB; y < 8 * RB * (nb + 1) / NB; ++y) prob(y / 8, 8 + y % 8);
+      diff_pin();
     }
-    constexpr int vbase = 2 * kDiffTile * (D / 8) * 16;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int nb = 0; nb < NB; ++nb) {
+      rd(KS + NB + nb + LA);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const bf16x8 v = tr.read(stage, vbase, nb, u);
-#pragma unroll
-        for (int x = 0; x < RB; ++x) o[x][nb] = mfma32(v, p[x][u], o[x][nb]);
-      }
+      for (int x = 0; x < RB; ++x) o[x][nb] = mfma32(buf[KS + NB + nb], p[x][1], o[x][nb]);
+      diff_pin();
+    }
   };
 
-  if (t_begin < t_end) load(t_begin, st0);
-  wait_vmem();
-  barrier_no_fence();
-  auto step = [&](const u32x4* cur, u32x4* nxt, int t) {
-    if (t + 1 < t_end) load(t + 1, nxt);
-    tile(cur, t);
-    wait_vmem();
-    wait_lds();
-    barrier_no_fence();
-  };
-  for (int t = t_begin; t < t_end; t += 2) {
-    step(st0, st1, t);
-    if (t + 1 < t_end) step(st1, st0, t + 1);
-  }
+  stream_tiles<C::STAGES, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
 
 #pragma unroll
   for (int x = 0; x < RB; ++x) l[x] += __shfl_xor(l[x], 32);
 
-  auto out_row = [&](int x) { return ((long long)b * a.H + row_h[x]) * a.NQ + row_i[x]; };
+  Row row[RB];
+#pragma unroll
+  for (int x = 0; x < RB; ++x) row[x] = row_of(x, opaque(lane) & 31);
+  auto out_row = [&](int x) { return ((long long)b * a.H + row[x].h) * a.NQ + row[x].i; };
   if (a.splits > 1) {
     const long long rows = (long long)a.B * a.H * a.NQ;
 #pragma unroll
     for (int x = 0; x < RB; ++x) {
-      if (!row_ok[x]) continue;
+      if (!row[x].ok) continue;
       const long long at = (out_row(x) * a.splits + blockIdx.y) * 2 + map;
       float* po = a.part + at * a.dv;
 #pragma unroll
@@ -243,30 +267,20 @@ diff_fwd_kernel(const DiffArgs a) {
     return;
   }
 
-  float f[RB];   // 1 / l, times lam for map 2 after out2 is written; 0 for rows that see nothing
-#pragma unroll
-  for (int x = 0; x < RB; ++x) f[x] = l[x] > 0.f || l[x] != l[x] ? 1.f / l[x] : 0.f;
-  {
-    float* lse = map ? a.lse2 : a.lse1;
-    if (lse && half == 0) {
-#pragma unroll
-      for (int x = 0; x < RB; ++x)
-        if (rw + 32 * x + (lane & 31) < R)
-          lse[out_row(x)] = !row_ok[x] || m[x] == kNegInf ? kNegInf : (log2f(l[x]) - nu[x]) * kLn2;
-    }
-  }
+  float* lse = map ? a.lse2 : a.lse1;
   auto store4 = [&](uint16_t* dst, const float (&v)[4]) {
     bf16x4 r;
 #pragma unroll
     for (int j = 0; j < 4; ++j) r[j] = (__bf16)v[j];
     *reinterpret_cast<bf16x4*>(dst) = r;
   };
-  float lam[RB];
-#pragma unroll
-  for (int x = 0; x < RB; ++x) lam[x] = rw + 32 * x + (lane & 31) < R ? a.lam[row_h[x]] : 0.f;
 #pragma unroll
   for (int x = 0; x < RB; ++x) {
-    const bool in = rw + 32 * x + (lane & 31) < R;
+    const bool in = row[x].in, ok = row[x].ok;
+    const float f = l[x] > 0.f || l[x] != l[x] ? 1.f / l[x] : 0.f;   // 0 for rows that see nothing
+    const float lam = in ? a.lam[row[x].h] : 0.f;
+    if (lse && half == 0 && in)
+      lse[out_row(x)] = !ok || m[x] == kNegInf ? kNegInf : (log2f(l[x]) - nu[x]) * kLn2;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       // the wave of map 2 hands its block to the wave of map 1, lane by lane
@@ -277,7 +291,7 @@ diff_fwd_kernel(const DiffArgs a) {
         for (int qd = 0; qd < 4; ++qd) {
           float v[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = row_ok[x] ? o[x][nb][4 * qd + j] * f[x] : 0.f;
+          for (int j = 0; j < 4; ++j) v[j] = ok ? o[x][nb][4 * qd + j] * f : 0.f;
           slot[64 * qd] = f32x4{v[0], v[1], v[2], v[3]};
           const int col = 32 * nb + 8 * qd + 4 * half;
           if (a.out2 && in && col < a.dv) store4(a.out2 + out_row(x) * a.dv + col, v);
@@ -290,8 +304,7 @@ diff_fwd_kernel(const DiffArgs a) {
           const f32x4 o2 = slot[64 * qd];
           float v[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            v[j] = row_ok[x] ? __builtin_fmaf(-lam[x], o2[j], o[x][nb][4 * qd + j] * f[x]) : 0.f;
+          for (int j = 0; j < 4; ++j) v[j] = ok ? __builtin_fmaf(-lam, o2[j], o[x][nb][4 * qd + j] * f) : 0.f;
           const int col = 32 * nb + 8 * qd + 4 * half;
           if (in && col < a.dv) store4(a.out + out_row(x) * a.dv + col, v);
         }

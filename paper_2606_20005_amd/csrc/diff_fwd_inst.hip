@@ -85,8 +85,7 @@ struct FwdPick {
   using C = DiffFwdCfg<D, DV, RB, NW>;
   static constexpr int rows() { return C::ROWS; }
   static constexpr int resident() {
-    constexpr int lds = (C::STAGE + (C::STAGE > C::XCHG ? C::STAGE : C::XCHG)) * 16;
-    constexpr int by_lds = 160 * 1024 / lds, by_waves = 4 * C::WAVES / NW;
+    constexpr int by_lds = 160 * 1024 / C::LDS, by_waves = 4 * C::WAVES / NW;
     return kCus * (by_lds < by_waves ? by_lds : by_waves);
   }
   static hipError_t launch(const DiffArgs& a) {
@@ -97,30 +96,22 @@ struct FwdPick {
   }
 };
 
-// Rows of one pair of waves where there are few (a whole block would be
-// mostly padding, and short blocks leave more of them resident), 128-row
-// blocks otherwise.
+// A pair of waves takes two 32-row blocks where its registers then leave room
+// for two waves per SIMD, one where they do not (d 128/128, 8 heads x 6007,
+// same box: 351 us with one block and two waves per SIMD, 423 with two blocks
+// and one). Few rows run in one pair of waves (a whole workgroup would be
+// mostly padding, and short ones leave more of them resident).
 template <typename F>
 auto pick(int d, int dv, long long rows, F f) {
-  auto by_rows = [&](auto kd, auto kv) {
+  return diff_by_dims(d, dv, [&](auto kd, auto kv) {
     constexpr int D = kd.value, DV = kv.value;
-    if constexpr (DV == 256) {
-      if (rows <= 32) return f(FwdPick<D, DV, 1, 2>{});
-      return f(FwdPick<D, DV, 1, 4>{});
-    } else {
+    constexpr int RB = DiffFwdCfg<D, DV, 2, 4>::WAVES >= 2 ? 2 : 1;
     if (rows <= 32) return f(FwdPick<D, DV, 1, 2>{});
-    if (rows <= 64) return f(FwdPick<D, DV, 2, 2>{});
-    return f(FwdPick<D, DV, 2, 4>{});
+    if constexpr (RB == 2) {
+      if (rows <= 64) return f(FwdPick<D, DV, 2, 2>{});
     }
-  };
-  auto by_dv = [&](auto kd) {
-    switch (diff_value_dim(dv)) {
-      case 64: return by_rows(kd, std::integral_constant<int, 64>{});
-      case 128: return by_rows(kd, std::integral_constant<int, 128>{});
-      default: return by_rows(kd, std::integral_constant<int, 256>{});
-    }
-  };
-  return diff_key_dim(d) == 64 ? by_dv(std::integral_constant<int, 64>{}) : by_dv(std::integral_constant<int, 128>{});
+    return f(FwdPick<D, DV, RB, 4>{});
+  });
 }
 
 }  // namespace

@@ -92,7 +92,7 @@ def _load():
     lib.streamkl_diff_bwd.argtypes = [rows, rows, rows, rows, rows, i, i, i, i, i, i, i, f, i, vp, vp, vp, vp, vp, vp,
                                       vp, vp, vp, sz, vp, vp, vp, vp, vp, vp, i, vp]
     lib.streamkl_diff_bwd.restype = i
-    lib.streamkl_diff_bwd_workspace_bytes.argtypes = [i, i, i]
+    lib.streamkl_diff_bwd_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
     lib.streamkl_diff_bwd_workspace_bytes.restype = sz
     lib.streamkl_strerror.argtypes = [i]
     lib.streamkl_strerror.restype = ctypes.c_char_p
@@ -700,9 +700,10 @@ def diff_workspace_bytes(B, H, n_q, dv, splits) -> int:
     return int(lib.streamkl_diff_fwd_workspace_bytes(int(B), int(H), int(n_q), int(dv), int(splits)))
 
 
-def diff_bwd_workspace_bytes(B, H, n_q) -> int:
+def diff_bwd_workspace_bytes(B, H, HK, n_q, n_k, d, dv, causal) -> int:
     """streamkl_diff_bwd_workspace_bytes: workspace of the backward."""
-    return int(lib.streamkl_diff_bwd_workspace_bytes(int(B), int(H), int(n_q)))
+    return int(lib.streamkl_diff_bwd_workspace_bytes(int(B), int(H), int(HK), int(n_q), int(n_k), int(d), int(dv),
+                                                     int(bool(causal))))
 
 
 def _bf16_out(t, shape, dev, name):
@@ -768,7 +769,7 @@ def diff_bwd(q1, k1, q2, k2, v, lam, dout, out, out2, lse1, lse2, scale=None, ca
     g = {n: torch.empty(s, dtype=torch.float32 if n == "dlam" else grad_dtype, device=dev) if n in want else None
          for n, s in shapes.items()}
     if workspace is None:
-        ws_bytes = lib.streamkl_diff_bwd_workspace_bytes(B, H, NQ)
+        ws_bytes = lib.streamkl_diff_bwd_workspace_bytes(*ext, int(bool(causal)))
         workspace = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=dev)
     else:
         ws_bytes = workspace.numel() * workspace.element_size()

@@ -122,7 +122,7 @@ def test_diff_refuses_workspaces_and_outputs(sk):
     none = dict(dq1=None, dk1=None, dq2=None, dk2=None, dvv=None, dlam=None)
     assert diff_bwd_call(sk, **none) == 1
     assert diff_bwd_call(sk, bf16=2) == 1
-    assert diff_bwd_call(sk, ws=None) == 1 and diff_bwd_call(sk, wsb=sk.diff_bwd_workspace_bytes(1, 4, 8) - 1) == 1
+    assert diff_bwd_call(sk, ws=None) == 1 and diff_bwd_call(sk, wsb=sk.diff_bwd_workspace_bytes(1, 4, 2, 8, 8, 64, 64, False) - 1) == 1
     for n in ("dout", "lse1", "lse2"):
         assert diff_bwd_call(sk, **{n: None}) == 1
     for n in ("dq1", "dvv", "dlam"):
