@@ -133,15 +133,22 @@ int hip_status(hipError_t e) { return e == hipSuccess ? STREAMKL_OK : STREAMKL_E
 
 }  // namespace
 
+// Two workgroups per CU where the single pass has fewer than half of that;
+// four tiles a range at least; and no more partials (written and read back in
+// float32) than three quarters of the bytes of the keys and values. Measured, us:
+// 16 sequences x 4 key heads x 65536 keys, one row each, d 64/128: 512
+// workgroups 357, 1024 362, 1536 393, 4096 411; 2 key heads x 66000, 61 rows of
+// 4 heads each, d 128/256: 256 workgroups 93, 384 101, 1024 129, 2048 200.
 extern "C" int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int N_K, int d, int dv) {
   if (check_extents(B, H, HK, N_Q, N_K, d, dv) != STREAMKL_OK) return 0;
   if ((long long)B * H * N_Q == 0) return 1;
   const long long R = (long long)N_Q * (H / HK);
   const int rows = streamkl::diff_fwd_rows(d, dv, R);
-  const long long base = (long long)B * HK * ((R + rows - 1) / rows), resident = streamkl::diff_fwd_resident(d, dv, R);
-  const long long tiles = (N_K + 31LL) / 32;
-  long long s = resident / base;   // one round of workgroups
-  if (s > tiles / 4) s = tiles / 4;   // each of them streams a few tiles
+  const long long base = (long long)B * HK * ((R + rows - 1) / rows), tiles = (N_K + 31LL) / 32;
+  long long s = 2LL * streamkl::kCus / base;
+  if (s > tiles / 4) s = tiles / 4;
+  const double partials = 2.0 * 8.0 * B * H * (double)N_Q * (dv + 2), bytes = 2.0 * B * HK * (double)N_K * (2 * d + dv);
+  if (s * partials > 0.75 * bytes) s = (long long)(0.75 * bytes / partials);
   if (s > streamkl::kDiffMaxSplits) s = streamkl::kDiffMaxSplits;
   return s < 2 ? 1 : (int)s;
 }

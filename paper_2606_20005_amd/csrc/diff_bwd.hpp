@@ -22,8 +22,9 @@
 // Prepared statistics (diff_bwd_prep_kernel): for every head and 32-row tile
 // 4 x 32 floats,
 //   [0] LSE_1 log2 e                    [1] LSE_2 log2 e - log2 |lam|
-//   [2] D_1                             [3] sign(lam) D_2
-// so that 2^(c s_2 - [1]) is |lam| P_2 without a multiply; rows that do not
+//   [2] -D_1                            [3] sign(lam) (D_2 - D_1)
+// so that 2^(c s_2 - [1]) is |lam| P_2 without a multiply, and dP - D_1 is what
+// the product gives when its accumulators start from [2]; rows that do not
 // exist or see nothing have +inf offsets (P = 0).
 #pragma once
 
@@ -43,11 +44,23 @@ struct DiffBwdCfg {
   // registers: gradients, resident rows, three logit tiles, about 64 for the rest
   static constexpr int REGS_Q = D + (2 * D + DV) / 4 + 48 + 64;
   static constexpr int REGS_K = (PART & 1 ? D + DV / 4 + 16 : 0) + (PART & 2 ? DV / 2 : 0) + D / 2 + 32 + 64;
-  static constexpr int WAVES_Q = REGS_Q <= 256 ? 2 : 1, WAVES_K = REGS_K <= 256 ? 2 : 1;
+  // 256 registers leave room for two waves per SIMD. The estimate is tight: d 64/192 meets 256 and spills in the
+  // query-owned kernel (190 us with one wave, 226 with two), as does dV alone at 128/192.
+  static constexpr int WAVES_Q = REGS_Q <= 248 ? 2 : 1, WAVES_K = REGS_K <= 256 - (PART == 2 ? 8 : 0) ? 2 : 1;
   static constexpr int LA_Q = WAVES_Q == 1 ? 4 : 3, LA_K = WAVES_K == 1 ? 4 : 2;   // operand reads in flight
-  // three stages where the workgroups that the registers leave room for have room for them too
-  static constexpr int STAGES_Q = 3 * STAGE * 16 * WAVES_Q <= 158 * 1024 ? 3 : 2;
-  static constexpr int STAGES_K = 3 * (STAGE + STATS) * 16 * WAVES_K <= 158 * 1024 ? 3 : 2;
+  // Three stages where the workgroups that the registers leave room for have
+  // room for them; two tiles a stage in the key-owned kernel with one wave per
+  // SIMD, which nothing else occupies while it waits for the others (d 64/128,
+  // 32 heads x 4096 causal: 414 -> 394 us together with the next item; no gain
+  // in the query-owned kernel).
+  static constexpr int ROOM = 158 * 1024;
+  static constexpr int TILE_Q = STAGE * 16 * WAVES_Q, TILE_K = (STAGE + STATS) * 16 * WAVES_K;
+  static constexpr int TR_K = WAVES_K == 1 && 4 * TILE_K <= ROOM ? 2 : 1;
+  static constexpr int STAGES_Q = 3 * TILE_Q <= ROOM ? 3 : 2, STAGES_K = 3 * TR_K * TILE_K <= ROOM ? 3 : 2;
+  // dP's accumulators start from -D_1, which saves a subtraction an element;
+  // with two waves per SIMD the registers that hold it early spill (d 64/64,
+  // 16 heads x 4096: 259 -> 291 us).
+  static constexpr bool START_D = WAVES_K == 1;
 };
 
 // One 32 x 32 block of raw products streamed x resident: A = rows of the
@@ -113,8 +126,8 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
   float ls1 = __builtin_inff(), ls2 = ls1, d1 = 0.f, d2 = 0.f;
   if (ok) {
     const float* st = a.stats + ((long long)bh * ntq + row / kDiffTile) * kDiffStatsTile + row % kDiffTile;
-    d1 = st[2 * kDiffTile];
-    d2 = lam < 0.f ? -st[3 * kDiffTile] : st[3 * kDiffTile];
+    d1 = -st[2 * kDiffTile];
+    d2 = d1 + (lam < 0.f ? -st[3 * kDiffTile] : st[3 * kDiffTile]);
     const float e1 = a.lse1[ri], e2 = a.lse2[ri];
     ls1 = e1 == kNegInf ? __builtin_inff() : e1 * kLog2e;
     ls2 = e2 == kNegInf ? __builtin_inff() : e2 * kLog2e;
@@ -221,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
     }
   };
 
-  stream_tiles<C::STAGES_Q, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
+  stream_tiles<C::STAGES_Q, 1, C::STAGE, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
 
   const size_t rows = (size_t)bh * a.NQ;
   void *o1 = a.dq1, *o2 = a.dq2;
@@ -254,9 +267,9 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
   using C = DiffBwdCfg<D, DV, PART>;
   constexpr bool WANT_K = (PART & 1) != 0, WANT_V = (PART & 2) != 0;
   constexpr int KD = D / 16, KV = DV / 16, ND = D / 32, NV = DV / 32;
-  __shared__ u32x4 st0[C::STAGE + C::STATS];
-  __shared__ u32x4 st1[C::STAGE + C::STATS];
-  __shared__ u32x4 st2[C::STAGES_K == 3 ? C::STAGE + C::STATS : 1];
+  __shared__ u32x4 st0[C::TR_K * (C::STAGE + C::STATS)];
+  __shared__ u32x4 st1[C::TR_K * (C::STAGE + C::STATS)];
+  __shared__ u32x4 st2[C::STAGES_K == 3 ? C::TR_K * (C::STAGE + C::STATS) : 1];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int T = (a.NK + C::ROWS - 1) / C::ROWS, G = a.H / a.HK;
@@ -361,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
     auto rd_st = [&](f32x4 (&g)[4], int which, int i) {
       if (i < 16) g[i >> 2] = st[8 * which + 2 * (i >> 2) + half];
     };
-    f32x16 s1 = zero16(), s2 = zero16(), dp = zero16();
+    f32x16 s1 = zero16(), s2 = zero16(), dp;
     float e1[16], e2[16], p[16];
     const bool mask = (a.causal && kw + 31 > r0 + off) || kw + 32 > klen;
     auto hide = [&](f32x16& s) {
@@ -396,6 +409,14 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
       diff_pin();
     }
     rd_st(gb, 1, 0);
+    if constexpr (WANT_K && C::START_D) {
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) rd_st(ga, 2, i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dp[i] = ga[i >> 2][i & 3];
+    } else {
+      dp = zero16();
+    }
     if (mask) hide(s2);
     diff_pin();
     bf16x8 ap[2];
@@ -423,19 +444,20 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
     bf16x8 a1[2], a2[2];
     auto grad = [&](int i) {
       if (i % 4 == 0) {
-        rd_st(ga, 2, i + 4);
         rd_st(gb, 3, i + 4);
+        if (!C::START_D) rd_st(ga, 2, i + 4);
       }
-      e1[i] *= dp[i] - ga[i >> 2][i & 3];
-      e2[i] *= __builtin_fmaf(nsign, dp[i], gb[i >> 2][i & 3]);
+      const float y = C::START_D ? dp[i] : dp[i] + ga[i >> 2][i & 3];   // dP - D_1
+      e1[i] *= y;
+      e2[i] *= __builtin_fmaf(nsign, y, gb[i >> 2][i & 3]);
       if (i % 8 == 7) {
         a1[i / 8] = pack8(e1 + i - 7);
         a2[i / 8] = pack8(e2 + i - 7);
       }
     };
     if constexpr (WANT_K) {
-      rd_st(ga, 2, 0);
       rd_st(gb, 3, 0);
+      if (!C::START_D) rd_st(ga, 2, 0);
       diff_pin();
       if constexpr (!WANT_V) {
 #pragma unroll
@@ -477,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
     }
   };
 
-  stream_tiles<C::STAGES_K, DiffDma<D, DV, C::NT>::NCH + 1>(st0, st1, st2, s_begin, s_end, load, tile);
+  stream_tiles<C::STAGES_K, C::TR_K, C::STAGE + C::STATS, DiffDma<D, DV, C::NT>::NCH + 1>(st0, st1, st2, s_begin, s_end, load, tile);
 
   const size_t rows = (size_t)bk * a.NK;
   void *o1 = a.dk1, *o2 = a.dk2, *o3 = a.dv_out;

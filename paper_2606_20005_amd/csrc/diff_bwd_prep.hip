@@ -50,8 +50,9 @@ __global__ void __launch_bounds__(kThreads) diff_bwd_prep_kernel(const DiffArgs 
       const bool none = e1 == kNegInf || e2 == kNegInf;   // sees nothing: P = 0, and no NaN from its sums
       st[r] = none ? __builtin_inff() : e1 * kLog2e;
       st[kDiffTile + r] = none ? __builtin_inff() : e2 * kLog2e - l2lam;
-      st[2 * kDiffTile + r] = none ? 0.f : __builtin_fmaf(lam, s2, s1);
-      st[3 * kDiffTile + r] = none ? 0.f : lam < 0.f ? -s2 : s2;
+      const float d1 = __builtin_fmaf(lam, s2, s1);
+      st[2 * kDiffTile + r] = none ? 0.f : -d1;
+      st[3 * kDiffTile + r] = none ? 0.f : lam < 0.f ? d1 - s2 : s2 - d1;
     }
   }
 }

@@ -127,36 +127,45 @@ struct DiffDma {
   }
 };
 
-// Streams tiles t0 .. t1 - 1 through STAGES (2 or 3) LDS stages: while a tile is
-// worked on, the loads of the next one or two are in flight. load(t, stage)
-// starts the loads of a tile, NLOAD instructions of this wave; tile(t, stage)
-// works on it. The stages are separate arrays, named explicitly, so that the
-// compiler can tell reads of one from loads into another. With two, s2 is unused.
-template <int STAGES, int NLOAD, typename Load, typename Tile>
+// Streams tiles t0 .. t1 - 1 through STAGES (2 or 3) LDS stages of TR (1 or 2)
+// tiles, CHUNKS chunks apart: while the tiles of one are worked on, the loads
+// of the next one or two are in flight, and the workgroup meets once a stage.
+// load(t, place) starts the loads of a tile, NLOAD instructions of this wave;
+// tile(t, place) works on it. The stages are separate arrays, named
+// explicitly, so that the compiler can tell reads of one from loads into
+// another. With two, s2 is unused.
+template <int STAGES, int TR, int CHUNKS, int NLOAD, typename Load, typename Tile>
 __device__ __forceinline__ void stream_tiles(u32x4* s0, u32x4* s1, u32x4* s2, int t0, int t1, Load load, Tile tile) {
-  static_assert(STAGES == 2 || STAGES == 3, "two or three stages");
-  if (t0 < t1) load(t0, s0);
-  if (STAGES == 3 && t0 + 1 < t1) {
-    load(t0 + 1, s1);
-    wait_vmem_le<NLOAD>();
-  } else {
-    wait_vmem();
-  }
+  static_assert((STAGES == 2 || STAGES == 3) && (TR == 1 || TR == 2), "two or three stages of one or two tiles");
+  auto fill = [&](u32x4* s, int t) {
+#pragma unroll
+    for (int i = 0; i < TR; ++i)
+      if (t + i < t1) load(t + i, s + i * CHUNKS);
+  };
+  // all loads but those of the stage that begins with tile t have landed
+  auto wait_but = [&](int t) {
+    if (STAGES == 3 && t + TR <= t1) wait_vmem_le<TR * NLOAD>();
+    else if (STAGES == 3 && TR == 2 && t < t1) wait_vmem_le<NLOAD>();
+    else wait_vmem();
+  };
+  fill(s0, t0);
+  if (STAGES == 3) fill(s1, t0 + TR);
+  wait_but(t0 + TR);
   barrier_no_fence();
   auto step = [&](u32x4* cur, u32x4* ahead, int t) {
-    const bool more = t + STAGES - 1 < t1;
-    if (more) load(t + STAGES - 1, ahead);
-    tile(t, cur);
-    if (STAGES == 3 && more) wait_vmem_le<NLOAD>();
-    else wait_vmem();
+    fill(ahead, t + (STAGES - 1) * TR);
+#pragma unroll
+    for (int i = 0; i < TR; ++i)
+      if (i == 0 || t + i < t1) tile(t + i, cur + i * CHUNKS);
+    wait_but(t + (STAGES - 1) * TR);
     wait_lds();
     barrier_no_fence();
   };
-  for (int t = t0; t < t1; t += STAGES) {
+  for (int t = t0; t < t1; t += STAGES * TR) {
     step(s0, STAGES == 3 ? s2 : s1, t);
-    if (t + 1 < t1) step(s1, s0, t + 1);
+    if (t + TR < t1) step(s1, s0, t + TR);
     if constexpr (STAGES == 3) {
-      if (t + 2 < t1) step(s2, s1, t + 2);
+      if (t + 2 * TR < t1) step(s2, s1, t + 2 * TR);
     }
   }
 }

@@ -26,9 +26,11 @@
 // same relative precision at any size. So the rescaling of O (DV / 2 multiplies
 // a lane and block) runs about once per row, not once per tile.
 //
-// Rounding: P to bf16 (each term of O is off by at most 2^-8 of itself, the
-// sum l keeps the float32 p), O to bf16 once at the end; everything else is
-// float32.
+// Rounding: P to bf16 (each term of O is off by at most 2^-8 of itself), O to
+// bf16 once at the end; everything else is float32. The sum l takes the
+// float32 p: with the rounded ones (two at a time by dot products, half of the
+// additions) the log-sum-exps, and with them the recomputed probabilities of
+// the backward pass and dlam, were off by up to 1e-3.
 //
 // splits > 1: blockIdx.y takes a contiguous range of the key tiles and leaves
 // unnormalised float32 sums and their reference in `part`; a second kernel
@@ -233,7 +235,7 @@ diff_fwd_kernel(const DiffArgs a) {
     }
   };
 
-  stream_tiles<C::STAGES, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
+  stream_tiles<C::STAGES, 1, C::STAGE, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
 
 #pragma unroll
   for (int x = 0; x < RB; ++x) l[x] += __shfl_xor(l[x], 32);

@@ -84,10 +84,6 @@ template <int D, int DV, int RB, int NW>
 struct FwdPick {
   using C = DiffFwdCfg<D, DV, RB, NW>;
   static constexpr int rows() { return C::ROWS; }
-  static constexpr int resident() {
-    constexpr int by_lds = 160 * 1024 / C::LDS, by_waves = 4 * C::WAVES / NW;
-    return kCus * (by_lds < by_waves ? by_lds : by_waves);
-  }
   static hipError_t launch(const DiffArgs& a) {
     const long long R = (long long)a.NQ * (a.H / a.HK);
     const unsigned grid = (unsigned)((long long)a.B * a.HK * ((R + C::ROWS - 1) / C::ROWS));
@@ -118,10 +114,6 @@ auto pick(int d, int dv, long long rows, F f) {
 
 int diff_fwd_rows(int d, int dv, long long rows) {
   return pick(d, dv, rows, [](auto p) { return p.rows(); });
-}
-
-int diff_fwd_resident(int d, int dv, long long rows) {
-  return pick(d, dv, rows, [](auto p) { return p.resident(); });
 }
 
 hipError_t launch_diff_fwd(const DiffArgs& a) {

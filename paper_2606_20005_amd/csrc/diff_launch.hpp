@@ -34,9 +34,8 @@ auto diff_by_dims(int d, int dv, F f) {
 template <int D, int DV>
 constexpr bool kDiffWideKeys = D + DV > 256;
 
-// Forward: rows per workgroup for NQ rows of G heads, and workgroups resident on the chip.
+// Forward: rows per workgroup where a key head serves `rows` packed rows.
 int diff_fwd_rows(int d, int dv, long long rows);
-int diff_fwd_resident(int d, int dv, long long rows);
 hipError_t launch_diff_fwd(const DiffArgs& a);
 hipError_t launch_diff_merge(const DiffArgs& a);
 

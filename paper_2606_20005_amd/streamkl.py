@@ -461,14 +461,14 @@ def rope_table(n_pos, rot_dim, base=10000.0, device="cuda"):
 
 def _rows(t, name, batch=0, head=1, row=2):
     """A tensor with contiguous 16-byte aligned rows as a streamkl_rows; batch, head and row are its axes."""
-    es, shape, stride = t.element_size(), t.shape, t.stride()
-    if stride[3] != 1 and shape[3] != 1:
+    n, st, p = t.shape, t.stride(), t.data_ptr()
+    if st[3] != 1 and n[3] != 1:
         raise ValueError(f"{name} must be contiguous along its last axis")
-    ptr = t.data_ptr()
-    st = [0 if shape[a] <= 1 else stride[a] for a in (batch, head, row)]   # the stride of one element says nothing
-    if ptr % 16 or any(x * es % 16 for x in st):
+    # the stride of an extent of one says nothing
+    sb, sh, sn = st[batch] if n[batch] > 1 else 0, st[head] if n[head] > 1 else 0, st[row] if n[row] > 1 else 0
+    if p & 15 or (sb | sh | sn) & (3 if t.dtype is torch.float32 else 7):
         raise ValueError(f"the rows of {name} must begin at multiples of 16 bytes")
-    return _Rows(ptr, *st)
+    return _Rows(p, sb, sh, sn)
 
 
 def _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k):
@@ -662,28 +662,29 @@ def _diff_inputs(q1, k1, q2, k2, v, lam, q_len, kv_len):
     for n, t in (("q1", q1), ("k1", k1), ("q2", q2), ("k2", k2), ("v", v)):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise ValueError(f"{n} must be a GPU tensor")
-        if t.dtype != torch.bfloat16:
+        if t.dtype is not torch.bfloat16:
             raise ValueError(f"{n} must be bfloat16, got {t.dtype}")
         if t.dim() != 4:
             raise ValueError(f"{n} must be a [B, H, N, d] tensor")
-    B, H, NQ, d = q1.shape
-    HK, NK = k1.shape[1:3]
-    dv = v.shape[3]
-    if q2.shape != q1.shape or k2.shape != k1.shape or k1.shape[0] != B or k1.shape[3] != d or \
-            tuple(v.shape) != (B, HK, NK, dv):
-        raise ValueError(f"inconsistent shapes q1{tuple(q1.shape)} k1{tuple(k1.shape)} q2{tuple(q2.shape)} "
-                         f"k2{tuple(k2.shape)} v{tuple(v.shape)}")
+    qs, ks, vs = q1.shape, k1.shape, v.shape
+    B, H, NQ, d = qs
+    kb, HK, NK, kd = ks
+    if q2.shape != qs or k2.shape != ks or kb != B or kd != d or vs[:3] != ks[:3]:
+        raise ValueError(f"inconsistent shapes q1{tuple(qs)} k1{tuple(ks)} q2{tuple(q2.shape)} "
+                         f"k2{tuple(k2.shape)} v{tuple(vs)}")
     if (HK == 0) != (H == 0) or (HK and H % HK):
         raise ValueError(f"{H} query heads do not share {HK} key heads evenly")
     dev = q1.device
-    if any(t.device != dev for t in (k1, q2, k2, v)):
+    if k1.device != dev or q2.device != dev or k2.device != dev or v.device != dev:
         raise ValueError("all inputs must be on one device")
+    if not isinstance(lam, torch.Tensor):
+        raise ValueError("lam must be a float32 tensor")
     _f32_rows(lam, (H,), dev, "lam")
     for n, t in (("q_len", q_len), ("kv_len", kv_len)):
         if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_contiguous() or
                               t.device != dev):
             raise ValueError(f"{n} must be a contiguous int32 tensor of shape {(B,)} on {dev}")
-    return dev, (B, H, HK, NQ, NK, d, dv)
+    return dev, (B, H, HK, NQ, NK, d, vs[3])
 
 
 def _diff_scale(scale, d):
