@@ -464,10 +464,9 @@ int streamkl_diff_fwd(const streamkl_rows* q1, const streamkl_rows* k1, const st
                       int splits, void* workspace, size_t workspace_bytes,
                       void* out, void* out2, float* lse1, float* lse2, hipStream_t stream);
 
-/* Split count of the library for these extents: as many as give two workgroups per CU, of four tiles each at least,
-   fewer where the partials would outweigh the keys and values; 1 where the single pass fills the chip. 0 for invalid
-   or unsupported arguments. */
-int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int N_K, int d, int dv);
+/* Split count of the library for these extents: the one with the least estimated time (1 where the single pass fills
+   the chip). Sequence lengths are not known to it. 0 for invalid or unsupported arguments. */
+int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int N_K, int d, int dv, int causal);
 
 /* Workspace bytes of streamkl_diff_fwd: 8 * splits * B * H * N_Q * (dv + 2) when splits > 1, else 0. */
 size_t streamkl_diff_fwd_workspace_bytes(int B, int H, int N_Q, int dv, int splits);

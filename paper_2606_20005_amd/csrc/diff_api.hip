@@ -133,24 +133,38 @@ int hip_status(hipError_t e) { return e == hipSuccess ? STREAMKL_OK : STREAMKL_E
 
 }  // namespace
 
-// Two workgroups per CU where the single pass has fewer than half of that;
-// four tiles a range at least; and no more partials (written and read back in
-// float32) than three quarters of the bytes of the keys and values. Measured, us:
-// 16 sequences x 4 key heads x 65536 keys, one row each, d 64/128: 512
-// workgroups 357, 1024 362, 1536 393, 4096 411; 2 key heads x 66000, 61 rows of
-// 4 heads each, d 128/256: 256 workgroups 93, 384 101, 1024 129, 2048 200.
-extern "C" int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int N_K, int d, int dv) {
+// The split count with the least estimated time. A workgroup takes 0.07 us for
+// an MFMA of a tile where two share a CU, 0.045 alone (measured 0.065 to 0.08
+// and 0.04 to 0.05 over the head dims); a grid of up to two workgroups per CU
+// takes as long as its longest range, a larger one as many rounds, causal ones
+// (longest block first) their share of the pairs. Keys and values come at 5.5
+// TB/s from 512 workgroups on; the float32 partials are written and read back
+// at 4 TB/s by a second launch.
+extern "C" int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int N_K, int d, int dv, int causal) {
   if (check_extents(B, H, HK, N_Q, N_K, d, dv) != STREAMKL_OK) return 0;
   if ((long long)B * H * N_Q == 0) return 1;
   const long long R = (long long)N_Q * (H / HK);
-  const int rows = streamkl::diff_fwd_rows(d, dv, R);
-  const long long base = (long long)B * HK * ((R + rows - 1) / rows), tiles = (N_K + 31LL) / 32;
-  long long s = 2LL * streamkl::kCus / base;
-  if (s > tiles / 4) s = tiles / 4;
-  const double partials = 2.0 * 8.0 * B * H * (double)N_Q * (dv + 2), bytes = 2.0 * B * HK * (double)N_K * (2 * d + dv);
-  if (s * partials > 0.75 * bytes) s = (long long)(0.75 * bytes / partials);
-  if (s > streamkl::kDiffMaxSplits) s = streamkl::kDiffMaxSplits;
-  return s < 2 ? 1 : (int)s;
+  const streamkl::DiffFwdShape w = streamkl::diff_fwd_shape(d, dv, R);
+  const long long base = (long long)B * HK * ((R + w.rows - 1) / w.rows), tiles = (N_K + 31LL) / 32;
+  const double partials = 16.0 * B * H * (double)N_Q * (dv + 2);
+  const double bytes = 2.0 * B * HK * (double)N_K * (2 * d + dv);
+  // share of the pairs that a causal mask leaves
+  const double share = !causal ? 1.0 : N_Q <= N_K ? 1.0 - 0.5 * N_Q / N_K : 0.5 * N_K / N_Q;
+  const double slots = 2.0 * streamkl::kCus;
+  int best = 1;
+  double least = 0;
+  for (long long s = 1; s <= streamkl::kDiffMaxSplits && (s == 1 || (s * 4 <= tiles && base * s <= 4 * slots)); ++s) {
+    const double wgs = (double)base * s, even = share * wgs / slots;
+    const double rounds = wgs <= slots || even < 1 ? 1 : causal || wgs > 4 * slots ? even : std::ceil(wgs / slots);
+    const double work = rounds * tiles / s * w.mfmas * (wgs > 0.5 * slots ? 0.07 : 0.045);
+    const double mem = bytes / 5.5e6 * (wgs < slots ? slots / wgs : 1.0);
+    const double t = (work > mem ? work : mem) + (s > 1 ? partials * s / 4e6 + 6.0 : 0.0);
+    if (s == 1 || t < 0.95 * least) {
+      best = (int)s;
+      least = t;
+    }
+  }
+  return best;
 }
 
 extern "C" size_t streamkl_diff_fwd_workspace_bytes(int B, int H, int N_Q, int dv, int splits) {

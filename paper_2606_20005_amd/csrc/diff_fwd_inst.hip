@@ -7,8 +7,70 @@ namespace streamkl {
 
 namespace {
 
-// Joins the partials of one output row (see diff_fwd.hpp). A quarter-column
-// group of four floats per lane; the groups of lanes share the splits.
+constexpr int kFewSplits = 8;
+
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
+
+// Writes four columns of an output row from its joined maps.
+__device__ __forceinline__ void write_joined(const DiffArgs& a, long long row, int col4, bool ok, f32x4 o1, float f1,
+                                             f32x4 o2, float f2, float lam) {
+  bf16x4 r, r2;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float v2 = ok ? o2[j] * f2 : 0.f;
+    r2[j] = (__bf16)v2;
+    r[j] = (__bf16)(ok ? __builtin_fmaf(-lam, v2, o1[j] * f1) : 0.f);
+  }
+  *reinterpret_cast<bf16x4*>(a.out + row * a.dv + 4 * col4) = r;
+  if (a.out2) *reinterpret_cast<bf16x4*>(a.out2 + row * a.dv + 4 * col4) = r2;
+}
+
+// Joins the partials of output rows (see diff_fwd.hpp) where there are few of
+// each: one wave per row, four columns a lane. (One workgroup per row took 80
+// us for 48056 rows of two partials, of which their bytes are 44.)
+__global__ void __launch_bounds__(kThreads) diff_merge_few_kernel(const DiffArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long long rows = (long long)a.B * a.H * a.NQ;
+  const long long row = (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const int bh = (int)(row / a.NQ), i = (int)(row - (long long)bh * a.NQ), b = bh / a.H, h = bh - b * a.H;
+  const bool ok = i < clamp_len(a.q_len, b, a.NQ);
+  const int S = a.splits, cols = a.dv / 4;
+  const float* po = a.part + row * S * 2 * a.dv;
+  const float* pm = a.part + rows * S * 2 * a.dv + row * S * 4;
+  float ref[2][kFewSplits], top[2] = {kNegInf, kNegInf}, sum[2] = {0.f, 0.f};
+  f32x4 o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  if (ok) {
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        ref[m][s] = s < S ? pm[(s * 2 + m) * 2] : kNegInf;
+        top[m] = fmaxf(top[m], ref[m][s]);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+      if (s < S) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const float f = ref[m][s] == kNegInf ? 0.f : exp2_fast(ref[m][s] - top[m]);
+          sum[m] = __builtin_fmaf(f, pm[(s * 2 + m) * 2 + 1], sum[m]);
+          if (lane < cols) o[m] += reinterpret_cast<const f32x4*>(po + (s * 2 + m) * a.dv)[lane] * f;
+        }
+      }
+    }
+  }
+  if (lane < cols) write_joined(a, row, lane, ok, o[0], inverse_sum(sum[0]), o[1], inverse_sum(sum[1]), a.lam[h]);
+  if (lane < 2) {
+    float* lse = lane ? a.lse2 : a.lse1;
+    const float t = lane ? top[1] : top[0], l = lane ? sum[1] : sum[0];
+    if (lse) lse[row] = !ok || t == kNegInf ? kNegInf : (log2f(l) + t) * kLn2;
+  }
+}
+
+// The same for many partials of few rows: one workgroup per row, whose groups
+// of lanes share the splits.
 __global__ void __launch_bounds__(kThreads) diff_merge_kernel(const DiffArgs a) {
   __shared__ float w[2][kDiffMaxSplits];
   __shared__ float top[2], total[2];
@@ -62,17 +124,7 @@ __global__ void __launch_bounds__(kThreads) diff_merge_kernel(const DiffArgs a) 
       o1 += acc[0][g * cols + tid];
       o2 += acc[1][g * cols + tid];
     }
-    auto inverse = [](float l) { return l > 0.f || l != l ? 1.f / l : 0.f; };
-    const float f1 = ok ? inverse(total[0]) : 0.f, f2 = ok ? inverse(total[1]) : 0.f, lam = a.lam[h];
-    bf16x4 r, r2;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float v2 = ok ? o2[j] * f2 : 0.f;
-      r2[j] = (__bf16)v2;
-      r[j] = (__bf16)(ok ? __builtin_fmaf(-lam, v2, o1[j] * f1) : 0.f);
-    }
-    *reinterpret_cast<bf16x4*>(a.out + row * a.dv + 4 * tid) = r;
-    if (a.out2) *reinterpret_cast<bf16x4*>(a.out2 + row * a.dv + 4 * tid) = r2;
+    write_joined(a, row, tid, ok, o1, inverse_sum(total[0]), o2, inverse_sum(total[1]), a.lam[h]);
   }
   if (tid < 2) {
     float* lse = tid ? a.lse2 : a.lse1;
@@ -83,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) diff_merge_kernel(const DiffArgs a) 
 template <int D, int DV, int RB, int NW>
 struct FwdPick {
   using C = DiffFwdCfg<D, DV, RB, NW>;
-  static constexpr int rows() { return C::ROWS; }
+  static constexpr DiffFwdShape shape() { return {C::ROWS, RB * (D / 16 + DV / 16)}; }
   static hipError_t launch(const DiffArgs& a) {
     const long long R = (long long)a.NQ * (a.H / a.HK);
     const unsigned grid = (unsigned)((long long)a.B * a.HK * ((R + C::ROWS - 1) / C::ROWS));
@@ -112,8 +164,8 @@ auto pick(int d, int dv, long long rows, F f) {
 
 }  // namespace
 
-int diff_fwd_rows(int d, int dv, long long rows) {
-  return pick(d, dv, rows, [](auto p) { return p.rows(); });
+DiffFwdShape diff_fwd_shape(int d, int dv, long long rows) {
+  return pick(d, dv, rows, [](auto p) { return p.shape(); });
 }
 
 hipError_t launch_diff_fwd(const DiffArgs& a) {
@@ -121,7 +173,12 @@ hipError_t launch_diff_fwd(const DiffArgs& a) {
 }
 
 hipError_t launch_diff_merge(const DiffArgs& a) {
-  hipLaunchKernelGGL(diff_merge_kernel, dim3((unsigned)((long long)a.B * a.H * a.NQ)), dim3(kThreads), 0, a.stream, a);
+  const long long rows = (long long)a.B * a.H * a.NQ;
+  if (a.splits <= kFewSplits && rows >= 8 * kCus)   // fewer waves than that would not hide a walk over the partials
+    hipLaunchKernelGGL(diff_merge_few_kernel, dim3((unsigned)((rows + kThreads / 64 - 1) / (kThreads / 64))),
+                       dim3(kThreads), 0, a.stream, a);
+  else
+    hipLaunchKernelGGL(diff_merge_kernel, dim3((unsigned)rows), dim3(kThreads), 0, a.stream, a);
   return hipGetLastError();
 }
 

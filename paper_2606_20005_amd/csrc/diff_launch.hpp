@@ -34,8 +34,11 @@ auto diff_by_dims(int d, int dv, F f) {
 template <int D, int DV>
 constexpr bool kDiffWideKeys = D + DV > 256;
 
-// Forward: rows per workgroup where a key head serves `rows` packed rows.
-int diff_fwd_rows(int d, int dv, long long rows);
+// Forward: rows per workgroup where a key head serves `rows` packed rows, and a wave's MFMAs per tile.
+struct DiffFwdShape {
+  int rows, mfmas;
+};
+DiffFwdShape diff_fwd_shape(int d, int dv, long long rows);
 hipError_t launch_diff_fwd(const DiffArgs& a);
 hipError_t launch_diff_merge(const DiffArgs& a);
 

@@ -85,7 +85,7 @@ def _load():
     lib.streamkl_diff_fwd.argtypes = [rows, rows, rows, rows, rows, i, i, i, i, i, i, i, f, i, vp, vp, vp, i, vp, sz,
                                       vp, vp, vp, vp, vp]
     lib.streamkl_diff_fwd.restype = i
-    lib.streamkl_diff_fwd_split_count.argtypes = [i, i, i, i, i, i, i]
+    lib.streamkl_diff_fwd_split_count.argtypes = [i, i, i, i, i, i, i, i]
     lib.streamkl_diff_fwd_split_count.restype = i
     lib.streamkl_diff_fwd_workspace_bytes.argtypes = [i, i, i, i, i]
     lib.streamkl_diff_fwd_workspace_bytes.restype = sz
@@ -691,9 +691,10 @@ def _diff_scale(scale, d):
     return 1.0 / math.sqrt(d) if scale is None else float(scale)
 
 
-def diff_split_count(B, H, HK, n_q, n_k, d, dv) -> int:
-    """streamkl_diff_fwd_split_count (0 for invalid arguments)."""
-    return int(lib.streamkl_diff_fwd_split_count(int(B), int(H), int(HK), int(n_q), int(n_k), int(d), int(dv)))
+def diff_split_count(B, H, HK, n_q, n_k, d, dv, causal=False) -> int:
+    """streamkl_diff_fwd_split_count: the library's choice of splits (0 for invalid arguments)."""
+    return int(lib.streamkl_diff_fwd_split_count(int(B), int(H), int(HK), int(n_q), int(n_k), int(d), int(dv),
+                                                 int(bool(causal))))
 
 
 def diff_workspace_bytes(B, H, n_q, dv, splits) -> int:
@@ -722,7 +723,7 @@ def diff_fwd(q1, k1, q2, k2, v, lam, scale=None, causal=False, q_len=None, kv_le
     the split workspace is allocated here unless ``workspace`` (diff_workspace_bytes) is given."""
     dev, ext = _diff_inputs(q1, k1, q2, k2, v, lam, q_len, kv_len)
     B, H, HK, NQ, NK, d, dv = ext
-    n = lib.streamkl_diff_fwd_split_count(*ext) or 1 if splits == "auto" else int(splits)
+    n = lib.streamkl_diff_fwd_split_count(*ext, int(bool(causal))) or 1 if splits == "auto" else int(splits)
     out = _bf16_out(out, (B, H, NQ, dv), dev, "out")
     out2 = lse1 = lse2 = None
     if save:
