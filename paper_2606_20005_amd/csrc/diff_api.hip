@@ -89,8 +89,10 @@ int check_inputs(const streamkl_rows* q1, const streamkl_rows* k1, const streamk
 // float32 gradients a further kernel adds up. The number of ranges is the one
 // with the least estimated time: rounds of resident workgroups times steps,
 // about 0.042 us an MFMA and resident wave of a SIMD (measured 0.038 to 0.048), and the
-// partials written and read back at 4 TB/s. Measured (us, split against not):
-// see diff_bwd.hpp.
+// partials written and read back at 4 TB/s. Measured, us, one range and the
+// choice: dQ of 16 heads x 64 rows against 65536 keys, d 128/128, 2196 and 186;
+// dK dV of 4 x 12 heads x 1021 on 4 key heads, d 96/160 causal, 200 and 144;
+// both of 8 heads x 6007, d 128/128, 465 and 415, 811 and 643.
 struct GradSplits {
   int q, k;
   size_t part_floats;
@@ -103,9 +105,9 @@ int grad_splits(long long blocks, int waves, long long steps, bool causal, int m
   for (int s = 1; s <= streamkl::kDiffMaxGradSplits; ++s) {
     if (s > 1 && steps < 4LL * s) break;
     const double rounds = (double)blocks * s / slots, each = (double)steps / s;
-    // causal blocks are handed out longest first and are half as long on average
+    // causal blocks are handed out longest first and are half as long on average; a part of the longest is left over
     const double filled = std::ceil(rounds) * each, even = 0.5 * rounds * each;
-    double t = (causal ? (even > each ? even : each) : rounds > 8 ? rounds * each : filled) * us;
+    double t = (causal ? (even > each ? even : each) + 0.15 * each : rounds > 8 ? rounds * each : filled) * us;
     if (s > 1) t += (s + 1) * bytes / 4e6 + 8.0;
     if (s == 1 || t < 0.95 * least) {
       best = s;

@@ -43,7 +43,7 @@ hipError_t launch_diff_fwd(const DiffArgs& a);
 hipError_t launch_diff_merge(const DiffArgs& a);
 
 // Backward. Blocks of 128 rows (keys).
-constexpr int kDiffMaxGradSplits = 16;
+constexpr int kDiffMaxGradSplits = 64;
 inline int diff_row_blocks(int n) { return (int)((n + 127LL) / 128); }
 size_t diff_bwd_stats_floats(int B, int H, int NQ);
 size_t diff_bwd_dlam_floats(int B, int H, int NQ, int q_splits);
