@@ -393,7 +393,7 @@ typedef struct {
  *             head, as streamkl_fwd reads them.
  *   yq, yk    bf16, contiguous [B, H, N_Q, d] and [B, HK k_copies, N_K, d],
  *             16-byte aligned. Sums and products are float32, rounded once.
- * At most 2^31 - 1 heads of tokens (B N H) a tensor, else
+ * At most 2^31 - 2^16 heads of tokens (B N H) a tensor, else
  * STREAMKL_ERR_UNSUPPORTED.
  */
 int streamkl_qk_norm_rope_fwd(const streamkl_rows* q, const streamkl_rows* k, int B, int H, int HK, int N_Q, int N_K,

@@ -83,6 +83,11 @@ int check_inputs(const streamkl_rows* q1, const streamkl_rows* k1, const streamk
   return STREAMKL_OK;
 }
 
+// Share of the pairs that the mask leaves.
+double visible_share(int N_Q, int N_K, int causal) {
+  return !causal ? 1.0 : N_Q <= N_K ? 1.0 - 0.5 * N_Q / N_K : 0.5 * N_K / N_Q;
+}
+
 // Ranges of the streamed axis in the backward kernels. A kernel's blocks own
 // 128 rows (keys) and walk over all keys (rows) of their head; where that
 // leaves the chip unevenly filled, the walk is cut into ranges whose partial
@@ -98,16 +103,16 @@ struct GradSplits {
   size_t part_floats;
 };
 
-int grad_splits(long long blocks, int waves, long long steps, bool causal, int mfmas, double bytes) {
+int grad_splits(long long blocks, int waves, long long steps, double share, int mfmas, double bytes) {
   const double slots = 256.0 * waves, us = 0.042 * mfmas * waves;
   int best = 1;
   double least = 0;
   for (int s = 1; s <= streamkl::kDiffMaxGradSplits; ++s) {
     if (s > 1 && steps < 4LL * s) break;
     const double rounds = (double)blocks * s / slots, each = (double)steps / s;
-    // causal blocks are handed out longest first and are half as long on average; a part of the longest is left over
-    const double filled = std::ceil(rounds) * each, even = 0.5 * rounds * each;
-    double t = (causal ? (even > each ? even : each) + 0.15 * each : rounds > 8 ? rounds * each : filled) * us;
+    const double filled = rounds > 8 ? rounds * each : std::ceil(rounds) * each, even = share * rounds * each;
+    // causal blocks are handed out longest first; a part of the longest is left over
+    double t = (share > 0.75 ? filled : (even > each ? even : each) + 0.15 * each) * us;
     if (s > 1) t += (s + 1) * bytes / 4e6 + 8.0;
     if (s == 1 || t < 0.95 * least) {
       best = s;
@@ -123,9 +128,9 @@ GradSplits bwd_splits(int B, int H, int HK, int N_Q, int N_K, int d, int dv, int
   const int kd = d <= 64 ? 64 : 128, kv = (dv + 63) / 64 * 64;
   const long long q_floats = 2LL * B * H * N_Q * d, k_floats = (long long)B * HK * N_K * (2 * d + dv);
   g.q = grad_splits((long long)B * H * streamkl::diff_row_blocks(N_Q), streamkl::diff_bwd_dq_waves(d, dv),
-                    (N_K + 31LL) / 32, causal != 0, kd / 4 + kv / 16, 4.0 * q_floats);
+                    (N_K + 31LL) / 32, visible_share(N_Q, N_K, causal), kd / 4 + kv / 16, 4.0 * q_floats);
   g.k = grad_splits((long long)B * HK * streamkl::diff_row_blocks(N_K), streamkl::diff_bwd_dkv_waves(d, dv),
-                    (long long)(H / HK) * ((N_Q + 31LL) / 32), causal != 0, kd / 4 + kv / 8, 4.0 * k_floats);
+                    (long long)(H / HK) * ((N_Q + 31LL) / 32), visible_share(N_Q, N_K, causal), kd / 4 + kv / 8, 4.0 * k_floats);
   const long long q_part = g.q > 1 ? g.q * q_floats : 0, k_part = g.k > 1 ? g.k * k_floats : 0;
   g.part_floats = (size_t)(q_part > k_part ? q_part : k_part);
   return g;
@@ -150,8 +155,7 @@ extern "C" int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int 
   const long long base = (long long)B * HK * ((R + w.rows - 1) / w.rows), tiles = (N_K + 31LL) / 32;
   const double partials = 16.0 * B * H * (double)N_Q * (dv + 2);
   const double bytes = 2.0 * B * HK * (double)N_K * (2 * d + dv);
-  // share of the pairs that a causal mask leaves
-  const double share = !causal ? 1.0 : N_Q <= N_K ? 1.0 - 0.5 * N_Q / N_K : 0.5 * N_K / N_Q;
+  const double share = visible_share(N_Q, N_K, causal);
   const double slots = 2.0 * streamkl::kCus;
   int best = 1;
   double least = 0;

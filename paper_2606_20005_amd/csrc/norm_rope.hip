@@ -399,13 +399,13 @@ int lanes_per_row(int d) { return d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32
 // leave the chip 16 waves a CU, at most 8.
 void plan(NrSide& s, int d, int most_blocks) {
   const int rpw = 64 / lanes_per_row(d);
-  const int groups = (s.tokens + rpw - 1) / rpw;
+  const int groups = (int)((s.tokens + rpw - 1LL) / rpw);
   int hpi = 1;
-  while (hpi < 8 && hpi < s.H && (long long)groups * ((s.H + 2 * hpi - 1) / (2 * hpi)) >= 16LL * kCus) hpi *= 2;
+  while (hpi < 8 && hpi < s.H && (long long)groups * ((s.H + 2LL * hpi - 1) / (2 * hpi)) >= 16LL * kCus) hpi *= 2;
   s.heads_per_item = hpi;
-  s.chunks = (s.H + hpi - 1) / hpi;
+  s.chunks = (int)((hpi - 1LL + s.H) / hpi);
   s.items = groups * s.chunks;
-  s.blocks = (s.items + kWaves - 1) / kWaves;
+  s.blocks = (int)((s.items + kWaves - 1LL) / kWaves);
   if (most_blocks > 0 && s.blocks > most_blocks) s.blocks = most_blocks;
 }
 
@@ -415,18 +415,23 @@ constexpr int kBwdBlocks = 8 * kCus;
 
 bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// Heads of tokens are counted in 31 bits, with room for a stride past the end.
+bool countable(int B, int N, int H) {
+  constexpr long long most = 0x7fff0000LL;
+  const long long tokens = (long long)B * N;
+  return tokens <= most && tokens * H <= most;
+}
+
 int elem_size(int dtype) { return dtype == STREAMKL_F32 ? 4 : 2; }
 
 // One side: extents, strides, positions, the tensor it writes. `present`: the
 // side has rows.
 int check_side(const streamkl_rows* x, int B, int N, int H, int copies, int dtype, const float* w, const void* pos,
                int pos64, const void* y, bool* present) {
-  *present = x != nullptr && (long long)B * N * H != 0;
+  *present = x != nullptr && B != 0 && N != 0 && H != 0;
   if (!x) return STREAMKL_OK;
   if (N < 0 || H < 0 || copies < 1) return STREAMKL_ERR_INVALID_ARG;
-  if ((long long)B * N > 0x7fffffffLL || (long long)H * copies > 0x7fffffffLL) return STREAMKL_ERR_UNSUPPORTED;
-  // items: at most one per token and head
-  if ((long long)B * N * H > 0x7fffffffLL) return STREAMKL_ERR_UNSUPPORTED;
+  if (!countable(B, N, H) || (long long)H * copies > 0x7fff0000LL) return STREAMKL_ERR_UNSUPPORTED;
   if (!*present) return STREAMKL_OK;
   const int per16 = 16 / elem_size(dtype);
   if (!x->data || !aligned_to(x->data, 16)) return STREAMKL_ERR_INVALID_ARG;
@@ -549,7 +554,7 @@ extern "C" int streamkl_qk_norm_rope_fwd(const streamkl_rows* q, const streamkl_
 
 extern "C" size_t streamkl_qk_norm_rope_bwd_workspace_bytes(int B, int H, int HK, int N_Q, int N_K, int d) {
   if (B < 0 || H < 0 || HK < 0 || N_Q < 0 || N_K < 0 || d < 32 || d > 256) return 0;
-  if ((long long)B * N_Q > 0x7fffffffLL || (long long)B * N_K > 0x7fffffffLL) return 0;
+  if (!countable(B, N_Q, H) || !countable(B, N_K, HK)) return 0;
   NrSide q = {}, k = {};
   q.tokens = B * N_Q;
   q.H = H;

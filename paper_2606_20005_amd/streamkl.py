@@ -9,12 +9,19 @@ not been built; there is no fallback implementation.
     kl, lse1, lse2 = fwd_split(q1, k1, q2, k2, s1, s2, causal, direction, splits="auto")
     dQ1, dK1, dQ2, dK2 = bwd(q1, k1, q2, k2, kl, lse1, lse2, dkl, ..., want=("dq2", "dk2"), strategy="auto")
     loss = attention_kl(q1, k1, q2, k2, causal=True).mean(); loss.backward()
+
+The operators around it:
+
+    yq, yk = qk_norm_rope(q, k, wq, wk, rope_table(n, rot))           # projections -> normed, rotated, head-major
+    loss = attention_kl_proj(q1, k1, q2, k2, QKPrep(...), QKPrep(...), causal=True).mean()
+    out = diff_attention(q1, k1, q2, k2, v, lam, causal=True)         # (softmax map 1 - lam * softmax map 2) v
 """
 from __future__ import annotations
 
 import ctypes
 import math
 import os
+import typing
 
 import torch
 
@@ -652,6 +659,29 @@ def qk_norm_rope(q, k, wq=None, wk=None, table=None, *, eps=1e-6, q_positions=No
         return _QKNormRope.apply(q, k, wq, wk, table, float(eps), q_positions, k_positions, bool(interleaved),
                                  bool(expand_k))
     return qk_norm_rope_fwd(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k)
+
+
+class QKPrep(typing.NamedTuple):
+    """How the projections of one side become its queries and keys: the arguments of qk_norm_rope."""
+    wq: torch.Tensor | None = None
+    wk: torch.Tensor | None = None
+    table: torch.Tensor | None = None
+    eps: float = 1e-6
+    interleaved: bool = False
+
+
+def attention_kl_proj(q1, k1, q2, k2, prep1=QKPrep(), prep2=QKPrep(), *, q_positions=None, k_positions=None, **kl):
+    """attention_kl from the projections of both sides, before norm and rotation.
+
+    q1, q2 [B, N_Q, H, d_t] and k1, k2 [B, N_K, HK_t, d_t] as qk_norm_rope takes them (H a multiple of each side's
+    HK_t; shared key heads are written once per query head). prep1, prep2: QKPrep of the sides. Positions are shared by
+    them. The other options are attention_kl's. Gradients reach the projections and the norms' weights that require them.
+    """
+    sides = []
+    for q, k, p in ((q1, k1, prep1), (q2, k2, prep2)):
+        sides += qk_norm_rope(q, k, p.wq, p.wk, p.table, eps=p.eps, q_positions=q_positions, k_positions=k_positions,
+                              interleaved=p.interleaved, expand_k=True)
+    return attention_kl(*sides, **kl)
 
 
 # --- differential attention -------------------------------------------------------------------------------------------

@@ -185,6 +185,33 @@ def test_reproducible_on_streams_and_in_graphs(gpu_lib):
             assert torch.equal(a, b)
 
 
+def test_attention_kl_from_projections(gpu_lib):
+    """attention_kl_proj is the norms, the rotation and attention_kl in a row: the divergence of the prepared tensors
+    against its own oracle, gradients equal to those of the steps taken one by one."""
+    import oracle
+    B, N, H, d1, d2 = 1, 80, 4, 64, 32
+    gen = torch.Generator(device="cuda").manual_seed(31)
+    mk = lambda *s: torch.randn(s, generator=gen, device="cuda")   # noqa: E731
+    q1, k1, q2, k2 = mk(B, N, H, d1).bfloat16(), mk(B, N, 2, d1).bfloat16(), mk(B, N, H, d2), mk(B, N, 1, d2)
+    w = [(1 + 0.2 * mk(d)).requires_grad_(d == d2) for d in (d1, d1, d2, d2)]
+    t1, t2 = gpu_lib.rope_table(N, d1), gpu_lib.rope_table(N, 16)
+    q2.requires_grad_(True), k2.requires_grad_(True)
+    p1, p2 = gpu_lib.QKPrep(w[0], w[1], t1), gpu_lib.QKPrep(w[2], w[3], t2, 1e-5, True)
+    kl = gpu_lib.attention_kl_proj(q1, k1, q2, k2, p1, p2, causal=True)
+    leaves = [q2, k2, w[2], w[3]]
+    got = torch.autograd.grad(kl.sum(), leaves)
+    a1, b1 = gpu_lib.qk_norm_rope(q1, k1, w[0], w[1], t1, expand_k=True)
+    a2, b2 = gpu_lib.qk_norm_rope(q2, k2, w[2], w[3], t2, eps=1e-5, interleaved=True, expand_k=True)
+    step = gpu_lib.attention_kl(a1, b1, a2, b2, causal=True)
+    assert torch.equal(kl, step)
+    for a, b in zip(got, torch.autograd.grad(step.sum(), leaves)):
+        assert torch.equal(a, b) and torch.isfinite(a).all() and a.any()
+    ref = oracle.forward(*(n64(x) for x in (a1, b1, a2, b2)), d1 ** -0.5, d2 ** -0.5, True, 0)[0]
+    assert (np.abs(n64(kl) - ref) <= 1e-3 + 1e-2 * np.abs(ref)).all()   # the bound that the divergence's own tests use
+    rev = gpu_lib.attention_kl_proj(q1, k1, q2, k2, p1, p2, causal=True, direction="rev", return_lse=True)
+    assert len(rev) == 3 and not torch.equal(rev[0], kl)
+
+
 def test_refusals(gpu_lib):
     q, k, wq, wk = make(2, 6, 6, 4, 2, 64, 64)
     t = gpu_lib.rope_table(6, 64)
