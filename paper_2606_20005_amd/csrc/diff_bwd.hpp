@@ -10,6 +10,21 @@
 // are reproducible bit for bit. That costs 16 d + 6 dv operations a pair where
 // a single pass with atomic adds would need 12 d + 4 dv.
 //
+// Order of a tile, pinned: logits of map 1; logits of map 2 beside the
+// exponentials of map 1; dP beside those of map 2; (dV beside the logit
+// gradients;) dQ or dK. Streamed operands are read from LDS a few MFMAs ahead.
+// Left to itself the compiler forms all products, then all vector work, and
+// reads each operand right before its MFMA (d 64/128, 32 heads x 4096 causal:
+// dQ 272 -> 257 us, dK dV 518 -> 392 in this order). Where two waves share a
+// SIMD, raised priority in the gradient MFMAs lets the vector work of the other
+// one fill their gaps (d 64/64, 16 heads x 4096: 208 -> 201, 249 -> 241).
+//
+// What bounds it: issue. At d 64/128 a tile of the key-owned kernel takes 32
+// MFMAs (1024 cycles of the matrix pipe) and about 330 instructions, 184 of
+// them vector ones, which one wave issues in 1850 cycles of 3200; timing
+// variants without the loads, the exponentials, the statistics or the
+// transpose reads are 3 to 6% faster each.
+//
 // The logit tile of the first contraction lies in the registers as the A
 // operand of the second (its 16-row k-blocks are a permutation of the 32
 // rows); the other operand comes from the streamed tile by transpose reads.
@@ -62,17 +77,6 @@ struct DiffBwdCfg {
   // 16 heads x 4096: 259 -> 291 us).
   static constexpr bool START_D = WAVES_K == 1;
 };
-
-// One 32 x 32 block of raw products streamed x resident: A = rows of the
-// streamed tile (matrix at `tile`), B = resident operands.
-template <int D>
-__device__ __forceinline__ f32x16 diff_product(const u32x4* tile, const bf16x8 (&op)[D / 16], int lane) {
-  f32x16 s = zero16();
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks)
-    s = mfma32(lds_row8<D / 8>(tile, lane & 31, 2 * ks + (lane >> 5)), op[ks], s);
-  return s;
-}
 
 // ---------------------------------------------------------------------------
 // dQ: workgroup = 128 query rows of one head, streams tiles [K_1 | K_2 | V].
@@ -220,6 +224,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
 #pragma unroll
     for (int i = 0; i < 8; ++i) grad(i);
     diff_pin();
+    if constexpr (C::WAVES_Q == 2) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = J3; j < J4; ++j) {
       rd(j + LA);
@@ -232,6 +237,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
       }
       diff_pin();
     }
+    if constexpr (C::WAVES_Q == 2) __builtin_amdgcn_s_setprio(0);
   };
 
   stream_tiles<C::STAGES_Q, 1, C::STAGE, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
@@ -465,6 +471,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
         diff_pin();
       }
     }
+    if constexpr (C::WAVES_K == 2) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = J3; j < J4; ++j) {
       rd(j + LA);
@@ -487,6 +494,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
       else g2[n] = mfma32(a2[u], buf[j], g2[n]);
       diff_pin();
     }
+    if constexpr (C::WAVES_K == 2) __builtin_amdgcn_s_setprio(0);
   };
   auto tile = [&](int, const u32x4* stage) {
     const int r0 = (t_first + ct) * kDiffTile;

@@ -378,8 +378,15 @@ norm_rope_dw_kernel(const float* __restrict__ pq, int nq, float* __restrict__ dw
   if (!out) return;
   const int rows = keys ? nk : nq;
   const int col = blockIdx.x * kDwCols + threadIdx.x % kDwCols, r0 = threadIdx.x / kDwCols;
+  // eight loads in flight: one after the other, 2048 partial rows took 11 us
   float v = 0.f;
-  for (int r = r0; r < rows; r += kDwRows) v += p[(long long)r * d + col];
+  for (int r = r0; r < rows; r += 8 * kDwRows) {
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = r + u * kDwRows < rows ? p[(long long)(r + u * kDwRows) * d + col] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += x[u];
+  }
   red[r0][threadIdx.x % kDwCols] = v;
   __syncthreads();
   if (threadIdx.x < kDwCols) {

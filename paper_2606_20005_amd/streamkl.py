@@ -24,6 +24,7 @@ import os
 import typing
 
 import torch
+from torch.autograd.function import once_differentiable
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libstreamkl.so")
 
@@ -39,6 +40,7 @@ ENTRY_POINTS = ("streamkl_fwd", "streamkl_bwd", "streamkl_bwd_ex", "streamkl_bwd
                 "streamkl_supported_head_dim", "streamkl_qk_norm_rope_fwd", "streamkl_qk_norm_rope_bwd",
                 "streamkl_qk_norm_rope_bwd_workspace_bytes", "streamkl_diff_fwd", "streamkl_diff_fwd_split_count",
                 "streamkl_diff_fwd_workspace_bytes", "streamkl_diff_bwd", "streamkl_diff_bwd_workspace_bytes")
+_MAX_INT = 0x7fffffff   # the ABI's extents; ctypes would cut a larger one silently
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
@@ -521,6 +523,8 @@ def _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k):
                              f"{dev}")
     if q_positions is not None and k_positions is not None and q_positions.dtype != k_positions.dtype:
         raise ValueError("q_positions and k_positions must have one type")
+    if max(B, NQ, NK, H, HK, n_pos) > _MAX_INT:
+        raise ValueError("an extent does not fit 31 bits")
     if table is not None and q is not None and k is not None and q_positions is None and NQ > NK:
         raise ValueError("more queries than keys: their positions have to be given")
     copies = 1
@@ -606,38 +610,24 @@ class _QKNormRope(torch.autograd.Function):
         return qk_norm_rope_fwd(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gq, gk):
         q, k, wq, wk, table, q_positions, k_positions = ctx.saved_tensors
         eps, interleaved, expand_k = ctx.cfg
         need = ctx.needs_input_grad
-        # an output that the loss does not reach has no gradient; the positions of the other do not change by that
-        if gq is not None:
-            gq = gq.contiguous()
-        if gk is not None:
-            gk = gk.contiguous()
-        if gq is not None and gk is not None and gq.dtype != gk.dtype:
-            gq, gk = gq.float(), gk.float()
         if gq is None and gk is None:
             return (None,) * 10
-        if (gq is None or gk is None) and q is not None and k is not None:
-            return (*_one_side(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k),
-                    *(None,) * 6)
+        # the gradient of an output that the loss does not reach is zero
+        if gq is None and q is not None:
+            gq = torch.zeros((q.shape[0], q.shape[2], q.shape[1], q.shape[3]), dtype=torch.bfloat16, device=q.device)
+        if gk is None and k is not None:
+            heads = q.shape[2] if expand_k else k.shape[2]
+            gk = torch.zeros((k.shape[0], heads, k.shape[1], k.shape[3]), dtype=torch.bfloat16, device=k.device)
+        gq, gk = (None if g is None else g.contiguous() for g in (gq, gk))
         dq, dk, dwq, dwk = qk_norm_rope_bwd(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved,
                                             expand_k, want_w=need[2] or need[3])
         return (dq if need[0] else None, dk if need[1] else None, dwq if need[2] else None, dwk if need[3] else None,
                 *(None,) * 6)
-
-
-def _one_side(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k):
-    """Gradients where only one of the two outputs has an upstream gradient: the other's is zero."""
-    if gq is None:
-        gq = torch.zeros((q.shape[0], q.shape[2], q.shape[1], q.shape[3]), dtype=gk.dtype, device=q.device)
-    else:
-        heads = q.shape[2] if expand_k else k.shape[2]
-        gk = torch.zeros((k.shape[0], heads, k.shape[1], k.shape[3]), dtype=gq.dtype, device=k.device)
-    dq, dk, dwq, dwk = qk_norm_rope_bwd(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved,
-                                        expand_k)
-    return dq, dk, None if wq is None else dwq, None if wk is None else dwk
 
 
 def qk_norm_rope(q, k, wq=None, wk=None, table=None, *, eps=1e-6, q_positions=None, k_positions=None,
@@ -702,6 +692,8 @@ def _diff_inputs(q1, k1, q2, k2, v, lam, q_len, kv_len):
     if q2.shape != qs or k2.shape != ks or kb != B or kd != d or vs[:3] != ks[:3]:
         raise ValueError(f"inconsistent shapes q1{tuple(qs)} k1{tuple(ks)} q2{tuple(q2.shape)} "
                          f"k2{tuple(k2.shape)} v{tuple(vs)}")
+    if NQ > _MAX_INT or NK > _MAX_INT or B > _MAX_INT or H > _MAX_INT:
+        raise ValueError("an extent does not fit 31 bits")
     if (HK == 0) != (H == 0) or (HK and H % HK):
         raise ValueError(f"{H} query heads do not share {HK} key heads evenly")
     dev = q1.device
@@ -824,6 +816,7 @@ class _DiffAttention(torch.autograd.Function):
         return saved[0]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q1, k1, q2, k2, v, lam, q_len, kv_len, *saved = ctx.saved_tensors
         scale, causal = ctx.cfg
@@ -846,6 +839,10 @@ def diff_attention(q1, k1, q2, k2, v, lam, *, scale=None, causal=False, q_len=No
     causal: bottom-right alignment, as everywhere in this library. q_len, kv_len: int32 [B] on the device; sequence b
     has its first q_len[b] rows and kv_len[b] keys (a right-padded batch, caches filled to different lengths). Rows
     behind q_len and rows that see no key give 0. scale defaults to 1/sqrt(d).
+
+    To capture a training step into a HIP graph, capture it while no eager graph of the same leaves is alive (drop the
+    warm-up's outputs first): autograd's accumulation nodes of an eager graph belong to its stream, and torch ends the
+    process where a captured backward meets them. The same holds for qk_norm_rope and attention_kl.
     """
     scale = _diff_scale(scale, q1.shape[-1])
     if torch.is_grad_enabled() and any(t.requires_grad for t in (q1, k1, q2, k2, v, lam)):

@@ -259,6 +259,54 @@ def test_reproducible_on_streams_and_in_graphs(gpu_lib):
             assert torch.equal(a, b)
 
 
+def test_captured_training_step(gpu_lib):
+    """A whole step through autograd (norm, rotation, attention, gradients) recorded into a graph, with the warm-up's
+    graph gone; replayed several times with new inputs and eager work in between."""
+    B, N, H, d = 2, 60, 4, 64
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    mk = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()   # noqa: E731
+    leaves = [mk(B, N, 2 * H, d), mk(B, N, 2 * H, d), mk(B, N, H, d), 1 + 0.1 * torch.randn(d, device="cuda"),
+              torch.rand(H, device="cuda")]
+    leaves = [t.requires_grad_(True) for t in leaves]
+    table, do = gpu_lib.rope_table(N, d), mk(B, H, N, d)
+
+    def step():
+        yq, yk = gpu_lib.qk_norm_rope(leaves[0], leaves[1], leaves[3], None, table)
+        (q1, q2), (k1, k2) = yq.split(H, 1), yk.split(H, 1)
+        out = gpu_lib.diff_attention(q1, k1, q2, k2, leaves[2].transpose(1, 2), leaves[4], causal=True)
+        return [out.detach(), *torch.autograd.grad(out, leaves, do)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(4):
+        with torch.no_grad():
+            for t in leaves[:3]:
+                t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+        ref = step()
+        for t in out:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(ref, out):
+            assert torch.equal(a, b), i
+
+
+def test_second_derivatives_are_refused(gpu_lib):
+    args, do = make(1, 1, 1, 8, 8, 64, 64)
+    q = args[0].requires_grad_(True)
+    g, = torch.autograd.grad(gpu_lib.diff_attention(q, *args[1:]), q, do.requires_grad_(True), create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(g.float().sum(), q)
+
+
 def test_inputs_are_untouched(gpu_lib):
     args, do = make(1, 2, 1, 70, 90, 96, 160)
     before = [a.clone() for a in (*args, do)]
