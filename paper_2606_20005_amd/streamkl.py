@@ -480,52 +480,69 @@ def _rows(t, name, batch=0, head=1, row=2):
     return _Rows(p, sb, sh, sn)
 
 
-def _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k):
-    """Checked arguments of the norm-and-rotation calls: (device, B, H, HK, N_Q, N_K, d, n_pos, rot, copies)."""
-    first = q if q is not None else k
-    if first is None:
-        raise ValueError("q and k are both None")
+def _bf16_out(t, shape, dev, name):
+    if t is None:
+        return torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    if t.dtype is not torch.bfloat16 or t.shape != shape or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name} must be a contiguous bfloat16 tensor of shape {shape} on {dev}")
+    return t
+
+
+def _prep_error(q, k):
+    """What is wrong with the tensors of a norm-and-rotation call."""
     for n, t in (("q", q), ("k", k)):
         if t is None:
             continue
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise ValueError(f"{n} must be a GPU tensor")
+            return ValueError(f"{n} must be a GPU tensor")
         if t.dtype not in DTYPES:
-            raise ValueError(f"{n} must be bfloat16, float16 or float32, got {t.dtype}")
+            return ValueError(f"{n} must be bfloat16, float16 or float32, got {t.dtype}")
         if t.dim() != 4:
-            raise ValueError(f"{n} must be a [B, N, H, d] tensor")
-        if t.dtype != first.dtype or t.device != first.device or t.shape[0] != first.shape[0] or \
-                t.shape[3] != first.shape[3]:
-            raise ValueError("q and k must have one type, device, batch and head dim")
-    dev, d = first.device, first.shape[3]
+            return ValueError(f"{n} must be a [B, N, H, d] tensor")
+    return ValueError("q and k must have one type, device, batch and head dim")
+
+
+def _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k):
+    """Checked arguments of the norm-and-rotation calls: (device, B, H, HK, N_Q, N_K, d, n_pos, rot, copies)."""
+    first = k if q is None else q
+    if first is None:
+        raise ValueError("q and k are both None")
+    if not (isinstance(first, torch.Tensor) and first.is_cuda and first.dim() == 4 and first.dtype in DTYPES):
+        raise _prep_error(q, k)
+    dev = first.device
+    B, N, heads, d = first.shape
+    NQ, H, NK, HK = (0, 0, N, heads) if q is None else (N, heads, 0, 0)
+    if q is not None and k is not None:
+        if not (isinstance(k, torch.Tensor) and k.dtype is first.dtype and k.device == dev and k.dim() == 4):
+            raise _prep_error(q, k)
+        kb, NK, HK, kd = k.shape
+        if kb != B or kd != d:
+            raise _prep_error(q, k)
     for n, w in (("wq", wq), ("wk", wk)):
-        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous() or
-                              w.device != dev):
+        if w is not None and not (w.dtype is torch.float32 and w.shape == (d,) and w.is_contiguous() and
+                                  w.device == dev):
             raise ValueError(f"{n} must be a contiguous float32 tensor of shape {(d,)} on {dev}")
     n_pos = rot = 0
     if table is not None:
-        if table.dtype != torch.float32 or table.dim() != 2 or not table.is_contiguous() or table.device != dev:
+        if not (table.dtype is torch.float32 and table.dim() == 2 and table.is_contiguous() and table.device == dev):
             raise ValueError(f"table must be a contiguous float32 [positions, rot_dim] tensor on {dev}")
         n_pos, rot = table.shape
         if rot <= 0 or rot > d or rot % 16:
             raise ValueError(f"the table's rot_dim must be a multiple of 16 up to the head dim {d}, got {rot}")
-    B = first.shape[0]
-    NQ, H = (q.shape[1], q.shape[2]) if q is not None else (0, 0)
-    NK, HK = (k.shape[1], k.shape[2]) if k is not None else (0, 0)
     for n, p, t, rows in (("q_positions", q_positions, q, NQ), ("k_positions", k_positions, k, NK)):
         if p is None:
             continue
         if t is None:
             raise ValueError(f"{n} given without {n[0]}")
-        if p.dtype not in (torch.int32, torch.int64) or tuple(p.shape) not in ((rows,), (B, rows)) or \
+        if p.dtype not in (torch.int32, torch.int64) or (p.shape != (B, rows) and p.shape != (rows,)) or \
                 not p.is_contiguous() or p.device != dev:
             raise ValueError(f"{n} must be a contiguous int32 or int64 tensor of shape {(rows,)} or {(B, rows)} on "
                              f"{dev}")
     if q_positions is not None and k_positions is not None and q_positions.dtype != k_positions.dtype:
         raise ValueError("q_positions and k_positions must have one type")
-    if max(B, NQ, NK, H, HK, n_pos) > _MAX_INT:
+    if B > _MAX_INT or NQ > _MAX_INT or NK > _MAX_INT or H > _MAX_INT or HK > _MAX_INT or n_pos > _MAX_INT:
         raise ValueError("an extent does not fit 31 bits")
-    if table is not None and q is not None and k is not None and q_positions is None and NQ > NK:
+    if NQ > NK and table is not None and k is not None and q is not None and q_positions is None:
         raise ValueError("more queries than keys: their positions have to be given")
     copies = 1
     if expand_k:
@@ -552,20 +569,15 @@ def qk_norm_rope_fwd(q, k, wq=None, wk=None, table=None, eps=1e-6, q_positions=N
     ``out`` may hold the two outputs, preallocated."""
     cfg = _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k)
     dev, B, H, HK, NQ, NK, d, _, _, copies = cfg
-    shapes = (None if q is None else (B, H, NQ, d), None if k is None else (B, HK * copies, NK, d))
-    ys = []
-    for n, shape, t in zip(("yq", "yk"), shapes, out or (None, None)):
-        if shape is not None and t is not None and (t.dtype != torch.bfloat16 or tuple(t.shape) != shape or
-                                                    not t.is_contiguous() or t.device != dev):
-            raise ValueError(f"{n} must be a contiguous bfloat16 tensor of shape {shape} on {dev}")
-        ys.append(None if shape is None else t if t is not None else torch.empty(shape, dtype=torch.bfloat16,
-                                                                                 device=dev))
+    yq, yk = out or (None, None)
+    yq = None if q is None else _bf16_out(yq, (B, H, NQ, d), dev, "yq")
+    yk = None if k is None else _bf16_out(yk, (B, HK * copies, NK, d), dev, "yk")
     args = _prep_args(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, cfg)
     with _on(dev):
-        st = lib.streamkl_qk_norm_rope_fwd(*args, _p(ys[0]), _p(ys[1]), _stream(dev))
+        st = lib.streamkl_qk_norm_rope_fwd(*args, _p(yq), _p(yk), _stream(dev))
     if st != OK:
         raise StreamKLError(st, "streamkl_qk_norm_rope_fwd")
-    return tuple(ys)
+    return yq, yk
 
 
 def qk_norm_rope_bwd(q, k, dyq, dyk, wq=None, wk=None, table=None, eps=1e-6, q_positions=None, k_positions=None,
@@ -645,7 +657,8 @@ def qk_norm_rope(q, k, wq=None, wk=None, table=None, *, eps=1e-6, q_positions=No
     of (j, j + rot_dim/2). expand_k: write every key head once per query head of its group, so that yk has H heads (the
     gradients of the copies are added).
     """
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, wq, wk)):
+    if torch.is_grad_enabled() and (q is not None and q.requires_grad or k is not None and k.requires_grad or
+                                    wq is not None and wq.requires_grad or wk is not None and wk.requires_grad):
         return _QKNormRope.apply(q, k, wq, wk, table, float(eps), q_positions, k_positions, bool(interleaved),
                                  bool(expand_k))
     return qk_norm_rope_fwd(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k)
@@ -677,36 +690,44 @@ def attention_kl_proj(q1, k1, q2, k2, prep1=QKPrep(), prep2=QKPrep(), *, q_posit
 # --- differential attention -------------------------------------------------------------------------------------------
 
 
-def _diff_inputs(q1, k1, q2, k2, v, lam, q_len, kv_len):
-    """Checked extents of the differential-attention calls: (device, (B, H, HK, N_Q, N_K, d, dv))."""
+def _diff_error(q1, k1, q2, k2, v):
+    """What is wrong with the tensors of a differential-attention call."""
     for n, t in (("q1", q1), ("k1", k1), ("q2", q2), ("k2", k2), ("v", v)):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise ValueError(f"{n} must be a GPU tensor")
-        if t.dtype is not torch.bfloat16:
-            raise ValueError(f"{n} must be bfloat16, got {t.dtype}")
+            return ValueError(f"{n} must be a GPU tensor")
+        if t.dtype != torch.bfloat16:
+            return ValueError(f"{n} must be bfloat16, got {t.dtype}")
         if t.dim() != 4:
-            raise ValueError(f"{n} must be a [B, H, N, d] tensor")
-    qs, ks, vs = q1.shape, k1.shape, v.shape
+            return ValueError(f"{n} must be a [B, H, N, d] tensor")
+    if len({t.device for t in (q1, k1, q2, k2, v)}) != 1:
+        return ValueError("all inputs must be on one device")
+    return ValueError(f"inconsistent shapes q1{tuple(q1.shape)} k1{tuple(k1.shape)} q2{tuple(q2.shape)} "
+                      f"k2{tuple(k2.shape)} v{tuple(v.shape)}")
+
+
+def _diff_inputs(q1, k1, q2, k2, v, lam, q_len, kv_len):
+    """Checked extents of the differential-attention calls: (device, (B, H, HK, N_Q, N_K, d, dv))."""
+    for t in (q1, k1, q2, k2, v):
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.dim() == 4):
+            raise _diff_error(q1, k1, q2, k2, v)
+    dev, qs, ks = q1.device, q1.shape, k1.shape
     B, H, NQ, d = qs
     kb, HK, NK, kd = ks
-    if q2.shape != qs or k2.shape != ks or kb != B or kd != d or vs[:3] != ks[:3]:
-        raise ValueError(f"inconsistent shapes q1{tuple(qs)} k1{tuple(ks)} q2{tuple(q2.shape)} "
-                         f"k2{tuple(k2.shape)} v{tuple(vs)}")
+    vb, vh, vn, dv = v.shape
+    if q2.shape != qs or k2.shape != ks or kb != B or kd != d or vb != B or vh != HK or vn != NK or \
+            k1.device != dev or q2.device != dev or k2.device != dev or v.device != dev:
+        raise _diff_error(q1, k1, q2, k2, v)
     if NQ > _MAX_INT or NK > _MAX_INT or B > _MAX_INT or H > _MAX_INT:
         raise ValueError("an extent does not fit 31 bits")
     if (HK == 0) != (H == 0) or (HK and H % HK):
         raise ValueError(f"{H} query heads do not share {HK} key heads evenly")
-    dev = q1.device
-    if k1.device != dev or q2.device != dev or k2.device != dev or v.device != dev:
-        raise ValueError("all inputs must be on one device")
-    if not isinstance(lam, torch.Tensor):
-        raise ValueError("lam must be a float32 tensor")
-    _f32_rows(lam, (H,), dev, "lam")
+    if not (isinstance(lam, torch.Tensor) and lam.dtype is torch.float32 and lam.shape == (H,) and
+            lam.is_contiguous() and lam.device == dev):
+        raise ValueError(f"lam must be a contiguous float32 tensor of shape {(H,)} on {dev}")
     for n, t in (("q_len", q_len), ("kv_len", kv_len)):
-        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_contiguous() or
-                              t.device != dev):
+        if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.device != dev):
             raise ValueError(f"{n} must be a contiguous int32 tensor of shape {(B,)} on {dev}")
-    return dev, (B, H, HK, NQ, NK, d, vs[3])
+    return dev, (B, H, HK, NQ, NK, d, dv)
 
 
 def _diff_scale(scale, d):
@@ -728,14 +749,6 @@ def diff_bwd_workspace_bytes(B, H, HK, n_q, n_k, d, dv, causal) -> int:
     """streamkl_diff_bwd_workspace_bytes: workspace of the backward."""
     return int(lib.streamkl_diff_bwd_workspace_bytes(int(B), int(H), int(HK), int(n_q), int(n_k), int(d), int(dv),
                                                      int(bool(causal))))
-
-
-def _bf16_out(t, shape, dev, name):
-    if t is None:
-        return torch.empty(shape, dtype=torch.bfloat16, device=dev)
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != dev:
-        raise ValueError(f"{name} must be a contiguous bfloat16 tensor of shape {shape} on {dev}")
-    return t
 
 
 def diff_fwd(q1, k1, q2, k2, v, lam, scale=None, causal=False, q_len=None, kv_len=None, splits="auto", save=False,
@@ -845,6 +858,7 @@ def diff_attention(q1, k1, q2, k2, v, lam, *, scale=None, causal=False, q_len=No
     process where a captured backward meets them. The same holds for qk_norm_rope and attention_kl.
     """
     scale = _diff_scale(scale, q1.shape[-1])
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (q1, k1, q2, k2, v, lam)):
+    if torch.is_grad_enabled() and (q1.requires_grad or k1.requires_grad or q2.requires_grad or k2.requires_grad or
+                                    v.requires_grad or lam.requires_grad):
         return _DiffAttention.apply(q1, k1, q2, k2, v, lam, scale, bool(causal), q_len, kv_len)
     return diff_fwd(q1, k1, q2, k2, v, lam, scale, causal, q_len, kv_len)
