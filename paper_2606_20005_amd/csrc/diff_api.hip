@@ -161,7 +161,10 @@ extern "C" int streamkl_diff_fwd_split_count(int B, int H, int HK, int N_Q, int 
   double least = 0;
   for (long long s = 1; s <= streamkl::kDiffMaxSplits && (s == 1 || (s * 4 <= tiles && base * s <= 4 * slots)); ++s) {
     const double wgs = (double)base * s, even = share * wgs / slots;
-    const double rounds = wgs <= slots || even < 1 ? 1 : causal || wgs > 4 * slots ? even : std::ceil(wgs / slots);
+    // a last round of at most one workgroup per CU runs at 0.045 / 0.07
+    const double whole = std::floor(wgs / slots), left = wgs - whole * slots;
+    const double filled = whole + (left == 0 ? 0.0 : left <= 0.5 * slots ? 0.64 : 1.0);
+    const double rounds = wgs <= slots || even < 1 ? 1 : causal || wgs > 4 * slots ? even : filled;
     const double work = rounds * tiles / s * w.mfmas * (wgs > 0.5 * slots ? 0.07 : 0.045);
     const double mem = bytes / 5.5e6 * (wgs < slots ? slots / wgs : 1.0);
     const double t = (work > mem ? work : mem) + (s > 1 ? partials * s / 4e6 + 6.0 : 0.0);
