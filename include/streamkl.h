@@ -434,8 +434,7 @@ size_t streamkl_qk_norm_rope_bwd_workspace_bytes(int B, int H, int HK, int N_Q, 
  *             that streamkl_rows can express with row strides below 2^25 elements (rows of a head may span
  *             more than 4 GiB). H is a multiple of HK: groups of H / HK consecutive query heads share a key
  *             head, and their keys and values are streamed once for the group.
- *   d         a multiple of 32, 32 to 128;  dv a multiple of 32, 32 to 256. The kernels are built for 64 and 128
- *             (and 256 for dv); others run the next one up with the missing columns read as zeros.
+ *   d         a multiple of 32, 32 to 128;  dv a multiple of 32, 32 to 256.
  *   scale     2^-64 to 2^64 (usual: 1/sqrt(d)); the scaled logits must stay in the float32 range.
  *   lam       float32 [H] on the device, any sign.
  *   q_len, kv_len  int32 [B] on the device, or NULL: sequence b has its first q_len[b] rows and kv_len[b] keys

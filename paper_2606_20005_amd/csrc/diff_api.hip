@@ -6,6 +6,32 @@
 #include "diff_launch.hpp"
 #include "streamkl.h"
 
+namespace streamkl {
+namespace {
+
+// From the runtime key dim to the unit that serves it.
+DiffFwdShape diff_fwd_shape(int d, int dv, long long rows) {
+  return diff_by_key_dim(d, [&](auto kd) { return diff_fwd_shape_of<kd.value>(dv, rows); });
+}
+hipError_t launch_diff_fwd(const DiffArgs& a) {
+  return diff_by_key_dim(a.d, [&](auto kd) { return launch_diff_fwd_of<kd.value>(a); });
+}
+int diff_bwd_dq_waves(int d, int dv) {
+  return diff_by_key_dim(d, [&](auto kd) { return diff_bwd_dq_waves_of<kd.value>(dv); });
+}
+int diff_bwd_dkv_waves(int d, int dv) {
+  return diff_by_key_dim(d, [&](auto kd) { return diff_bwd_dkv_waves_of<kd.value>(dv); });
+}
+hipError_t launch_diff_bwd_dq(const DiffArgs& a) {
+  return diff_by_key_dim(a.d, [&](auto kd) { return launch_diff_bwd_dq_of<kd.value>(a); });
+}
+hipError_t launch_diff_bwd_dkv(const DiffArgs& a) {
+  return diff_by_key_dim(a.d, [&](auto kd) { return launch_diff_bwd_dkv_of<kd.value>(a); });
+}
+
+}  // namespace
+}  // namespace streamkl
+
 namespace {
 
 using streamkl::DiffArgs;
@@ -125,12 +151,11 @@ int grad_splits(long long blocks, int waves, long long steps, double share, int 
 GradSplits bwd_splits(int B, int H, int HK, int N_Q, int N_K, int d, int dv, int causal) {
   GradSplits g = {1, 1, 0};
   if ((long long)B * H * N_Q == 0 || (long long)B * HK * N_K == 0) return g;
-  const int kd = d <= 64 ? 64 : 128, kv = (dv + 63) / 64 * 64;
   const long long q_floats = 2LL * B * H * N_Q * d, k_floats = (long long)B * HK * N_K * (2 * d + dv);
   g.q = grad_splits((long long)B * H * streamkl::diff_row_blocks(N_Q), streamkl::diff_bwd_dq_waves(d, dv),
-                    (N_K + 31LL) / 32, visible_share(N_Q, N_K, causal), kd / 4 + kv / 16, 4.0 * q_floats);
+                    (N_K + 31LL) / 32, visible_share(N_Q, N_K, causal), d / 4 + dv / 16, 4.0 * q_floats);
   g.k = grad_splits((long long)B * HK * streamkl::diff_row_blocks(N_K), streamkl::diff_bwd_dkv_waves(d, dv),
-                    (long long)(H / HK) * ((N_Q + 31LL) / 32), visible_share(N_Q, N_K, causal), kd / 4 + kv / 8, 4.0 * k_floats);
+                    (long long)(H / HK) * ((N_Q + 31LL) / 32), visible_share(N_Q, N_K, causal), d / 4 + dv / 8, 4.0 * k_floats);
   const long long q_part = g.q > 1 ? g.q * q_floats : 0, k_part = g.k > 1 ? g.k * k_floats : 0;
   g.part_floats = (size_t)(q_part > k_part ? q_part : k_part);
   return g;

@@ -53,16 +53,16 @@ constexpr int kDiffStatsTile = 4 * kDiffTile;   // floats per tile
 template <int D, int DV, int PART = 3>
 struct DiffBwdCfg {
   static constexpr int NW = 4, NT = 64 * NW, ROWS = 32 * NW;
-  static constexpr int CD = D / 8, CV = DV / 8;
+  static constexpr int CD = lds_cols(D) / 8, CV = lds_cols(DV) / 8;   // chunks of a row in LDS
   static constexpr int STAGE = DiffDma<D, DV, NT>::CHUNKS;
   static constexpr int STATS = kDiffStatsTile / 4;   // chunks of prepared statistics behind a stage (dK, dV)
   // registers: gradients, resident rows, three logit tiles, about 64 for the rest
   static constexpr int REGS_Q = D + (2 * D + DV) / 4 + 48 + 64;
-  static constexpr int REGS_K = (PART & 1 ? D + DV / 4 + 16 : 0) + (PART & 2 ? DV / 2 : 0) + D / 2 + 32 + 64;
+  static constexpr int REGS_K = (PART & 1 ? D + DV / 4 + 16 : 0) + (PART & 2 ? DV / 2 : 0) + D / 2 + DV / 16 + 28 + 64;
   // 256 registers leave room for two waves per SIMD. The estimate is tight: d 64/192 meets 256 and spills in the
   // query-owned kernel (190 us with one wave, 226 with two), as does dV alone at 128/192.
   static constexpr int WAVES_Q = REGS_Q <= 248 ? 2 : 1, WAVES_K = REGS_K <= 256 - (PART == 2 ? 8 : 0) ? 2 : 1;
-  static constexpr int LA_Q = WAVES_Q == 1 ? 4 : 3, LA_K = WAVES_K == 1 ? 4 : 2;   // operand reads in flight
+  static constexpr int LA_Q = WAVES_Q == 1 ? 4 : REGS_Q > 232 ? 2 : 3, LA_K = WAVES_K == 1 ? 4 : 2;   // operand reads in flight
   // Three stages where the workgroups that the registers leave room for have
   // room for them; two tiles a stage in the key-owned kernel with one wave per
   // SIMD, which nothing else occupies while it waits for the others (d 64/128,
@@ -121,10 +121,10 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
   auto row_of = [&](const DiffRows& x) {
     return x.p + (ok ? (long long)b * x.sb + (long long)h * x.sh + (long long)row * x.sn : 0);
   };
-  load_row_operand<D>(q1, row_of(a.q1), ok, half, a.d);
-  load_row_operand<D>(q2, row_of(a.q2), ok, half, a.d);
+  load_row_operand<D>(q1, row_of(a.q1), ok, half);
+  load_row_operand<D>(q2, row_of(a.q2), ok, half);
   const long long ri = (long long)bh * a.NQ + row;
-  load_row_operand<DV>(go, a.dout + (ok ? ri * a.dv : 0), ok, half, a.dv);
+  load_row_operand<DV>(go, a.dout + (ok ? ri * DV : 0), ok, half);
   const int ntq = (a.NQ + kDiffTile - 1) / kDiffTile;
   const float lam = a.lam[h];
   float ls1 = __builtin_inff(), ls2 = ls1, d1 = 0.f, d2 = 0.f;
@@ -150,9 +150,9 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
   const uint16_t* k1 = a.k1.p + (long long)b * a.k1.sb + (long long)hk * a.k1.sh;
   const uint16_t* k2 = a.k2.p + (long long)b * a.k2.sb + (long long)hk * a.k2.sh;
   const uint16_t* vv = a.v.p + (long long)b * a.v.sb + (long long)hk * a.v.sh;
-  const DiffDma<D, DV, C::NT> dma(tid, a.d, a.dv, bk1, bk2, bv);
+  const DiffDma<D, DV, C::NT> dma(tid, bk1, bk2, bv);
   const TrCols<D> tr(lane);
-  TileRows r1(k1, bk1, a.d), r2(k2, bk2, a.d), r3(vv, bv, a.dv);
+  TileRows r1(k1, bk1, D), r2(k2, bk2, D), r3(vv, bv, DV);
   r1.skip(t_begin);
   r2.skip(t_begin);
   r3.skip(t_begin);
@@ -246,13 +246,13 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
   void *o1 = a.dq1, *o2 = a.dq2;
   bool as_bf16 = a.bf16_grads != 0;
   if (a.q_splits > 1) {
-    const long long each = (long long)a.B * a.H * a.NQ * a.d;
+    const long long each = (long long)a.B * a.H * a.NQ * D;
     as_bf16 = false;
     if (o1) o1 = a.grad_part + (2 * (long long)blockIdx.y) * each;
     if (o2) o2 = a.grad_part + (2 * (long long)blockIdx.y + 1) * each;
   }
-  if (o1) write_grad<D>(o1, as_bf16, g1, rows, rw, a.NQ, a.scale, lane, a.d);
-  if (o2) write_grad<D>(o2, as_bf16, g2, rows, rw, a.NQ, -a.scale * lam, lane, a.d);
+  if (o1) write_grad<D>(o1, as_bf16, g1, rows, rw, a.NQ, a.scale, lane);
+  if (o2) write_grad<D>(o2, as_bf16, g2, rows, rw, a.NQ, -a.scale * lam, lane);
   if (a.dlam) {
     if (!ok) dl = 0.f;
 #pragma unroll
@@ -310,9 +310,9 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
   auto row_of = [&](const DiffRows& x) {
     return x.p + (ok ? (long long)b * x.sb + (long long)hk * x.sh + (long long)key * x.sn : 0);
   };
-  load_row_operand<D>(k1, row_of(a.k1), ok, half, a.d);
-  load_row_operand<D>(k2, row_of(a.k2), ok, half, a.d);
-  if constexpr (WANT_K) load_row_operand<DV>(vv, row_of(a.v), ok, half, a.dv);
+  load_row_operand<D>(k1, row_of(a.k1), ok, half);
+  load_row_operand<D>(k2, row_of(a.k2), ok, half);
+  if constexpr (WANT_K) load_row_operand<DV>(vv, row_of(a.v), ok, half);
   wait_vmem();   // before the tile loop: a first use inside it would wait on every trip
 
   f32x16 g1[D / 32], g2[D / 32], gv[DV / 32];
@@ -324,21 +324,21 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
 #pragma unroll
   for (int n = 0; n < DV / 32; ++n) gv[n] = zero16();
 
-  const uint32_t bq1 = (uint32_t)a.q1.sn * 2u, bq2 = (uint32_t)a.q2.sn * 2u, bo = (uint32_t)a.dv * 2u;
-  const DiffDma<D, DV, C::NT> dma(tid, a.d, a.dv, bq1, bq2, bo);
+  const uint32_t bq1 = (uint32_t)a.q1.sn * 2u, bq2 = (uint32_t)a.q2.sn * 2u, bo = (uint32_t)DV * 2u;
+  const DiffDma<D, DV, C::NT> dma(tid, bq1, bq2, bo);
   const TrCols<D> trd(lane);
   const TrCols<DV> trv(lane);
   const int ntq = (a.NQ + kDiffTile - 1) / kDiffTile;
   // step u: head hk G + u / per, row tile t_first + u % per. The loads run
   // ahead, so each side keeps its own place.
   int lg = g_begin, lt = t_begin;
-  TileRows r1(nullptr, bq1, a.d), r2(nullptr, bq2, a.d), r3(nullptr, bo, a.dv);
+  TileRows r1(nullptr, bq1, D), r2(nullptr, bq2, D), r3(nullptr, bo, DV);
   const float* ps = nullptr;
   auto begin_head = [&](int h, int t0) {
     const long long bh = (long long)b * a.H + h;
     r1.p = reinterpret_cast<const char*>(a.q1.p + (long long)b * a.q1.sb + (long long)h * a.q1.sh);
     r2.p = reinterpret_cast<const char*>(a.q2.p + (long long)b * a.q2.sb + (long long)h * a.q2.sh);
-    r3.p = reinterpret_cast<const char*>(a.dout + bh * a.NQ * a.dv);
+    r3.p = reinterpret_cast<const char*>(a.dout + bh * a.NQ * DV);
     r1.skip(t_first + t0);
     r2.skip(t_first + t0);
     r3.skip(t_first + t0);
@@ -514,15 +514,15 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV, PART>::WAVES_K)) 
   bool as_bf16 = a.bf16_grads != 0;
   if (a.k_splits > 1) {
     const long long keys = (long long)a.B * a.HK * a.NK;
-    float* part = a.grad_part + blockIdx.y * keys * (2 * a.d + a.dv);
+    float* part = a.grad_part + blockIdx.y * keys * (2 * D + DV);
     as_bf16 = false;
     if (o1) o1 = part;
-    if (o2) o2 = part + keys * a.d;
-    if (o3) o3 = part + keys * 2 * a.d;
+    if (o2) o2 = part + keys * D;
+    if (o3) o3 = part + keys * 2 * D;
   }
-  if (WANT_K && o1) write_grad<D>(o1, as_bf16, g1, rows, kw, a.NK, a.scale, lane, a.d);
-  if (WANT_K && o2) write_grad<D>(o2, as_bf16, g2, rows, kw, a.NK, a.scale, lane, a.d);
-  if (WANT_V && o3) write_grad<DV>(o3, as_bf16, gv, rows, kw, a.NK, 1.f, lane, a.dv);
+  if (WANT_K && o1) write_grad<D>(o1, as_bf16, g1, rows, kw, a.NK, a.scale, lane);
+  if (WANT_K && o2) write_grad<D>(o2, as_bf16, g2, rows, kw, a.NK, a.scale, lane);
+  if (WANT_V && o3) write_grad<DV>(o3, as_bf16, gv, rows, kw, a.NK, 1.f, lane);
 }
 
 }  // namespace streamkl

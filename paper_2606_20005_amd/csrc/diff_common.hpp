@@ -16,6 +16,11 @@ namespace streamkl {
 
 constexpr int kDiffTile = 32;   // streamed rows per tile: one 32 x 32 MFMA block
 
+// The kernels are built for every head dim (a multiple of 32). In LDS a row
+// takes the next multiple of 64 columns, which the swizzles of kl_common.hpp
+// need; the columns past its end are written as zeros and never read.
+constexpr int lds_cols(int d) { return (d + 63) / 64 * 64; }
+
 // Rows [batch, head, row] with element strides; see streamkl_rows.
 struct DiffRows {
   const uint16_t* p;
@@ -54,7 +59,7 @@ __device__ __forceinline__ int clamp_len(const int* len, int b, int n) {
 }
 
 // Byte offset, from the first row of a tile, of logical chunk c of row r, or
-// kOutOfSlab for a chunk past the row's real length (a padded head dim).
+// kOutOfSlab for a chunk past the row's end.
 __device__ __forceinline__ uint32_t row_chunk_offset(int r, int c, int creal, uint32_t row_bytes) {
   return c < creal ? (uint32_t)r * row_bytes + (uint32_t)c * 16u : kOutOfSlab;
 }
@@ -85,7 +90,7 @@ struct TileRows {
 // [A | B | C], every matrix in the swizzled layout of kl_common.hpp.
 template <int DA, int DC, int NT>
 struct DiffDma {
-  static constexpr int CA = DA / 8, CC = DC / 8;
+  static constexpr int CA = lds_cols(DA) / 8, CC = lds_cols(DC) / 8;
   static constexpr int CHUNKS = kDiffTile * (2 * CA + CC);
   static constexpr int NCH = CHUNKS / NT;
   // every load instruction of a wave (64 chunks) serves one matrix; which one is known at compile time unless the
@@ -99,18 +104,18 @@ struct DiffDma {
     return p < kDiffTile * CA ? 0 : p < 2 * kDiffTile * CA ? 1 : 2;
   }
 
-  __device__ __forceinline__ DiffDma(int tid, int da_real, int dc_real, uint32_t ba, uint32_t bb, uint32_t bc) {
+  __device__ __forceinline__ DiffDma(int tid, uint32_t ba, uint32_t bb, uint32_t bc) {
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int p = tid + NT * i, m = matrix(p);
       if (m < 2) {
         const int pp = p - m * kDiffTile * CA;
         const int r = pp / CA, c = (pp - r * CA) ^ swz<CA>(r);
-        voff[i] = row_chunk_offset(r, c, da_real / 8, m == 0 ? ba : bb);
+        voff[i] = row_chunk_offset(r, c, DA / 8, m == 0 ? ba : bb);
       } else {
         const int pp = p - 2 * kDiffTile * CA;
         const int r = pp / CC, c = (pp - r * CC) ^ swz<CC>(r);
-        voff[i] = row_chunk_offset(r, c, dc_real / 8, bc);
+        voff[i] = row_chunk_offset(r, c, DC / 8, bc);
       }
     }
   }
@@ -172,11 +177,11 @@ __device__ __forceinline__ void stream_tiles(u32x4* s0, u32x4* s1, u32x4* s2, in
 
 // Byte offsets within a matrix of D columns of the transpose reads that
 // deliver, for 16-row block s, the 32 columns 32 nb + l % 32 of rows
-// 4 half + 0..3 (h = 0) and 8 + 4 half + 0..3 (h = 1): offset(nb, h) + 256 D / 8 s.
+// 4 half + 0..3 (h = 0) and 8 + 4 half + 0..3 (h = 1): offset(nb, h) + 256 CPR s.
 // Computed once and hidden from the optimizer (see TrOffsets in kl_bwd.hpp).
 template <int D>
 struct TrCols {
-  static constexpr int CPR = D / 8, NB = D / 32;
+  static constexpr int CPR = lds_cols(D) / 8, NB = D / 32;
   int o[NB][2];
   __device__ __forceinline__ explicit TrCols(int lane) {
     const int half = lane >> 5;
@@ -196,17 +201,14 @@ struct TrCols {
   }
 };
 
-// 16-byte chunks 2 ks + half of a row as MFMA operands; zeros past its end or
-// where the row does not exist.
+// 16-byte chunks 2 ks + half of a row as MFMA operands; zeros where the row
+// does not exist.
 template <int D>
-__device__ __forceinline__ void load_row_operand(bf16x8 (&op)[D / 16], const uint16_t* row, bool ok, int half,
-                                                 int dreal) {
+__device__ __forceinline__ void load_row_operand(bf16x8 (&op)[D / 16], const uint16_t* row, bool ok, int half) {
   const u32x4* p = reinterpret_cast<const u32x4*>(row);
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) {
-    const int c = 2 * ks + half;
-    op[ks] = __builtin_bit_cast(bf16x8, ok && 8 * c < dreal ? p[c] : u32x4{0u, 0u, 0u, 0u});
-  }
+  for (int ks = 0; ks < D / 16; ++ks)
+    op[ks] = __builtin_bit_cast(bf16x8, ok ? p[2 * ks + half] : u32x4{0u, 0u, 0u, 0u});
 }
 
 }  // namespace streamkl

@@ -49,10 +49,11 @@ struct DiffFwdCfg {
   static constexpr int RB = RB_, NW = NW_, NT = 64 * NW_;
   static constexpr int GROUPS = NW / 2;               // pairs of waves
   static constexpr int ROWS = 32 * RB * GROUPS;       // query rows per workgroup
+  static constexpr int CD = lds_cols(D) / 8;           // chunks of a key row in LDS
   static constexpr int STAGE = DiffDma<D, DV, NT>::CHUNKS;
   static constexpr int XCHG = GROUPS * 256;           // chunks of the exchange of one 32 x 32 block per pair
   // registers: accumulators, resident rows, logits, about 64 for the rest
-  static constexpr int REGS = RB * (DV / 2 + D / 4 + 16) + 64;
+  static constexpr int REGS = RB * (DV / 2 + D / 4 + 16) + 60 + D / 16;
   static constexpr int WAVES = REGS <= 168 ? 3 : REGS <= 256 ? 2 : 1;   // waves per SIMD
   static constexpr int LA = WAVES == 1 ? 4 : REGS > 248 ? 2 : 3;   // operand reads in flight ahead of their MFMAs
   // three stages where the workgroups that the registers leave room for have room for them too
@@ -119,7 +120,7 @@ diff_fwd_kernel(const DiffArgs a) {
     const Row w = row_of(x, lane & 31);
     limit[x] = w.ok ? limit_of(w.i) : klen;   // rows that do not exist take part unmasked, nothing reads them
     const uint16_t* p = qv.p + (w.ok ? (long long)b * qv.sb + (long long)w.h * qv.sh + (long long)w.i * qv.sn : 0);
-    load_row_operand<D>(q[x], p, w.ok, half, a.d);
+    load_row_operand<D>(q[x], p, w.ok, half);
   }
   wait_vmem();   // before the tile loop: a first use inside it would wait on every trip
 
@@ -139,9 +140,9 @@ diff_fwd_kernel(const DiffArgs a) {
   const uint16_t* k1 = a.k1.p + (long long)b * a.k1.sb + (long long)hk * a.k1.sh;
   const uint16_t* k2 = a.k2.p + (long long)b * a.k2.sb + (long long)hk * a.k2.sh;
   const uint16_t* vv = a.v.p + (long long)b * a.v.sb + (long long)hk * a.v.sh;
-  const DiffDma<D, DV, C::NT> dma(tid, a.d, a.dv, bk1, bk2, bv);
+  const DiffDma<D, DV, C::NT> dma(tid, bk1, bk2, bv);
   const TrCols<DV> tr(lane);
-  TileRows r1(k1, bk1, a.d), r2(k2, bk2, a.d), r3(vv, bv, a.dv);
+  TileRows r1(k1, bk1, D), r2(k2, bk2, D), r3(vv, bv, DV);
   r1.skip(t_begin);
   r2.skip(t_begin);
   r3.skip(t_begin);
@@ -153,11 +154,11 @@ diff_fwd_kernel(const DiffArgs a) {
   auto tile = [&](int t, const u32x4* stage) {
     const int k0 = t * kDiffTile;
     if (k0 >= wave_max) return;
-    const u32x4* kt = stage + map * kDiffTile * (D / 8);
-    constexpr int vbase = 2 * kDiffTile * (D / 8) * 16, NR = KS + 2 * NB, LA = C::LA;
+    const u32x4* kt = stage + map * kDiffTile * C::CD;
+    constexpr int vbase = 2 * kDiffTile * C::CD * 16, NR = KS + 2 * NB, LA = C::LA;
     bf16x8 buf[NR];   // streamed operands: key chunks, then value blocks; read LA of them ahead of their MFMAs
     auto rd = [&](int j) {
-      if (j < KS) buf[j] = lds_row8<D / 8>(kt, lane & 31, 2 * j + half);
+      if (j < KS) buf[j] = lds_row8<C::CD>(kt, lane & 31, 2 * j + half);
       else if (j < NR) buf[j] = tr.read(stage, vbase, (j - KS) % NB, (j - KS) / NB);
     };
     f32x16 s[RB];
@@ -256,18 +257,17 @@ diff_fwd_kernel(const DiffArgs a) {
     for (int x = 0; x < RB; ++x) {
       if (!row[x].ok) continue;
       const long long at = (out_row(x) * a.splits + blockIdx.y) * 2 + map;
-      float* po = a.part + at * a.dv;
+      float* po = a.part + at * DV;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int qd = 0; qd < 4; ++qd) {
           const int col = 32 * nb + 8 * qd + 4 * half;
-          if (col < a.dv)
-            *reinterpret_cast<f32x4*>(po + col) =
-                f32x4{o[x][nb][4 * qd], o[x][nb][4 * qd + 1], o[x][nb][4 * qd + 2], o[x][nb][4 * qd + 3]};
+          *reinterpret_cast<f32x4*>(po + col) =
+              f32x4{o[x][nb][4 * qd], o[x][nb][4 * qd + 1], o[x][nb][4 * qd + 2], o[x][nb][4 * qd + 3]};
         }
       if (half == 0) {
-        float* pm = a.part + rows * a.splits * 2 * a.dv + at * 2;
+        float* pm = a.part + rows * a.splits * 2 * DV + at * 2;
         pm[0] = m[x] == kNegInf ? kNegInf : -nu[x];
         pm[1] = l[x];
       }
@@ -302,7 +302,7 @@ diff_fwd_kernel(const DiffArgs a) {
           for (int j = 0; j < 4; ++j) v[j] = ok ? o[x][nb][4 * qd + j] * f : 0.f;
           slot[64 * qd] = f32x4{v[0], v[1], v[2], v[3]};
           const int col = 32 * nb + 8 * qd + 4 * half;
-          if (a.out2 && in && col < a.dv) store4(a.out2 + out_row(x) * a.dv + col, v);
+          if (a.out2 && in) store4(a.out2 + out_row(x) * DV + col, v);
         }
       }
       __syncthreads();
@@ -314,7 +314,7 @@ diff_fwd_kernel(const DiffArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] = ok ? __builtin_fmaf(-lam, o2[j], o[x][nb][4 * qd + j] * f) : 0.f;
           const int col = 32 * nb + 8 * qd + 4 * half;
-          if (in && col < a.dv) store4(a.out + out_row(x) * a.dv + col, v);
+          if (in) store4(a.out + out_row(x) * DV + col, v);
         }
       }
     }

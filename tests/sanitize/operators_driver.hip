@@ -16,16 +16,27 @@ static hipError_t stub() {
   ++g_launches;
   return hipSuccess;
 }
-DiffFwdShape diff_fwd_shape(int, int, long long rows) { return {rows <= 32 ? 32 : 128, 24}; }
-hipError_t launch_diff_fwd(const DiffArgs&) { return stub(); }
+#define KEY_DIM(D)                                                                             \
+  template <>                                                                                  \
+  DiffFwdShape diff_fwd_shape_of<D>(int, long long rows) { return {rows <= 32 ? 32 : 128, 24}; } \
+  template <>                                                                                  \
+  hipError_t launch_diff_fwd_of<D>(const DiffArgs&) { return stub(); }                         \
+  template <>                                                                                  \
+  int diff_bwd_dq_waves_of<D>(int) { return 2; }                                               \
+  template <>                                                                                  \
+  int diff_bwd_dkv_waves_of<D>(int) { return 1; }                                              \
+  template <>                                                                                  \
+  hipError_t launch_diff_bwd_dq_of<D>(const DiffArgs&) { return stub(); }                      \
+  template <>                                                                                  \
+  hipError_t launch_diff_bwd_dkv_of<D>(const DiffArgs&) { return stub(); }
+KEY_DIM(32)
+KEY_DIM(64)
+KEY_DIM(96)
+KEY_DIM(128)
 hipError_t launch_diff_merge(const DiffArgs&) { return stub(); }
 size_t diff_bwd_stats_floats(int B, int H, int NQ) { return (size_t)B * H * ((NQ + 31LL) / 32) * 128; }
 size_t diff_bwd_dlam_floats(int B, int H, int NQ, int s) { return (size_t)B * H * diff_row_blocks(NQ) * s; }
-int diff_bwd_dq_waves(int, int) { return 2; }
-int diff_bwd_dkv_waves(int, int) { return 1; }
 hipError_t launch_diff_bwd_prep(const DiffArgs&) { return stub(); }
-hipError_t launch_diff_bwd_dq(const DiffArgs&) { return stub(); }
-hipError_t launch_diff_bwd_dkv(const DiffArgs&) { return stub(); }
 hipError_t launch_diff_bwd_join_q(const DiffArgs&) { return stub(); }
 hipError_t launch_diff_bwd_join_k(const DiffArgs&) { return stub(); }
 hipError_t launch_diff_bwd_dlam(const DiffArgs&) { return stub(); }

@@ -10,7 +10,9 @@ import pytest
 from paper_2606_20005_amd import build
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-UNITS = ("norm_rope", "diff_fwd_inst", "diff_bwd_dq_inst", "diff_bwd_dkv_inst", "diff_bwd_wide_inst", "diff_bwd_prep")
+KEY_DIMS, VALUE_DIMS = range(32, 129, 32), range(32, 257, 32)
+UNITS = ("norm_rope", "diff_fwd_merge", "diff_bwd_prep",
+         *(f"diff_{k}_d{d}" for k in ("fwd", "bwd_dq", "bwd_dkv", "bwd_wide") for d in KEY_DIMS))
 SCRATCH, OCCUPANCY = "ScratchSize [bytes/lane]", "Occupancy [waves/SIMD]"
 
 
@@ -39,7 +41,7 @@ def _remarks(unit, outdir):
 @pytest.fixture(scope="module")
 def kernels(tmp_path_factory):
     outdir = str(tmp_path_factory.mktemp("ru"))
-    with cf.ThreadPoolExecutor(max_workers=len(UNITS)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=8) as ex:
         parts = list(ex.map(lambda u: _remarks(u, outdir), UNITS))
     return {k: v for p in parts for k, v in p.items()}
 
@@ -65,7 +67,7 @@ def test_diff_forward(kernels):
             seen.add((d, dv, rb, nw))
             assert r[SCRATCH] == 0, (name, r)
             assert r[OCCUPANCY] >= (2 if nw == 4 else 1), (name, r)
-    assert {s[:2] for s in seen} == {(d, dv) for d in (64, 128) for dv in (64, 128, 192, 256)}
+    assert {s[:2] for s in seen} == {(d, dv) for d in KEY_DIMS for dv in VALUE_DIMS}
 
 
 def test_diff_backward(kernels):
@@ -78,7 +80,8 @@ def test_diff_backward(kernels):
             continue
         kind, d, dv = m.group(1), int(m.group(2)), int(m.group(3))
         seen.add((kind, d, dv))
-        two = (d, dv) == (64, 64) or (kind == "dq" and (d, dv) == (64, 128))
+        two = d + dv <= 128 if kind == "dkv" else d == 32 or (d == 64 and dv <= 128)
+        two = two and (kind, d, dv) != ("dkv", 96, 32)
         assert r[OCCUPANCY] >= (2 if two else 1), (name, r)
         assert r[SCRATCH] <= (96 if (kind, d, dv) == ("dkv", 64, 64) else 0), (name, r)
-    assert len(seen) == 2 * 8
+    assert len(seen) == 2 * len(KEY_DIMS) * len(VALUE_DIMS)
