@@ -39,10 +39,15 @@ auto diff_by_value_dim(int dv, F f) {
   }
 }
 
-// Dims of the key-owned backward kernel that are built without the MFMA
-// results kept in the lower half of the register file (see build.py).
+// Dims of the key-owned backward kernel that are built without MFMA results
+// kept in the lower half of the register file (see build.py): from 160
+// accumulator registers on (dK_1, dK_2: D, dV: DV / 2) they do not stay there
+// beside three logit tiles and their operands, and those moved up and down
+// again for every tile are more than the logits that this form spares.
+// 6007 rows and keys, 8 heads, d 128/128: 653 us kept low, 634 not; 16 heads x 4096,
+// 128/96: 437 and 420; 64/160 (144 registers): 373 and 379.
 template <int D, int DV>
-constexpr bool kDiffWideKeys = D + DV > 256;
+constexpr bool kDiffWideKeys = D + DV / 2 >= 160;
 
 // Forward: rows per workgroup where a key head serves `rows` packed rows, and a wave's MFMAs per tile.
 struct DiffFwdShape {
