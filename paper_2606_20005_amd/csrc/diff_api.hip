@@ -37,7 +37,7 @@ namespace {
 using streamkl::DiffArgs;
 using streamkl::DiffRows;
 
-constexpr long long kMaxInt = 0x7fffffffLL;
+constexpr long long kMaxInt = 0x7fffffffLL, kMaxBlocks = (1LL << 24) - 1;
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -61,7 +61,10 @@ int check_extents(int B, int H, int HK, int N_Q, int N_K, int d, int dv) {
   // rows and 128-row blocks are counted in 31 bits
   if (bh > kMaxInt || (H && (long long)N_Q * (H / HK) > kMaxInt - 256) || (bh && N_Q > (kMaxInt - 256) / bh))
     return STREAMKL_ERR_UNSUPPORTED;
-  if (N_K > kMaxInt - 256 || (HK && B && (N_K + 127LL) / 128 > kMaxInt / ((long long)B * HK))) return STREAMKL_ERR_UNSUPPORTED;
+  if (N_K > kMaxInt - 256) return STREAMKL_ERR_UNSUPPORTED;
+  // and an axis of a grid holds less than 2^32 threads, 256 a tile of 32 rows or a block of 128 keys
+  if (bh * ((N_Q + 31LL) / 32) > kMaxBlocks || (long long)B * HK * ((N_K + 127LL) / 128) > kMaxBlocks)
+    return STREAMKL_ERR_UNSUPPORTED;
   return STREAMKL_OK;
 }
 
@@ -216,7 +219,7 @@ extern "C" int streamkl_diff_fwd(const streamkl_rows* q1, const streamkl_rows* k
                               &a);
   if (st != STREAMKL_OK) return st;
   if (splits < 1) return STREAMKL_ERR_INVALID_ARG;
-  if (splits > streamkl::kDiffMaxSplits) return STREAMKL_ERR_UNSUPPORTED;
+  if (splits > streamkl::kDiffMaxSplits || (splits > 1 && (long long)B * H * N_Q > kMaxBlocks)) return STREAMKL_ERR_UNSUPPORTED;
   if ((long long)B * H * N_Q == 0) return STREAMKL_OK;
   if (splits > 1 && (!workspace || !aligned(workspace, 16) ||
                      workspace_bytes < streamkl_diff_fwd_workspace_bytes(B, H, N_Q, dv, splits)))

@@ -202,9 +202,10 @@ template <typename T, int TPR, int ROT>
 __global__ void __launch_bounds__(kThreads) norm_rope_fwd_kernel(const NrArgs a) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool keys = (int)blockIdx.x >= a.q.blocks;
+  const int block = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+  const bool keys = block >= a.q.blocks;
   const NrSide& s = keys ? a.k : a.q;
-  const int item = ((int)blockIdx.x - (keys ? a.q.blocks : 0)) * kWaves + wave;
+  const int item = (block - (keys ? a.q.blocks : 0)) * kWaves + wave;
   if (item >= s.items) return;
   const int group = item / s.chunks, h0 = (item - group * s.chunks) * s.heads_per_item;
   const int h1 = min(h0 + s.heads_per_item, s.H);
@@ -484,7 +485,9 @@ NrSide make_side(const streamkl_rows* x, bool present, int B, int N, int H, int 
 
 template <typename T, int TPR, int ROT>
 void run_fwd(const NrArgs& a, hipStream_t st) {
-  norm_rope_fwd_kernel<T, TPR, ROT><<<dim3((unsigned)(a.q.blocks + a.k.blocks)), dim3(kThreads), 0, st>>>(a);
+  // an axis of the grid holds less than 2^32 threads
+  const unsigned blocks = (unsigned)(a.q.blocks + a.k.blocks), x = blocks < 1u << 22 ? blocks : 1u << 22;
+  norm_rope_fwd_kernel<T, TPR, ROT><<<dim3(x, (blocks + x - 1) / x), dim3(kThreads), 0, st>>>(a);
 }
 
 template <typename T, typename TG, int TPR, int ROT>

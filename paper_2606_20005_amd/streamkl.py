@@ -488,6 +488,13 @@ def _bf16_out(t, shape, dev, name):
     return t
 
 
+def _workspace(t, dev):
+    """A caller's workspace, checked: its bytes."""
+    if not (isinstance(t, torch.Tensor) and t.device == dev and t.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    return t.numel() * t.element_size()
+
+
 def _prep_error(q, k):
     """What is wrong with the tensors of a norm-and-rotation call."""
     for n, t in (("q", q), ("k", k)):
@@ -600,7 +607,7 @@ def qk_norm_rope_bwd(q, k, dyq, dyk, wq=None, wk=None, table=None, eps=1e-6, q_p
     dw = [None if t is None or not want_w else torch.empty(d, dtype=torch.float32, device=dev) for t in (q, k)]
     ws_bytes = 0
     if workspace is not None:
-        ws_bytes = workspace.numel() * workspace.element_size()
+        ws_bytes = _workspace(workspace, dev)
     elif want_w:
         ws_bytes = lib.streamkl_qk_norm_rope_bwd_workspace_bytes(B, H, HK, NQ, NK, d)
         workspace = torch.empty(max(ws_bytes, 4), dtype=torch.uint8, device=dev)
@@ -766,7 +773,7 @@ def diff_fwd(q1, k1, q2, k2, v, lam, scale=None, causal=False, q_len=None, kv_le
         lse1, lse2 = torch.empty((2, B, H, NQ), dtype=torch.float32, device=dev).unbind(0)
     ws_bytes = 0
     if workspace is not None:
-        ws_bytes = workspace.numel() * workspace.element_size()
+        ws_bytes = _workspace(workspace, dev)
     elif n > 1:
         ws_bytes = lib.streamkl_diff_fwd_workspace_bytes(B, H, NQ, dv, n)
         workspace = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=dev)
@@ -809,7 +816,7 @@ def diff_bwd(q1, k1, q2, k2, v, lam, dout, out, out2, lse1, lse2, scale=None, ca
         ws_bytes = lib.streamkl_diff_bwd_workspace_bytes(*ext, int(bool(causal)))
         workspace = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=dev)
     else:
-        ws_bytes = workspace.numel() * workspace.element_size()
+        ws_bytes = _workspace(workspace, dev)
     with _on(dev):
         st = lib.streamkl_diff_bwd(_rows(q1, "q1"), _rows(k1, "k1"), _rows(q2, "q2"), _rows(k2, "k2"), _rows(v, "v"),
                                    *ext, _diff_scale(scale, d), int(bool(causal)), _p(lam), _p(q_len), _p(kv_len),

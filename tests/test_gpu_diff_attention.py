@@ -386,3 +386,17 @@ def test_refusals(gpu_lib):
         gpu_lib.diff_bwd(*args, do.float(), *saved)
     with pytest.raises(ValueError):
         gpu_lib.diff_bwd(*args, do, *saved, grad_dtype=torch.float16)
+
+
+def test_workspace_refusals(gpu_lib):
+    """A workspace on the host, or one whose elements lie apart, is not what the kernels write to."""
+    args, do = make(2, 4, 2, 6, 600, 64, 64)
+    n = gpu_lib.diff_workspace_bytes(2, 4, 6, 64, 4)
+    m = gpu_lib.diff_bwd_workspace_bytes(2, 4, 2, 6, 600, 64, 64, False)
+    saved = gpu_lib.diff_fwd(*args, save=True)
+    for make_ws in (lambda n: torch.empty(n, dtype=torch.uint8),
+                    lambda n: torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            gpu_lib.diff_fwd(*args, splits=4, workspace=make_ws(n))
+        with pytest.raises(ValueError):
+            gpu_lib.diff_bwd(*args, do, *saved, workspace=make_ws(m))

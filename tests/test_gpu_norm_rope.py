@@ -235,3 +235,29 @@ def test_refusals(gpu_lib):
         gpu_lib.qk_norm_rope(x, None)
     with pytest.raises(ValueError):
         gpu_lib.rope_table(8, 24)
+
+
+def test_more_workgroups_than_one_grid_axis_holds(gpu_lib):
+    """2^30 + 5 tokens of one head: 2^24 + 1 workgroups, and offsets past 32 bits in every unit. All tokens are one row."""
+    n = (1 << 30) + 5
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 64 GiB of outputs")
+    row = torch.randn(1, 1, 1, 32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)).bfloat16()
+    expect, _ = gpu_lib.qk_norm_rope_fwd(row, None)
+    y, _ = gpu_lib.qk_norm_rope_fwd(row.expand(1, n, 1, 32), None)
+    step = 1 << 27
+    for i in range(0, n, step):
+        assert bool((y[0, 0, i:i + step] == expect[0, 0]).all()), i
+    del y
+    torch.cuda.empty_cache()
+
+
+def test_workspace_refusals(gpu_lib):
+    q, k, wq, wk = make(2, 6, 6, 4, 2, 64, 64)
+    y = gpu_lib.qk_norm_rope_fwd(q, k, wq, wk)
+    n = gpu_lib.lib.streamkl_qk_norm_rope_bwd_workspace_bytes(2, 4, 2, 6, 6, 64)
+    for ws in (torch.empty(n, dtype=torch.uint8), torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            gpu_lib.qk_norm_rope_bwd(q, k, *y, wq, wk, workspace=ws)
+    with pytest.raises(gpu_lib.StreamKLError):
+        gpu_lib.qk_norm_rope_bwd(q, k, *y, wq, wk, workspace=torch.empty(n - 1, dtype=torch.uint8, device="cuda"))

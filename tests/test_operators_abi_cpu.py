@@ -129,6 +129,19 @@ def test_diff_refuses_workspaces_and_outputs(sk):
         assert diff_bwd_call(sk, **{n: ODD}) == 1
 
 
+@pytest.mark.parametrize("call", [diff_call, diff_bwd_call])
+@pytest.mark.parametrize("kw", [
+    dict(B=1 << 24, NQ=1), dict(B=1 << 22, NQ=1), dict(B=1 << 13, NQ=1 << 14, NK=0), dict(B=1 << 20, HK=4, NK=513),
+])
+def test_diff_refuses_grids_past_an_axis(sk, call, kw):
+    """2^24 workgroups of 256 threads: more than one axis of a grid holds."""
+    assert call(sk, **kw) == 2
+
+
+def test_diff_refuses_splits_of_very_many_rows(sk):
+    assert diff_call(sk, B=1 << 18, NQ=16, splits=2, ws=FAKE, wsb=1 << 50) == 2
+
+
 def test_diff_empty_extents_launch_nothing(sk):
     none = rows(sk, data=None)
     assert diff_call(sk, B=0, q1=none, k1=none, q2=none, k2=none, v=none, out=None) == 0
