@@ -20,6 +20,8 @@ online_model  the online forward (Sec. 3.2) evaluated from per-tile partial
               is not the oracle; it pins the paper's online derivation
               (eq:kl-final, eq:acc-invariant) to the plain definition so that
               a GPU/oracle mismatch can be attributed.
+operators_oracle  norm and rotation of queries and keys, and differential
+              attention, with their gradients, from the definitions in fp64.
 """
 from .kl_oracle import (  # noqa: F401
     forward,
