@@ -400,3 +400,21 @@ def test_workspace_refusals(gpu_lib):
             gpu_lib.diff_fwd(*args, splits=4, workspace=make_ws(n))
         with pytest.raises(ValueError):
             gpu_lib.diff_bwd(*args, do, *saved, workspace=make_ws(m))
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_a_non_finite_row_stays_alone(gpu_lib, value, splits):
+    """A query row that is not finite spoils its own output and dQ, and no other row's, nor those of other heads."""
+    (q1, k1, q2, k2, v, lam), do = make(1, 4, 2, 70, 200, 64, 96)
+    clean = gpu_lib.diff_fwd(q1, k1, q2, k2, v, lam, splits=splits, save=True)
+    g = gpu_lib.diff_bwd(q1, k1, q2, k2, v, lam, do, *clean, want=("dq1", "dq2"))
+    bad = q1.clone()
+    bad[0, 1, 33, 5] = value
+    dirty = gpu_lib.diff_fwd(bad, k1, q2, k2, v, lam, splits=splits, save=True)
+    h = gpu_lib.diff_bwd(bad, k1, q2, k2, v, lam, do, *dirty, want=("dq1", "dq2"))
+    keep = torch.ones(1, 4, 70, dtype=torch.bool, device="cuda")
+    keep[0, 1, 33] = False
+    assert not torch.isfinite(dirty[0][0, 1, 33]).any()
+    for a, b in ((clean[0], dirty[0]), (clean[1], dirty[1]), (g[0], h[0]), (g[2], h[2])):
+        assert torch.equal(a[keep], b[keep])
