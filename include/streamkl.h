@@ -442,7 +442,7 @@ size_t streamkl_qk_norm_rope_bwd_workspace_bytes(int B, int H, int HK, int N_Q, 
  *             Rows behind q_len give O = 0, LSE = -inf and zero gradients, and take no part in any other.
  *   causal    1: row i sees the keys j <= kv_len[b] - q_len[b] + i (bottom-right alignment). Rows that see no
  *             key give O = 0, LSE = -inf and zero gradients.
- *   B H ceil(N_Q / 32) and B HK ceil(N_K / 128) are below 2^24, as is B H N_Q with splits, else
+ *   B H ceil(N_Q / 32) and B HK ceil(N_K / 64) are below 2^24, as is B H N_Q with splits, else
  *             STREAMKL_ERR_UNSUPPORTED.
  *   splits    1: one pass. 2 to 256: the keys are cut into this many ranges of whole 32-key tiles, streamed by
  *             workgroups of their own and joined by a second kernel: for few rows against many keys.

@@ -62,8 +62,8 @@ int check_extents(int B, int H, int HK, int N_Q, int N_K, int d, int dv) {
   if (bh > kMaxInt || (H && (long long)N_Q * (H / HK) > kMaxInt - 256) || (bh && N_Q > (kMaxInt - 256) / bh))
     return STREAMKL_ERR_UNSUPPORTED;
   if (N_K > kMaxInt - 256) return STREAMKL_ERR_UNSUPPORTED;
-  // and an axis of a grid holds less than 2^32 threads, 256 a tile of 32 rows or a block of 128 keys
-  if (bh * ((N_Q + 31LL) / 32) > kMaxBlocks || (long long)B * HK * ((N_K + 127LL) / 128) > kMaxBlocks)
+  // and an axis of a grid holds less than 2^32 threads, 256 a tile of 32 rows or a block of 64 keys
+  if (bh * ((N_Q + 31LL) / 32) > kMaxBlocks || (long long)B * HK * ((N_K + 63LL) / 64) > kMaxBlocks)
     return STREAMKL_ERR_UNSUPPORTED;
   return STREAMKL_OK;
 }

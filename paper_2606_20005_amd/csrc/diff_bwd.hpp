@@ -21,9 +21,9 @@
 //
 // What bounds it: issue. At d 64/128 a tile of the key-owned kernel takes 32
 // MFMAs (1024 cycles of the matrix pipe) and about 330 instructions, 184 of
-// them vector ones, which one wave issues in 1850 cycles of 3200; timing
-// variants without the loads, the exponentials, the statistics or the
-// transpose reads are 3 to 6% faster each.
+// them vector ones, which one wave issued in 1850 cycles of 3200. So where 32
+// keys a wave leave room for one wave per SIMD, diff_bwd_dkv16_kernel
+// (diff_bwd_keys16.hpp) has 16 and room for two.
 //
 // The logit tile of the first contraction lies in the registers as the A
 // operand of the second (its 16-row k-blocks are a permutation of the 32

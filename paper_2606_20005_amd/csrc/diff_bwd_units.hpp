@@ -1,10 +1,10 @@
 // Instantiations of the differential-attention backward for one key dim (one
 // unit per kernel and dim, so that they compile side by side). The key-owned
-// kernel's widest pairs (kDiffWideKeys) are in units of their own
-// (diff_bwd_wide_units.hpp), built with other flags (see build.py).
+// kernel's widest pairs, one wave of 32 keys per SIMD, are in units of their
+// own (diff_bwd_wide_units.hpp), built with other flags (see build.py).
 #pragma once
 
-#include "diff_bwd.hpp"
+#include "diff_bwd_keys16.hpp"
 #include "diff_launch.hpp"
 
 namespace streamkl {
@@ -43,7 +43,11 @@ hipError_t launch_diff_bwd_dq_of(const DiffArgs& a) {
 template <int D>
 hipError_t launch_diff_bwd_dkv_of(const DiffArgs& a) {
   return diff_by_value_dim(a.dv, [&](auto kv) {
-    if constexpr (kDiffWideKeys<D, kv.value>) {
+    if constexpr (kDiffKeys16<D, kv.value>) {
+      const dim3 grid((unsigned)((long long)a.B * a.HK * ((a.NK + 63LL) / 64)), (unsigned)a.k_splits);
+      hipLaunchKernelGGL((diff_bwd_dkv16_kernel<D, kv.value>), grid, dim3(kThreads), 0, a.stream, a);
+      return hipGetLastError();
+    } else if constexpr (DiffBwdCfg<D, kv.value>::WAVES_K == 1) {
       return launch_diff_bwd_dkv_wide_of<D>(a);
     } else {
       hipLaunchKernelGGL((diff_bwd_dkv_kernel<D, kv.value, 3>), key_grid(a), dim3(kThreads), 0, a.stream, a);

@@ -1,5 +1,13 @@
 // Instantiations of the key-owned kernel of the differential-attention
-// backward for one key dim and the values that kDiffWideKeys names.
+// backward for one key dim and the values that leave room for one wave of 32
+// keys per SIMD and for none of 16 twice: 2 d + dv above 384.
+//
+// Built without MFMA results kept in the lower half of the register file: from
+// 160 accumulator registers on (dK_1, dK_2: d, dV: dv / 2) they do not stay
+// there beside three logit tiles and their operands, and those moved up and
+// down again for every tile are more than the logits that this form spares
+// (measured with this kernel at d 128/128, 8 heads x 6007: 653 us kept low, 634 not;
+// 128/96, 16 heads x 4096: 437 and 420; 64/160, 144 registers: 373 and 379).
 #pragma once
 
 #include "diff_bwd_units.hpp"
@@ -13,7 +21,7 @@ namespace streamkl {
 template <int D>
 hipError_t launch_diff_bwd_dkv_wide_of(const DiffArgs& a) {
   return diff_by_value_dim(a.dv, [&](auto kv) {
-    if constexpr (!kDiffWideKeys<D, kv.value>) {
+    if constexpr (DiffBwdCfg<D, kv.value>::WAVES_K > 1 || kDiffKeys16<D, kv.value>) {
       return hipErrorInvalidValue;
     } else if constexpr (D + kv.value >= 352) {
       hipError_t e = hipSuccess;

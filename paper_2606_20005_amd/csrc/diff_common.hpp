@@ -87,8 +87,22 @@ struct TileRows {
 
 // Staging of a tile of three matrices A, B (DA columns each) and C (DC
 // columns), 32 rows each, by direct-to-LDS loads of NT threads: stage layout
-// [A | B | C], every matrix in the swizzled layout of kl_common.hpp.
-template <int DA, int DC, int NT>
+// [A | B | C], every matrix in the swizzled layout of kl_common.hpp, or in
+// that of swz16 (K16).
+// Swizzle of a tile that is read as 16x16x32 operands: bijective in the 16
+// rows of a row read, whose service groups of 16 lanes are rows 0-3 and 12-15
+// at one chunk with rows 4-11 at the next (chunk c and c ^ 1), and the reverse;
+// and distinct in all but the lowest bit for the eight rows that 32 lanes of a
+// transpose read touch at one pair of chunks. With rows of 8 chunks two rows
+// share the 16 slots. (Bank conflicts counted: none; 29% of the LDS cycles
+// with a swizzle that ignores the service groups.)
+template <int CPR>
+__host__ __device__ constexpr int swz16(int r) {
+  const int low = 2 * (((r >> 2) ^ (r >> 3)) & 1) + ((r >> 3) & 1);
+  return CPR % 16 == 0 ? 4 * (r & 3) + low : 4 * ((r >> 1) & 1) + low;
+}
+
+template <int DA, int DC, int NT, bool K16 = false>
 struct DiffDma {
   static constexpr int CA = lds_cols(DA) / 8, CC = lds_cols(DC) / 8;
   static constexpr int CHUNKS = kDiffTile * (2 * CA + CC);
@@ -110,11 +124,11 @@ struct DiffDma {
       const int p = tid + NT * i, m = matrix(p);
       if (m < 2) {
         const int pp = p - m * kDiffTile * CA;
-        const int r = pp / CA, c = (pp - r * CA) ^ swz<CA>(r);
+        const int r = pp / CA, c = (pp - r * CA) ^ (K16 ? swz16<CA>(r) : swz<CA>(r));
         voff[i] = row_chunk_offset(r, c, DA / 8, m == 0 ? ba : bb);
       } else {
         const int pp = p - 2 * kDiffTile * CA;
-        const int r = pp / CC, c = (pp - r * CC) ^ swz<CC>(r);
+        const int r = pp / CC, c = (pp - r * CC) ^ (K16 ? swz16<CC>(r) : swz<CC>(r));
         voff[i] = row_chunk_offset(r, c, DC / 8, bc);
       }
     }

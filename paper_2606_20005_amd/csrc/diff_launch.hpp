@@ -39,16 +39,6 @@ auto diff_by_value_dim(int dv, F f) {
   }
 }
 
-// Dims of the key-owned backward kernel that are built without MFMA results
-// kept in the lower half of the register file (see build.py): from 160
-// accumulator registers on (dK_1, dK_2: D, dV: DV / 2) they do not stay there
-// beside three logit tiles and their operands, and those moved up and down
-// again for every tile are more than the logits that this form spares.
-// 6007 rows and keys, 8 heads, d 128/128: 653 us kept low, 634 not; 16 heads x 4096,
-// 128/96: 437 and 420; 64/160 (144 registers): 373 and 379.
-template <int D, int DV>
-constexpr bool kDiffWideKeys = D + DV / 2 >= 160;
-
 // Forward: rows per workgroup where a key head serves `rows` packed rows, and a wave's MFMAs per tile.
 struct DiffFwdShape {
   int rows, mfmas;
@@ -60,7 +50,7 @@ template <int D>
 hipError_t launch_diff_fwd_of(const DiffArgs& a);
 hipError_t launch_diff_merge(const DiffArgs& a);
 
-// Backward. Blocks of 128 rows (keys).
+// Backward. Blocks of 128 rows (keys), or pairs of 64 keys.
 constexpr int kDiffMaxGradSplits = 64;
 inline int diff_row_blocks(int n) { return (int)((n + 127LL) / 128); }
 size_t diff_bwd_stats_floats(int B, int H, int NQ);

@@ -418,3 +418,25 @@ def test_a_non_finite_row_stays_alone(gpu_lib, value, splits):
     assert not torch.isfinite(dirty[0][0, 1, 33]).any()
     for a, b in ((clean[0], dirty[0]), (clean[1], dirty[1]), (g[0], h[0]), (g[2], h[2])):
         assert torch.equal(a[keep], b[keep])
+
+
+@pytest.mark.parametrize("d,dv", [(64, 128), (96, 96), (128, 128), (64, 192), (32, 256), (128, 160)])
+@pytest.mark.parametrize("B,H,HK,NQ,NK,ql,kl", [
+    (1, 1, 1, 1, 1, None, None), (1, 2, 1, 1, 63, None, None), (1, 2, 1, 65, 64, None, None), (1, 2, 2, 131, 65, None, None),
+    (2, 4, 2, 70, 150, [70, 33], [129, 17]), (2, 2, 2, 40, 70, [0, 40], [70, 0]), (1, 8, 1, 300, 200, None, [190])])
+@pytest.mark.parametrize("causal", [False, True])
+def test_key_blocks(gpu_lib, d, dv, B, H, HK, NQ, NK, ql, kl, causal):
+    """Extents around the blocks of 16, 64 and 128 keys and the tiles of 32 rows, shared heads, split row ranges."""
+    args, do = make(B, H, HK, NQ, NK, d, dv, seed=d + NK)
+    check(gpu_lib, args, do, causal, ql, kl)
+
+
+@pytest.mark.parametrize("d,dv", [(64, 64), (64, 128), (128, 128), (128, 256)])
+def test_bf16_gradients_of_every_key_form(gpu_lib, d, dv):
+    """The float32 gradients, rounded once; the last key block is ragged."""
+    args, do = make(2, 2, 1, 130, 201, d, dv, seed=d)
+    saved = gpu_lib.diff_fwd(*args, None, True, save=True)
+    a = gpu_lib.diff_bwd(*args, do, *saved, None, True)
+    b = gpu_lib.diff_bwd(*args, do, *saved, None, True, grad_dtype=torch.bfloat16)
+    for n, x, y in zip(NAMES, a, b):
+        assert torch.equal(x if n == "dlam" else x.bfloat16(), y), n

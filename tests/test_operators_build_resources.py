@@ -12,7 +12,7 @@ from paper_2606_20005_amd import build
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 KEY_DIMS, VALUE_DIMS = range(32, 129, 32), range(32, 257, 32)
 UNITS = ("norm_rope", "diff_fwd_merge", "diff_bwd_prep",
-         *(f"diff_{k}_d{d}" for k in ("fwd", "bwd_dq", "bwd_dkv", "bwd_wide") for d in KEY_DIMS))
+         *(f"diff_{k}_d{d}" for k in ("fwd", "bwd_dq", "bwd_dkv") for d in KEY_DIMS), "diff_bwd_wide_d96", "diff_bwd_wide_d128")
 SCRATCH, OCCUPANCY = "ScratchSize [bytes/lane]", "Occupancy [waves/SIMD]"
 
 
@@ -75,13 +75,14 @@ def test_diff_backward(kernels):
     (two waves with a small spill beat one without)."""
     seen = set()
     for name, r in kernels.items():
-        m = re.search(r"diff_bwd_(dq|dkv)_kernelILi(\d+)ELi(\d+)E", name)
+        m = re.search(r"diff_bwd_(dq|dkv|dkv16)_kernelILi(\d+)ELi(\d+)E", name)
         if not m:
             continue
         kind, d, dv = m.group(1), int(m.group(2)), int(m.group(3))
-        seen.add((kind, d, dv))
-        two = d + dv <= 128 if kind == "dkv" else d == 32 or (d == 64 and dv <= 128)
-        two = two and (kind, d, dv) != ("dkv", 96, 32)
+        seen.add((kind[:3], d, dv))
+        small = (d, dv) in ((32, 32), (32, 64), (32, 96), (64, 32), (64, 64))   # 32 keys a wave, two per SIMD
+        two = d == 32 or (d == 64 and dv <= 128) if kind == "dq" else 2 * d + dv <= 384
+        assert kind == "dq" or (kind == "dkv16") == (two and not small), name
         assert r[OCCUPANCY] >= (2 if two else 1), (name, r)
         assert r[SCRATCH] <= (96 if (kind, d, dv) == ("dkv", 64, 64) else 0), (name, r)
     assert len(seen) == 2 * len(KEY_DIMS) * len(VALUE_DIMS)
