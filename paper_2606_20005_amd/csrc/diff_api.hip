@@ -19,6 +19,9 @@ hipError_t launch_diff_fwd(const DiffArgs& a) {
 int diff_bwd_dq_waves(int d, int dv) {
   return diff_by_key_dim(d, [&](auto kd) { return diff_bwd_dq_waves_of<kd.value>(dv); });
 }
+int diff_bwd_dq_rows(int d, int dv) {
+  return diff_by_key_dim(d, [&](auto kd) { return diff_bwd_dq_rows_of<kd.value>(dv); });
+}
 int diff_bwd_dkv_waves(int d, int dv) {
   return diff_by_key_dim(d, [&](auto kd) { return diff_bwd_dkv_waves_of<kd.value>(dv); });
 }
@@ -278,6 +281,8 @@ extern "C" int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k
   const GradSplits g = bwd_splits(B, H, HK, N_Q, N_K, d, dv, causal);
   a.q_splits = g.q;
   a.k_splits = g.k;
+  const int rows_each = streamkl::diff_bwd_dq_rows(d, dv);
+  a.row_blocks = (int)(((long long)N_Q + rows_each - 1) / rows_each);
   if (a.stats) {
     a.dlam_part = a.stats + streamkl::diff_bwd_stats_floats(B, H, N_Q);
     a.grad_part = a.dlam_part + streamkl::diff_bwd_dlam_floats(B, H, N_Q, g.q);

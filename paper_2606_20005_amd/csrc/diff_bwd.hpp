@@ -60,16 +60,17 @@ struct DiffBwdCfg {
   static constexpr int REGS_Q = D + (2 * D + DV) / 4 + 48 + 64;
   static constexpr int REGS_K = (PART & 1 ? D + DV / 4 + 16 : 0) + (PART & 2 ? DV / 2 : 0) + D / 2 + DV / 16 + 28 + 64;
   // 256 registers leave room for two waves per SIMD. The estimate is tight: d 64/192 meets 256 and spills in the
-  // query-owned kernel (190 us with one wave, 226 with two), as does dV alone at 128/192.
+  // query-owned kernel (190 us with one wave, 226 with two), as does dV alone at 128/192. Where WAVES_Q or WAVES_K is 1,
+  // the kernels with 16 rows or keys a wave take over (diff_bwd_rows16.hpp, diff_bwd_keys16.hpp), but for the widest keys.
   static constexpr int WAVES_Q = REGS_Q <= 248 ? 2 : 1, WAVES_K = REGS_K <= 256 - (PART == 2 ? 8 : 0) ? 2 : 1;
-  static constexpr int LA_Q = WAVES_Q == 1 ? 4 : REGS_Q > 232 ? 2 : 3, LA_K = WAVES_K == 1 ? 4 : 2;   // operand reads in flight
+  static constexpr int LA_Q = REGS_Q > 232 ? 2 : 3, LA_K = WAVES_K == 1 ? 4 : 2;   // operand reads in flight
   // Three stages where the workgroups that the registers leave room for have
   // room for them; two tiles a stage in the key-owned kernel with one wave per
   // SIMD, which nothing else occupies while it waits for the others (d 64/128,
   // 32 heads x 4096 causal: 414 -> 394 us together with the next item; no gain
   // in the query-owned kernel).
   static constexpr int ROOM = 158 * 1024;
-  static constexpr int TILE_Q = STAGE * 16 * WAVES_Q, TILE_K = (STAGE + STATS) * 16 * WAVES_K;
+  static constexpr int TILE_Q = STAGE * 16 * 2, TILE_K = (STAGE + STATS) * 16 * WAVES_K;
   static constexpr int TR_K = WAVES_K == 1 && 4 * TILE_K <= ROOM ? 2 : 1;
   static constexpr int STAGES_Q = 3 * TILE_Q <= ROOM ? 3 : 2, STAGES_K = 3 * TR_K * TILE_K <= ROOM ? 3 : 2;
   // dP's accumulators start from -D_1, which saves a subtraction an element;
@@ -82,7 +83,7 @@ struct DiffBwdCfg {
 // dQ: workgroup = 128 query rows of one head, streams tiles [K_1 | K_2 | V].
 // ---------------------------------------------------------------------------
 template <int D, int DV>
-__global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_bwd_dq_kernel(const DiffArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq_kernel(const DiffArgs a) {
   using C = DiffBwdCfg<D, DV>;
   constexpr int KD = D / 16, KV = DV / 16, ND = D / 32;
   __shared__ u32x4 st0[C::STAGE];
@@ -94,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
   const int T = (a.NQ + C::ROWS - 1) / C::ROWS;
   int bh, blk;
   if (a.causal) {
-    causal_block(blockIdx.x, gridDim.x, T, kCus * C::WAVES_Q, bh, blk);
+    causal_block(blockIdx.x, gridDim.x, T, 2 * kCus, bh, blk);
     blk = T - 1 - blk;
   } else {
     const int x = xcd_logical(blockIdx.x, gridDim.x);
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
 #pragma unroll
     for (int i = 0; i < 8; ++i) grad(i);
     diff_pin();
-    if constexpr (C::WAVES_Q == 2) __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = J3; j < J4; ++j) {
       rd(j + LA);
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, (DiffBwdCfg<D, DV>::WAVES_Q)) diff_b
       }
       diff_pin();
     }
-    if constexpr (C::WAVES_Q == 2) __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_s_setprio(0);
   };
 
   stream_tiles<C::STAGES_Q, 1, C::STAGE, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);

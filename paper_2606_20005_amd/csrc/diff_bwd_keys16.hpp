@@ -15,18 +15,12 @@
 // Workgroups of 64 keys, two on a CU, each at its own place in a tile: eight
 // waves that meet at one barrier took 3 to 6% longer at 64/128.
 //
-// Registers: 16x16 results have the row of S^T^T = Q K^T in 4 quad + i and the
-// key in the lane (l % 16, quad = l / 16), two blocks of 16 rows a tile. A
-// lane's eight logits are, as they lie, the A operand of one MFMA over the 32
-// rows, in the order 4 quad + 0..3, 16 + 4 quad + 0..3; transpose reads deliver
-// the other operand in that order.
-//
 // LDS: rows are swizzled by swz16 (diff_common.hpp), not as in the other
 // kernels: here 32 lanes of a transpose read touch eight rows at one pair of
 // chunks, not four rows at two, and 32 lanes of a row read two chunks.
 #pragma once
 
-#include "diff_bwd.hpp"
+#include "diff_bwd_16.hpp"
 
 namespace streamkl {
 
@@ -34,30 +28,14 @@ namespace streamkl {
 template <int D, int DV>
 constexpr bool kDiffKeys16 = DiffBwdCfg<D, DV>::WAVES_K == 1 && 2 * D + DV <= 384;
 
-__device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
-template <int D, int DV>
-struct DiffKeys16Cfg {
-  static constexpr int NW = 4, NT = 64 * NW, ROWS = 16 * NW;
-  static constexpr int CD = lds_cols(D) / 8, CV = lds_cols(DV) / 8;
-  static constexpr int STAGE = DiffDma<D, DV, NT, true>::CHUNKS;
-  static constexpr int STATS = kDiffStatsTile / 4;
-  static constexpr int ROOM = 79 * 1024, TILE = (STAGE + STATS) * 16;
-  // two tiles a stage where they fit twice (d 64/128: 423 us with one, 400 with two, eight waves), else three stages
-  static constexpr int TR = 4 * TILE <= ROOM ? 2 : 1, STAGES = 3 * TR * TILE <= ROOM ? 3 : 2;
-  static constexpr int LA = 3;   // operand reads in flight; four spill at d 96/192 and gain nothing
-};
-
 template <int D, int DV>
 __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dkv16_kernel(const DiffArgs a) {
-  using C = DiffKeys16Cfg<D, DV>;
+  using C = Diff16Cfg<D, DV, kDiffStatsTile / 4>;
   constexpr int KD = D / 32, KV = DV / 32, ND = D / 16, NV = DV / 16;
-  __shared__ u32x4 st0[C::TR * (C::STAGE + C::STATS)];
-  __shared__ u32x4 st1[C::TR * (C::STAGE + C::STATS)];
-  __shared__ u32x4 st2[C::STAGES == 3 ? C::TR * (C::STAGE + C::STATS) : 1];
-  const int tid = threadIdx.x, lane = tid & 63, quad = lane >> 4, col = lane & 15;
+  __shared__ u32x4 st0[C::TR * C::STAGE];
+  __shared__ u32x4 st1[C::TR * C::STAGE];
+  __shared__ u32x4 st2[C::STAGES == 3 ? C::TR * C::STAGE : 1];
+  const int tid = threadIdx.x, lane = tid & 63, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int T = (a.NK + C::ROWS - 1) / C::ROWS, G = a.H / a.HK;
   int bk, blk;
@@ -72,7 +50,7 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dkv16_kernel(const DiffA
   const int qlen = clamp_len(a.q_len, b, a.NQ), klen = clamp_len(a.kv_len, b, a.NK);
   const int off = klen - qlen;
   const float c = a.scale * kLog2e;
-  const int kb0 = blk * C::ROWS, kw = kb0 + 16 * wave, key = kw + col;
+  const int kb0 = blk * C::ROWS, kw = kb0 + 16 * wave, key = kw + (lane & 15);
 
   // row tiles that see a key of the block, for every head of the group
   const int t_all = (qlen + kDiffTile - 1) / kDiffTile;
@@ -90,18 +68,11 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dkv16_kernel(const DiffA
   const int first = !ok ? 0x7fffffff : a.causal ? key - off : 0;   // the first row that sees the lane's key
   bf16x8 k1[KD], k2[KD], vv[KV];
   auto row_of = [&](const DiffRows& x) {
-    const long long at = ok ? (long long)b * x.sb + (long long)hk * x.sh + (long long)key * x.sn : 0;
-    return reinterpret_cast<const u32x4*>(x.p + at);
+    return x.p + (ok ? (long long)b * x.sb + (long long)hk * x.sh + (long long)key * x.sn : 0);
   };
-  auto resident = [&](const DiffRows& x, auto& op) {
-    const u32x4* p = row_of(x);
-#pragma unroll
-    for (int ks = 0; ks < (int)(sizeof(op) / 16); ++ks)
-      op[ks] = __builtin_bit_cast(bf16x8, ok ? p[4 * ks + quad] : u32x4{0u, 0u, 0u, 0u});
-  };
-  resident(a.k1, k1);
-  resident(a.k2, k2);
-  resident(a.v, vv);
+  load_resident16(k1, row_of(a.k1), ok, quad);
+  load_resident16(k2, row_of(a.k2), ok, quad);
+  load_resident16(vv, row_of(a.v), ok, quad);
   wait_vmem();   // before the tile loop: a first use inside it would wait on every trip
 
   f32x4 g1[ND], g2[ND], gv[NV];
@@ -111,22 +82,9 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dkv16_kernel(const DiffA
   for (int n = 0; n < NV; ++n) gv[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const uint32_t bq1 = (uint32_t)a.q1.sn * 2u, bq2 = (uint32_t)a.q2.sn * 2u, bo = (uint32_t)DV * 2u;
-  const DiffDma<D, DV, C::NT, true> dma(tid, bq1, bq2, bo);
-  // places of the lane's operands: chunk of row l % 16 and step ks, byte offset of the transpose read of 16 columns; a
-  // second block of 16 rows lies a constant further
-  int od[KD], ov[KV], td[ND], tv[NV];
-#pragma unroll
-  for (int ks = 0; ks < KD; ++ks) od[ks] = opaque(col * C::CD + ((4 * ks + quad) ^ swz16<C::CD>(col)));
-#pragma unroll
-  for (int ks = 0; ks < KV; ++ks) ov[ks] = opaque(col * C::CV + ((4 * ks + quad) ^ swz16<C::CV>(col)));
-  const int tr_row = 4 * quad + (col >> 2);
-#pragma unroll
-  for (int n = 0; n < ND; ++n)
-    td[n] = opaque((tr_row * C::CD + ((2 * n + ((col >> 1) & 1)) ^ swz16<C::CD>(tr_row))) * 16 + (col & 1) * 8);
-#pragma unroll
-  for (int n = 0; n < NV; ++n)
-    tv[n] = opaque((tr_row * C::CV + ((2 * n + ((col >> 1) & 1)) ^ swz16<C::CV>(tr_row))) * 16 + (col & 1) * 8);
-
+  const typename C::Dma dma(tid, bq1, bq2, bo);
+  const Places16<D> pd(lane);
+  const Places16<DV> pv(lane);
   const int ntq = (a.NQ + kDiffTile - 1) / kDiffTile;
   // step u: head hk G + u / per, row tile t_first + u % per. The loads run
   // ahead, so each side keeps its own place.
@@ -151,7 +109,7 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dkv16_kernel(const DiffA
     // every wave loads a quarter of the statistics: one instruction each, half of its lanes
     const rsrc_t rs = make_rsrc(ps, kDiffStatsTile * 4u);
     if (lane < 32)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(reinterpret_cast<float*>(stage + C::STAGE) + 32 * wave),
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(reinterpret_cast<float*>(stage + C::Dma::CHUNKS) + 32 * wave),
                                                4, 4u * lane + 128u * wave, 0, 0, 0);
 #endif
     ps += kDiffStatsTile;
@@ -168,19 +126,13 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dkv16_kernel(const DiffA
     constexpr int B2 = kDiffTile * C::CD, B3 = 2 * B2;   // chunks before Q_2 and dO
     bf16x8 buf[J5];   // streamed operands, read LA of them ahead of their MFMAs
     auto rd = [&](int j) {
-      if (j < J2)
-        buf[j] = __builtin_bit_cast(bf16x8, stage[od[j % J1 / 2] + j / J1 * B2 + (j & 1) * 16 * C::CD]);
-      else if (j < J3)
-        buf[j] = __builtin_bit_cast(bf16x8, stage[ov[(j - J2) / 2] + B3 + (j & 1) * 16 * C::CV]);
-      else if (j < J4)
-        buf[j] = cat8(lds_tr4_at(stage, tv[j - J3] + 16 * B3), lds_tr4_at(stage, tv[j - J3] + 16 * B3 + 256 * C::CV));
-      else if (j < J5) {
-        const int m = (j - J4) / ND * 16 * B2, n = (j - J4) % ND;
-        buf[j] = cat8(lds_tr4_at(stage, td[n] + m), lds_tr4_at(stage, td[n] + m + 256 * C::CD));
-      }
+      if (j < J2) buf[j] = pd.rows(stage, j / J1 * B2, j % J1 / 2, j & 1);
+      else if (j < J3) buf[j] = pv.rows(stage, B3, (j - J2) / 2, j & 1);
+      else if (j < J4) buf[j] = pv.cols(stage, B3, j - J3);
+      else if (j < J5) buf[j] = pd.cols(stage, (j - J4) / ND * B2, (j - J4) % ND);
     };
     // statistics of the lane's rows: block x of kind w at st[8 w + 4 x]
-    const f32x4* st = reinterpret_cast<const f32x4*>(stage + C::STAGE) + quad;
+    const f32x4* st = reinterpret_cast<const f32x4*>(stage + C::Dma::CHUNKS) + quad;
     f32x4 s1[2], s2[2], dp[2], ga[2], gb[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) s1[x] = s2[x] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -272,8 +224,7 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dkv16_kernel(const DiffA
     }
   };
 
-  stream_tiles<C::STAGES, C::TR, C::STAGE + C::STATS, DiffDma<D, DV, C::NT, true>::NCH + 1>(st0, st1, st2, s_begin, s_end,
-                                                                                            load, tile);
+  stream_tiles<C::STAGES, C::TR, C::STAGE, C::Dma::NCH + 1>(st0, st1, st2, s_begin, s_end, load, tile);
 
   const size_t rows = (size_t)bk * a.NK;
   void *o1 = a.dk1, *o2 = a.dk2, *o3 = a.dv_out;
@@ -286,40 +237,9 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dkv16_kernel(const DiffA
     if (o2) o2 = part + keys * D;
     if (o3) o3 = part + keys * 2 * D;
   }
-  // see write_grad in kl_bwd.hpp: adjacent lanes trade values, so that each stores a dword of bf16
-  auto write = [&](void* out, auto& acc, float s) {
-    constexpr int NB = sizeof(acc) / sizeof(f32x4);
-    if (as_bf16) {
-      const bool odd = (lane & 1) != 0;
-#pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        const int row = kw + 4 * quad + i + (lane & 1);
-        uint32_t* o = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(out) + (rows + row) * (16 * NB) + (lane & 14));
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const float v0 = acc[n][i] * s, v1 = acc[n][i + 1] * s;
-          const float got = __int_as_float(
-              __builtin_amdgcn_update_dpp(0, __float_as_int(odd ? v0 : v1), 0xB1, 0xF, 0xF, true));
-          const uint16_t lo = __builtin_bit_cast(uint16_t, (__bf16)(odd ? got : v0));
-          const uint16_t hi = __builtin_bit_cast(uint16_t, (__bf16)(odd ? v1 : got));
-          if (row < a.NK) o[8 * n] = (uint32_t)lo | ((uint32_t)hi << 16);
-        }
-      }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = kw + 4 * quad + i;
-      if (row < a.NK) {
-        float* o = static_cast<float*>(out) + (rows + row) * (16 * NB) + col;
-#pragma unroll
-        for (int n = 0; n < NB; ++n) o[16 * n] = acc[n][i] * s;
-      }
-    }
-  };
-  if (o1) write(o1, g1, a.scale);
-  if (o2) write(o2, g2, a.scale);
-  if (o3) write(o3, gv, 1.f);
+  if (o1) write_grad16(o1, as_bf16, g1, rows, kw, a.NK, a.scale, lane);
+  if (o2) write_grad16(o2, as_bf16, g2, rows, kw, a.NK, a.scale, lane);
+  if (o3) write_grad16(o3, as_bf16, gv, rows, kw, a.NK, 1.f, lane);
 }
 
 }  // namespace streamkl

@@ -112,11 +112,11 @@ hipError_t join(const float* part, long long each, int n, void* out, long long c
 }  // namespace
 
 size_t diff_bwd_stats_floats(int B, int H, int NQ) {
-  return (size_t)B * H * ((NQ + kDiffTile - 1) / kDiffTile) * kDiffStatsTile;
+  return (size_t)B * H * ((NQ + kDiffTile - 1LL) / kDiffTile) * kDiffStatsTile;
 }
 
 size_t diff_bwd_dlam_floats(int B, int H, int NQ, int q_splits) {
-  return ((size_t)B * H * diff_row_blocks(NQ) * q_splits + 3) / 4 * 4;
+  return ((size_t)B * H * 2 * diff_row_blocks(NQ) * q_splits + 3) / 4 * 4;   // blocks of 64 rows
 }
 
 hipError_t launch_diff_bwd_prep(const DiffArgs& a) {
@@ -130,7 +130,7 @@ hipError_t launch_diff_bwd_prep(const DiffArgs& a) {
 
 hipError_t launch_diff_bwd_dlam(const DiffArgs& a) {
   hipLaunchKernelGGL(diff_bwd_dlam_kernel, dim3((unsigned)a.H), dim3(kThreads), 0, a.stream, a,
-                     diff_row_blocks(a.NQ) * a.q_splits);
+                     a.row_blocks * a.q_splits);
   return hipGetLastError();
 }
 

@@ -5,6 +5,7 @@
 #pragma once
 
 #include "diff_bwd_keys16.hpp"
+#include "diff_bwd_rows16.hpp"
 #include "diff_launch.hpp"
 
 namespace streamkl {
@@ -26,6 +27,11 @@ int diff_bwd_dq_waves_of(int dv) {
 }
 
 template <int D>
+int diff_bwd_dq_rows_of(int dv) {
+  return diff_by_value_dim(dv, [](auto kv) { return kDiffRows16<D, kv.value> ? 64 : 128; });
+}
+
+template <int D>
 int diff_bwd_dkv_waves_of(int dv) {
   return diff_by_value_dim(dv, [](auto kv) { return DiffBwdCfg<D, kv.value>::WAVES_K; });
 }
@@ -33,9 +39,11 @@ int diff_bwd_dkv_waves_of(int dv) {
 template <int D>
 hipError_t launch_diff_bwd_dq_of(const DiffArgs& a) {
   return diff_by_value_dim(a.dv, [&](auto kv) {
-    hipLaunchKernelGGL((diff_bwd_dq_kernel<D, kv.value>),
-                       dim3((unsigned)((long long)a.B * a.H * diff_row_blocks(a.NQ)), (unsigned)a.q_splits),
-                       dim3(kThreads), 0, a.stream, a);
+    const dim3 grid((unsigned)((long long)a.B * a.H * a.row_blocks), (unsigned)a.q_splits);
+    if constexpr (kDiffRows16<D, kv.value>)
+      hipLaunchKernelGGL((diff_bwd_dq16_kernel<D, kv.value>), grid, dim3(kThreads), 0, a.stream, a);
+    else
+      hipLaunchKernelGGL((diff_bwd_dq_kernel<D, kv.value>), grid, dim3(kThreads), 0, a.stream, a);
     return hipGetLastError();
   });
 }

@@ -44,6 +44,7 @@ struct DiffArgs {
   float* stats;              // prepared row statistics, see diff_bwd.hpp
   float* dlam_part;          // partial sums of dlam
   int q_splits, k_splits;    // ranges of the streamed axis in the query- and the key-owned kernel
+  int row_blocks;            // of the query-owned kernel
   float* grad_part;          // their partial gradients where there is more than one
   void *dq1, *dk1, *dq2, *dk2, *dv_out;
   float* dlam;

@@ -50,7 +50,7 @@ template <int D>
 hipError_t launch_diff_fwd_of(const DiffArgs& a);
 hipError_t launch_diff_merge(const DiffArgs& a);
 
-// Backward. Blocks of 128 rows (keys), or pairs of 64 keys.
+// Backward. Blocks of 128 rows (keys), or twice as many of 64.
 constexpr int kDiffMaxGradSplits = 64;
 inline int diff_row_blocks(int n) { return (int)((n + 127LL) / 128); }
 size_t diff_bwd_stats_floats(int B, int H, int NQ);
@@ -58,6 +58,8 @@ size_t diff_bwd_dlam_floats(int B, int H, int NQ, int q_splits);
 // Defined in diff_bwd_units.hpp, instantiated for one key dim per unit; waves: per SIMD.
 template <int D>
 int diff_bwd_dq_waves_of(int dv);
+template <int D>
+int diff_bwd_dq_rows_of(int dv);   // rows of a workgroup
 template <int D>
 int diff_bwd_dkv_waves_of(int dv);
 template <int D>

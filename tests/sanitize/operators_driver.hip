@@ -24,6 +24,8 @@ static hipError_t stub() {
   template <>                                                                                  \
   int diff_bwd_dq_waves_of<D>(int) { return 2; }                                               \
   template <>                                                                                  \
+  int diff_bwd_dq_rows_of<D>(int) { return 64; }                                               \
+  template <>                                                                                  \
   int diff_bwd_dkv_waves_of<D>(int) { return 1; }                                              \
   template <>                                                                                  \
   hipError_t launch_diff_bwd_dq_of<D>(const DiffArgs&) { return stub(); }                      \

@@ -75,14 +75,16 @@ def test_diff_backward(kernels):
     (two waves with a small spill beat one without)."""
     seen = set()
     for name, r in kernels.items():
-        m = re.search(r"diff_bwd_(dq|dkv|dkv16)_kernelILi(\d+)ELi(\d+)E", name)
+        m = re.search(r"diff_bwd_(dq|dq16|dkv|dkv16)_kernelILi(\d+)ELi(\d+)E", name)
         if not m:
             continue
         kind, d, dv = m.group(1), int(m.group(2)), int(m.group(3))
-        seen.add((kind[:3], d, dv))
-        small = (d, dv) in ((32, 32), (32, 64), (32, 96), (64, 32), (64, 64))   # 32 keys a wave, two per SIMD
-        two = d == 32 or (d == 64 and dv <= 128) if kind == "dq" else 2 * d + dv <= 384
-        assert kind == "dq" or (kind == "dkv16") == (two and not small), name
-        assert r[OCCUPANCY] >= (2 if two else 1), (name, r)
+        seen.add((kind.replace("16", ""), d, dv))
+        if kind.startswith("dq"):   # 16 rows a wave where 32 leave room for one wave per SIMD
+            assert (kind == "dq16") == (d > 64 or (d == 64 and dv > 160)), name
+        else:
+            small = (d, dv) in ((32, 32), (32, 64), (32, 96), (64, 32), (64, 64))   # 32 keys a wave, two per SIMD
+            assert (kind == "dkv16") == (2 * d + dv <= 384 and not small), name
+        assert r[OCCUPANCY] >= (1 if kind == "dkv" and 2 * d + dv > 384 else 2), (name, r)
         assert r[SCRATCH] <= (96 if (kind, d, dv) == ("dkv", 64, 64) else 0), (name, r)
     assert len(seen) == 2 * len(KEY_DIMS) * len(VALUE_DIMS)
