@@ -4,6 +4,8 @@
 // dQ with 32 and 16 rows a wave, us: 4 x 12 heads x 1021 ragged, d 96/160, 62 and 54;
 // 16 heads x 4096 causal, 64/192, 159 and 149, 128/192, 209 and 202; 8 heads x 6007, 128/128,
 // 399 and 388; 16 heads x 4096, 96/96, 284 and 276, 128/256, 404 and 396.
+// Where 32 rows leave room for two waves, they are ahead: 64/128, 249 and 262 (250 with three
+// waves of 16 rows), 64/64, 193 and 215.
 #pragma once
 
 #include "diff_bwd_16.hpp"

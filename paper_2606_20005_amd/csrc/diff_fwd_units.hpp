@@ -24,7 +24,7 @@ struct FwdPick {
 
 // A pair of waves takes two 32-row blocks where its registers then leave room
 // for two waves per SIMD, one where they do not (d 128/128, 8 heads x 6007,
-// same box: 351 us with one block and two waves per SIMD, 423 with two blocks
+// same card: 351 us with one block and two waves per SIMD, 423 with two blocks
 // and one). Few rows run in one pair of waves (a whole workgroup would be
 // mostly padding, and short ones leave more of them resident).
 template <int D, typename F>
