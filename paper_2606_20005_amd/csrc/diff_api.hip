@@ -284,8 +284,9 @@ extern "C" int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k
   const int rows_each = streamkl::diff_bwd_dq_rows(d, dv);
   a.row_blocks = (int)(((long long)N_Q + rows_each - 1) / rows_each);
   if (a.stats) {
-    a.dlam_part = a.stats + streamkl::diff_bwd_stats_floats(B, H, N_Q);
-    a.grad_part = a.dlam_part + streamkl::diff_bwd_dlam_floats(B, H, N_Q, g.q);
+    float* part = a.stats + streamkl::diff_bwd_stats_floats(B, H, N_Q);   // whole tiles of statistics: 16-byte aligned
+    a.dlam_part = reinterpret_cast<double*>(part);
+    a.grad_part = part + streamkl::diff_bwd_dlam_floats(B, H, N_Q, g.q);
   }
   a.dq1 = dq1;
   a.dk1 = dk1;

@@ -31,8 +31,26 @@
 //
 // Rounding: the logit gradients and P_1 - lam P_2 to bf16 as operands of the
 // second contraction (each term is off by at most 2^-8 of itself), gradients
-// once when they are written. D_t is formed from the bf16 outputs O and O_2;
-// dlam is not: P_2 dP is summed in float32 from the recomputed values.
+// once when they are written. D_t is formed from the bf16 outputs O and O_2.
+//
+// dlam can cancel to far below its terms P_2 dP, so it is held to what float32
+// gives each of them:
+// - sum_j P_2 dP = D_2 + sum_j P_2 (dP - D_2), as P_2 sums to 1: an error common
+//   to the P_2 of a row (of its log-sum-exp) meets only what D_2 is off by. D_2
+//   (from bf16 outputs) is rounded to 12 bits, so that dP - D_2 is exact: its
+//   rounding would be the same for many keys of a row.
+// - P_2 is formed times 2^n, n = log2 of the keys rounded down, which leaves its
+//   exponent near 0 instead of near -n, where float32 has fewer bits for it.
+// - Odd rows run with -dO, -D_1 and -D_2, and their results change sign at the
+//   end: the matrix unit's sums fall short by about 2^-33 of their size,
+//   whatever their sign (with -dO for dO throughout, dlam + dlam' was 2.0e-5 for
+//   each of 8 heads x 6007, d 128/128), which adds up over rows of one sign.
+// - The 16 (or 8) terms of a tile are added in float32, tiles, rows and blocks in
+//   64 bits.
+// Error relative to the root of the sum of the squared terms: 256 x 256, d 64/64,
+// 1.5e-7; 64 rows x 8192 keys, 64/64, 1.2e-7; 6007 x 6007, 128/128, 2.3e-7. With
+// P_2 dP in one float32 chain over a row's keys 3.9e-7, 7.3e-7 and 1.1e-6, in
+// plain float32 1.9e-7, 1.9e-7 and 4.5e-7.
 //
 // Prepared statistics (diff_bwd_prep_kernel): for every head and 32-row tile
 // 4 x 32 floats,
@@ -49,6 +67,56 @@
 namespace streamkl {
 
 constexpr int kDiffStatsTile = 4 * kDiffTile;   // floats per tile
+
+// *p += v in LDS, where only this lane touches *p. Written out, since the
+// compiler waits for every load into LDS in flight before a write to it that it
+// knows of. Nothing comes back; LDS operations of a wave take effect in order.
+__device__ __forceinline__ void lds_add_f64(double* p, double v) {
+  typedef __attribute__((address_space(3))) double lds_f64;
+  asm volatile("ds_add_f64 %0, %1" ::"v"((uint32_t)(uintptr_t)(lds_f64*)p), "v"(v) : "memory");
+}
+
+// x rounded to its leading 12 bits.
+__device__ __forceinline__ float leading_bits(float x) {
+  return __uint_as_float((__float_as_uint(x) + 0x800u) & 0xfffff000u);
+}
+
+// The rows of odd lanes with the other sign.
+template <int K>
+__device__ __forceinline__ void negate_odd_rows(bf16x8 (&op)[K], float& d1, float& d2, int lane) {
+  const uint32_t sign = (lane & 1) ? 0x80008000u : 0u;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    u32x4 t = __builtin_bit_cast(u32x4, op[k]);
+    t ^= sign;
+    op[k] = __builtin_bit_cast(bf16x8, t);
+  }
+  d1 = (lane & 1) ? -d1 : d1;
+  d2 = (lane & 1) ? -d2 : d2;
+}
+
+// The query gradients of a wave (element i of an accumulator is in a row of i's
+// parity) as they are: signs of odd rows, 2^lift of map 2.
+template <typename Acc, int N>
+__device__ __forceinline__ void restore_rows(Acc (&g1)[N], Acc (&g2)[N], int lift) {
+  const float f = __builtin_ldexpf(1.f, -lift);
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Acc) / sizeof(float)); ++i) {
+      g1[n][i] = (i & 1) ? -g1[n][i] : g1[n][i];
+      g2[n][i] *= (i & 1) ? -f : f;
+    }
+}
+
+// The sum over a workgroup of its lanes' parts of sum_j P_2 dP, to part[0].
+__device__ __forceinline__ void write_dlam_part(double* part, double* red, double dl, int tid) {
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) dl += __shfl_xor(dl, x);
+  if ((tid & 63) == 0) red[tid >> 6] = dl;
+  __syncthreads();
+  if (tid == 0) part[0] = (red[0] + red[1]) + (red[2] + red[3]);
+}
 
 template <int D, int DV, int PART = 3>
 struct DiffBwdCfg {
@@ -89,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq_kernel(const DiffArgs
   __shared__ u32x4 st0[C::STAGE];
   __shared__ u32x4 st1[C::STAGE];
   __shared__ u32x4 st2[C::STAGES_Q == 3 ? C::STAGE : 1];
-  __shared__ float red[C::NW];
+  __shared__ double red[C::NW];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int T = (a.NQ + C::ROWS - 1) / C::ROWS;
@@ -128,15 +196,17 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq_kernel(const DiffArgs
   load_row_operand<DV>(go, a.dout + (ok ? ri * DV : 0), ok, half);
   const int ntq = (a.NQ + kDiffTile - 1) / kDiffTile;
   const float lam = a.lam[h];
+  const int lift = klen > 1 ? 31 - __builtin_clz(klen) : 0;   // P_2 is formed times 2^lift
   float ls1 = __builtin_inff(), ls2 = ls1, d1 = 0.f, d2 = 0.f;
   if (ok) {
     const float* st = a.stats + ((long long)bh * ntq + row / kDiffTile) * kDiffStatsTile + row % kDiffTile;
     d1 = -st[2 * kDiffTile];
-    d2 = d1 + (lam < 0.f ? -st[3 * kDiffTile] : st[3 * kDiffTile]);
+    d2 = leading_bits(d1 + (lam < 0.f ? -st[3 * kDiffTile] : st[3 * kDiffTile]));
     const float e1 = a.lse1[ri], e2 = a.lse2[ri];
     ls1 = e1 == kNegInf ? __builtin_inff() : e1 * kLog2e;
-    ls2 = e2 == kNegInf ? __builtin_inff() : e2 * kLog2e;
+    ls2 = e2 == kNegInf ? __builtin_inff() : e2 * kLog2e - (float)lift;
   }
+  negate_odd_rows(go, d1, d2, lane);
   wait_vmem();   // before the tile loop: a first use inside it would wait on every trip
 
   f32x16 g1[D / 32], g2[D / 32];
@@ -145,7 +215,9 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq_kernel(const DiffArgs
     g1[n] = zero16();
     g2[n] = zero16();
   }
-  float dl = 0.f;   // sum of P_2 dP
+  // 2^lift times the sum of P_2 (dP - D_2) of every lane, in LDS: the two registers spill at d 64/128
+  __shared__ double dl[C::NT];
+  dl[tid] = 0.;
 
   const uint32_t bk1 = (uint32_t)a.k1.sn * 2u, bk2 = (uint32_t)a.k2.sn * 2u, bv = (uint32_t)a.v.sn * 2u;
   const uint16_t* k1 = a.k1.p + (long long)b * a.k1.sb + (long long)hk * a.k1.sh;
@@ -213,10 +285,11 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq_kernel(const DiffArgs
       diff_pin();
     }
     bf16x8 a1[2], a2[2];
+    float dt = 0.f;
     auto grad = [&](int i) {
       e1[i] *= dp[i] - d1;
-      dl = __builtin_fmaf(e2[i], dp[i], dl);
       e2[i] *= dp[i] - d2;
+      dt += e2[i];
       if (i % 8 == 7) {
         a1[i / 8] = pack8(e1 + i - 7);
         a2[i / 8] = pack8(e2 + i - 7);
@@ -239,10 +312,12 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq_kernel(const DiffArgs
       diff_pin();
     }
     __builtin_amdgcn_s_setprio(0);
+    lds_add_f64(&dl[tid], (double)dt);
   };
 
   stream_tiles<C::STAGES_Q, 1, C::STAGE, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
 
+  restore_rows(g1, g2, lift);
   const size_t rows = (size_t)bh * a.NQ;
   void *o1 = a.dq1, *o2 = a.dq2;
   bool as_bf16 = a.bf16_grads != 0;
@@ -255,12 +330,9 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq_kernel(const DiffArgs
   if (o1) write_grad<D>(o1, as_bf16, g1, rows, rw, a.NQ, a.scale, lane);
   if (o2) write_grad<D>(o2, as_bf16, g2, rows, rw, a.NQ, -a.scale * lam, lane);
   if (a.dlam) {
-    if (!ok) dl = 0.f;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) dl += __shfl_xor(dl, x);
-    if (lane == 0) red[wave] = dl;
-    __syncthreads();
-    if (tid == 0) a.dlam_part[((long long)bh * T + blk) * a.q_splits + blockIdx.y] = (red[0] + red[1]) + (red[2] + red[3]);
+    const double part = __builtin_ldexp(dl[tid], -lift) + (half == 0 && blockIdx.y == 0 ? (double)d2 : 0.);   // D_2 once a row
+    write_dlam_part(a.dlam_part + ((long long)bh * T + blk) * a.q_splits + blockIdx.y, red,
+                    !ok ? 0. : (lane & 1) ? -part : part, tid);
   }
 }
 

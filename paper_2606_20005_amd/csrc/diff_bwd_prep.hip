@@ -59,9 +59,9 @@ __global__ void __launch_bounds__(kThreads) diff_bwd_prep_kernel(const DiffArgs 
 
 // dlam_h = -sum of its blocks' partial sums, one workgroup per head.
 __global__ void __launch_bounds__(kThreads) diff_bwd_dlam_kernel(const DiffArgs a, int T) {
-  __shared__ float red[kThreads / 64];
+  __shared__ double red[kThreads / 64];
   const int h = blockIdx.x, tid = threadIdx.x;
-  float s = 0.f;
+  double s = 0.;
   for (int i = tid; i < a.B * T; i += kThreads) {
     const int b = i / T;
     s += a.dlam_part[((long long)b * a.H + h) * T + (i - b * T)];
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kThreads) diff_bwd_dlam_kernel(const DiffArgs 
   for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m);
   if ((tid & 63) == 0) red[tid >> 6] = s;
   __syncthreads();
-  if (tid == 0) a.dlam[h] = -((red[0] + red[1]) + (red[2] + red[3]));
+  if (tid == 0) a.dlam[h] = (float)-((red[0] + red[1]) + (red[2] + red[3]));
 }
 
 // Sum of n partial arrays in their order, `each` floats apart: `count` values
@@ -116,7 +116,7 @@ size_t diff_bwd_stats_floats(int B, int H, int NQ) {
 }
 
 size_t diff_bwd_dlam_floats(int B, int H, int NQ, int q_splits) {
-  return ((size_t)B * H * 2 * diff_row_blocks(NQ) * q_splits + 3) / 4 * 4;   // blocks of 64 rows
+  return ((size_t)B * H * 2 * diff_row_blocks(NQ) * q_splits + 1) / 2 * 4;   // a double each, blocks of 64 rows
 }
 
 hipError_t launch_diff_bwd_prep(const DiffArgs& a) {

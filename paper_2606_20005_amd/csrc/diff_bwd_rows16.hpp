@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq16_kernel(const DiffAr
   __shared__ u32x4 st0[C::TR * C::STAGE];
   __shared__ u32x4 st1[C::TR * C::STAGE];
   __shared__ u32x4 st2[C::STAGES == 3 ? C::TR * C::STAGE : 1];
-  __shared__ float red[kThreads / 64];
+  __shared__ double red[kThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int T = (a.NQ + C::ROWS - 1) / C::ROWS;
@@ -61,21 +61,23 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq16_kernel(const DiffAr
   load_resident16(go, a.dout + (ok ? ri * DV : 0), ok, quad);
   const int ntq = (a.NQ + kDiffTile - 1) / kDiffTile;
   const float lam = a.lam[h];
+  const int lift = klen > 1 ? 31 - __builtin_clz(klen) : 0;   // P_2 is formed times 2^lift
   float ls1 = __builtin_inff(), ls2 = ls1, d1 = 0.f, d2 = 0.f;
   if (ok) {
     const float* st = a.stats + ((long long)bh * ntq + row / kDiffTile) * kDiffStatsTile + row % kDiffTile;
     d1 = -st[2 * kDiffTile];
-    d2 = d1 + (lam < 0.f ? -st[3 * kDiffTile] : st[3 * kDiffTile]);
+    d2 = leading_bits(d1 + (lam < 0.f ? -st[3 * kDiffTile] : st[3 * kDiffTile]));
     const float e1 = a.lse1[ri], e2 = a.lse2[ri];
     ls1 = e1 == kNegInf ? __builtin_inff() : e1 * kLog2e;
-    ls2 = e2 == kNegInf ? __builtin_inff() : e2 * kLog2e;
+    ls2 = e2 == kNegInf ? __builtin_inff() : e2 * kLog2e - (float)lift;
   }
+  negate_odd_rows(go, d1, d2, lane);
   wait_vmem();   // before the tile loop: a first use inside it would wait on every trip
 
   f32x4 g1[ND], g2[ND];
 #pragma unroll
   for (int n = 0; n < ND; ++n) g1[n] = g2[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float dl = 0.f;   // sum of P_2 dP
+  double dl = 0.;   // 2^lift times the sum of P_2 (dP - D_2)
 
   const uint32_t bk1 = (uint32_t)a.k1.sn * 2u, bk2 = (uint32_t)a.k2.sn * 2u, bv = (uint32_t)a.v.sn * 2u;
   const uint16_t* k1 = a.k1.p + (long long)b * a.k1.sb + (long long)hk * a.k1.sh;
@@ -150,6 +152,7 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq16_kernel(const DiffAr
     for (int i = 0; i < 8; ++i) e1[i] *= dp[i >> 2][i & 3] - d1;
     const bf16x8 a1 = pack8(e1);
     diff_pin();
+    float dt = 0.f;
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = J3; j < J3 + ND; ++j) {
@@ -157,9 +160,8 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq16_kernel(const DiffAr
       g1[j - J3] = mfma16(a1, buf[j], g1[j - J3]);
 #pragma unroll
       for (int i = 8 * (j - J3) / ND; i < 8 * (j - J3 + 1) / ND; ++i) {
-        const float y = dp[i >> 2][i & 3];
-        dl = __builtin_fmaf(e2[i], y, dl);
-        e2[i] *= y - d2;
+        e2[i] *= dp[i >> 2][i & 3] - d2;
+        dt += e2[i];
       }
       diff_pin();
     }
@@ -172,10 +174,12 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq16_kernel(const DiffAr
       diff_pin();
     }
     __builtin_amdgcn_s_setprio(0);
+    dl += (double)dt;
   };
 
   stream_tiles<C::STAGES, C::TR, C::STAGE, C::Dma::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
 
+  restore_rows(g1, g2, lift);
   const size_t rows = (size_t)bh * a.NQ;
   void *o1 = a.dq1, *o2 = a.dq2;
   bool as_bf16 = a.bf16_grads != 0;
@@ -188,12 +192,9 @@ __global__ void __launch_bounds__(kThreads, 2) diff_bwd_dq16_kernel(const DiffAr
   if (o1) write_grad16(o1, as_bf16, g1, rows, rw, a.NQ, a.scale, lane);
   if (o2) write_grad16(o2, as_bf16, g2, rows, rw, a.NQ, -a.scale * lam, lane);
   if (a.dlam) {
-    if (!ok) dl = 0.f;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) dl += __shfl_xor(dl, x);
-    if (lane == 0) red[wave] = dl;
-    __syncthreads();
-    if (tid == 0) a.dlam_part[((long long)bh * T + blk) * a.q_splits + blockIdx.y] = (red[0] + red[1]) + (red[2] + red[3]);
+    dl = __builtin_ldexp(dl, -lift) + (quad == 0 && blockIdx.y == 0 ? (double)d2 : 0.);   // D_2 once a row
+    write_dlam_part(a.dlam_part + ((long long)bh * T + blk) * a.q_splits + blockIdx.y, red,
+                    !ok ? 0. : (lane & 1) ? -dl : dl, tid);
   }
 }
 

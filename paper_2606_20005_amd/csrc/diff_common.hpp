@@ -42,7 +42,7 @@ struct DiffArgs {
   // backward
   const uint16_t* dout;      // [B, H, NQ, dv]
   float* stats;              // prepared row statistics, see diff_bwd.hpp
-  float* dlam_part;          // partial sums of dlam
+  double* dlam_part;         // partial sums of dlam
   int q_splits, k_splits;    // ranges of the streamed axis in the query- and the key-owned kernel
   int row_blocks;            // of the query-owned kernel
   float* grad_part;          // their partial gradients where there is more than one

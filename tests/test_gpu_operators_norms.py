@@ -1,0 +1,67 @@
+"""Differential attention on the GPU against the plain fp64 form, in norm: roundings of many elements that are independent
+of each other average, which elementwise bounds (sums of worst cases) cannot see."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as oo
+
+pytestmark = pytest.mark.gpu
+
+NAMES = ("dq1", "dk1", "dq2", "dk2", "dv", "dlam")
+
+
+def n64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def make(B, H, HK, NQ, NK, d, dv, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    mk = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()   # noqa: E731
+    args = (mk(B, H, NQ, d), mk(B, HK, NK, d), mk(B, H, NQ, d), mk(B, HK, NK, d), mk(B, HK, NK, dv))
+    return (*args, 0.2 + 0.6 * torch.rand(H, generator=gen, device="cuda")), mk(B, H, NQ, dv)
+
+
+def dlam_terms(args, do, causal):
+    """dlam and the root of the sum of the squares of its terms P_2 dP, per head, in 64 bits."""
+    q, k, v = (args[i].double() for i in (2, 3, 4))
+    B, H, NQ, d = q.shape
+    HK, NK = k.shape[1:3]
+    hidden = torch.ones(NQ, NK, dtype=torch.bool, device="cuda").triu(NK - NQ + 1) if causal else None
+    value, size = np.zeros(H), np.zeros(H)
+    for b in range(B):
+        for h in range(H):
+            j = h // (H // HK)
+            z = q[b, h] @ k[b, j].t().contiguous() / math.sqrt(d)
+            if causal:
+                z = z.masked_fill(hidden, -math.inf)
+            t = torch.softmax(z, 1) * (do[b, h].double() @ v[b, j].t().contiguous())
+            value[h] -= float(t.sum())
+            size[h] += float((t * t).sum())
+    return value, np.sqrt(size)
+
+
+# Relative to the root of the sum of the squared terms, to which errors that are independent from term to term add up.
+# A term is off by the rounding of its exponent (half a step, 2^-22 below 8, 2^-21 below 16, times ln 2), the exponential
+# (2^-23), its logit and dP (d products in a few float32 sums: 2^-22 each): in norm, a rounding of at most r having the
+# norm r / sqrt(3), 2^-22 with 256 keys and 2^-21 with 8192 (2^13 keys: exponents to 16).
+@pytest.mark.parametrize("B,H,HK,NQ,NK,d,dv,causal,seeds,bound", [
+    (1, 1, 1, 256, 256, 64, 64, False, 24, 2.0 ** -22),    # one head, where the sum cancels
+    (1, 16, 16, 64, 8192, 64, 64, False, 1, 2.0 ** -21),   # long sums; 32 rows a wave
+    (1, 8, 2, 300, 8192, 128, 128, False, 1, 2.0 ** -21),  # 16 rows a wave, the key axis in ranges
+    (2, 4, 2, 200, 4096, 64, 192, True, 2, 2.0 ** -21),
+    (1, 2, 2, 6007, 6007, 128, 128, False, 1, 2.0 ** -21),  # many rows: what their errors have in common adds up
+    (1, 2, 1, 4001, 4001, 64, 128, True, 1, 2.0 ** -21)])
+def test_dlam_is_as_exact_as_its_terms(gpu_lib, B, H, HK, NQ, NK, d, dv, causal, seeds, bound):
+    rel = []
+    for seed in range(seeds):
+        args, do = make(B, H, HK, NQ, NK, d, dv, seed)
+        saved = gpu_lib.diff_fwd(*args, None, causal, save=True)
+        got = gpu_lib.diff_bwd(*args, do, *saved, None, causal, want=("dlam",))[5]
+        value, size = dlam_terms(args, do, causal)
+        rel.append((n64(got) - value) / size)
+    rms = float(np.sqrt(np.mean(np.concatenate(rel) ** 2)))
+    print(f"dlam {rms:.2e}, bound {bound:.2e}", flush=True)
+    assert rms <= bound
