@@ -59,6 +59,12 @@ __device__ __forceinline__ int clamp_len(const int* len, int b, int n) {
   return len ? min(max(len[b], 0), n) : n;
 }
 
+// Natural logarithm of 2^ref l, rounded once: the integer part of log2 l is added in 64 bits.
+__device__ __forceinline__ float diff_lse(float l, float ref) {
+  const double whole = (double)ref + (double)__builtin_amdgcn_frexp_expf(l);
+  return (float)((whole + (double)log2f(__builtin_amdgcn_frexp_mantf(l))) * 0.69314718055994531);
+}
+
 // Byte offset, from the first row of a tile, of logical chunk c of row r, or
 // kOutOfSlab for a chunk past the row's end.
 __device__ __forceinline__ uint32_t row_chunk_offset(int r, int c, int creal, uint32_t row_bytes) {

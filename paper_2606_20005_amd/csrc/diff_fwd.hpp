@@ -28,7 +28,10 @@
 //
 // Rounding: P to bf16 (each term of O is off by at most 2^-8 of itself), O to
 // bf16 once at the end; everything else is float32. The sum l takes the
-// float32 p: with the rounded ones (two at a time by dot products, half of the
+// float32 p, in chunks of kDiffChunk tiles (over 131072 keys the log-sum-exps are
+// off by 3.3e-7, of which 2.7e-7 are the rounding of a value near 12; in one
+// chain by 3.0e-6. Tiles added apart, in float32 or 64 bits, took 1.5 to 2% longer
+// at d 128/256): with the rounded ones (two at a time by dot products, half of the
 // additions) the log-sum-exps, and with them the recomputed probabilities of
 // the backward pass and dlam, were off by up to 1e-3.
 //
@@ -43,6 +46,7 @@
 namespace streamkl {
 
 constexpr float kDiffSlack = 64.f;
+constexpr int kDiffChunk = 16;   // tiles
 
 template <int D, int DV, int RB_, int NW_>
 struct DiffFwdCfg {
@@ -125,11 +129,13 @@ diff_fwd_kernel(const DiffArgs a) {
   wait_vmem();   // before the tile loop: a first use inside it would wait on every trip
 
   f32x16 o[RB][NB];
-  float m[RB], nu[RB], l[RB];   // raw maximum at the last rescaling, -u, the sum of this half-wave's keys
+  float m[RB], nu[RB];   // raw maximum at the last rescaling, -u
+  float lc[RB], l[RB];   // the sum of this half-wave's keys since the last multiple of kDiffChunk tiles, and up to there
 #pragma unroll
   for (int x = 0; x < RB; ++x) {
     m[x] = kNegInf;
     nu[x] = 0.f;
+    lc[x] = 0.f;
     l[x] = 0.f;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) o[x][nb] = zero16();
@@ -198,6 +204,7 @@ diff_fwd_kernel(const DiffArgs a) {
           const float f = m[x] == kNegInf ? 0.f : exp2_fast(c * (m[x] - both));
           m[x] = both;
           nu[x] = -c * both;
+          lc[x] *= f;
           l[x] *= f;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) o[x][nb] *= f;
@@ -209,7 +216,7 @@ diff_fwd_kernel(const DiffArgs a) {
     bf16x8 p[RB][2];
     auto prob = [&](int x, int i) {
       e[x][i] = exp2_fast(__builtin_fmaf(s[x][i], c, nu[x]));
-      l[x] += e[x][i];
+      lc[x] += e[x][i];
       if (i % 8 == 7) p[x][i / 8] = pack8(e[x] + i - 7);
     };
 #pragma unroll
@@ -240,12 +247,22 @@ diff_fwd_kernel(const DiffArgs a) {
       diff_pin();
     }
     __builtin_amdgcn_s_setprio(0);
+    if (t % kDiffChunk == kDiffChunk - 1) {
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        l[x] += lc[x];
+        lc[x] = 0.f;
+      }
+    }
   };
 
   stream_tiles<C::STAGES, 1, C::STAGE, DiffDma<D, DV, C::NT>::NCH>(st0, st1, st2, t_begin, t_end, load, tile);
 
 #pragma unroll
-  for (int x = 0; x < RB; ++x) l[x] += __shfl_xor(l[x], 32);
+  for (int x = 0; x < RB; ++x) {
+    l[x] += lc[x];
+    l[x] += __shfl_xor(l[x], 32);
+  }
 
   Row row[RB];
 #pragma unroll
@@ -288,7 +305,7 @@ diff_fwd_kernel(const DiffArgs a) {
     const float f = l[x] > 0.f || l[x] != l[x] ? 1.f / l[x] : 0.f;   // 0 for rows that see nothing
     const float lam = in ? a.lam[row[x].h] : 0.f;
     if (lse && half == 0 && in)
-      lse[out_row(x)] = !ok || m[x] == kNegInf ? kNegInf : (log2f(l[x]) - nu[x]) * kLn2;
+      lse[out_row(x)] = !ok || m[x] == kNegInf ? kNegInf : diff_lse(l[x], -nu[x]);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       // the wave of map 2 hands its block to the wave of map 1, lane by lane

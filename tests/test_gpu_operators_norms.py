@@ -65,3 +65,20 @@ def test_dlam_is_as_exact_as_its_terms(gpu_lib, B, H, HK, NQ, NK, d, dv, causal,
     rms = float(np.sqrt(np.mean(np.concatenate(rel) ** 2)))
     print(f"dlam {rms:.2e}, bound {bound:.2e}", flush=True)
     assert rms <= bound
+
+
+# The saved value is rounded once: 2^-24 of it, at most 2^-21 below 16, in norm 2^-21 / sqrt(3) = 2.8e-7. The sum over the
+# keys of a half-wave has 256 additions in a chunk and 256 chunks here, each addition off by 2^-24 of a sum that grows:
+# sqrt(256) 2^-24 / 3 in norm, over the two half-waves 2.2e-7. Exponentials (2^-23 each) and the factor of the logits (two
+# roundings of 2^-25, times a mean logit of about 1) are small next to that. Together 3.6e-7.
+@pytest.mark.parametrize("splits", [1, 5, "auto"])
+@pytest.mark.parametrize("d,dv,NQ", [(64, 64, 80), (128, 128, 8)])
+def test_log_sum_exp_does_not_drift(gpu_lib, d, dv, NQ, splits):
+    """Over 131072 keys, in one pass and joined from ranges."""
+    (q1, k1, q2, k2, v, lam), _ = make(1, 2, 1, NQ, 131072, d, dv, seed=d)
+    saved = gpu_lib.diff_fwd(q1, k1, q2, k2, v, lam, splits=splits, save=True)
+    for lse, q, k in ((saved[2], q1, k1), (saved[3], q2, k2)):
+        ref = torch.logsumexp(q[0].double().flatten(0, 1) @ k[0, 0].double().t().contiguous() / math.sqrt(d), 1)
+        rms = float((lse.flatten().double() - ref).pow(2).mean().sqrt())
+        print(f"lse {rms:.2e}", flush=True)
+        assert rms <= 2.0 ** -21
