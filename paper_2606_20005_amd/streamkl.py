@@ -24,6 +24,7 @@ import os
 import typing
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libstreamkl.so")
@@ -452,6 +453,18 @@ def attention_kl(q1, k1, q2, k2, *, s1=None, s2=None, causal=False, direction="f
     return (kl, st1, st2) if return_lse else kl
 
 
+def _differentiated(*tensors):
+    """Whether autograd has to see a call: an input requires a gradient, or may carry a tangent of forward mode (for which
+    the autograd functions have no formula, and raise)."""
+    if forward_ad._current_level >= 0:   # inside dual_level()
+        return True
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
+
+
 # --- norms of queries and keys with the position rotation -------------------------------------------------------------
 
 
@@ -664,8 +677,9 @@ def qk_norm_rope(q, k, wq=None, wk=None, table=None, *, eps=1e-6, q_positions=No
     of (j, j + rot_dim/2). expand_k: write every key head once per query head of its group, so that yk has H heads (the
     gradients of the copies are added).
     """
-    if torch.is_grad_enabled() and (q is not None and q.requires_grad or k is not None and k.requires_grad or
-                                    wq is not None and wq.requires_grad or wk is not None and wk.requires_grad):
+    if _differentiated(q, k, wq, wk, table):
+        if table is not None and table.requires_grad and torch.is_grad_enabled():
+            raise ValueError("the table takes no gradient: pass it detached")
         return _QKNormRope.apply(q, k, wq, wk, table, float(eps), q_positions, k_positions, bool(interleaved),
                                  bool(expand_k))
     return qk_norm_rope_fwd(q, k, wq, wk, table, eps, q_positions, k_positions, interleaved, expand_k)
@@ -865,7 +879,6 @@ def diff_attention(q1, k1, q2, k2, v, lam, *, scale=None, causal=False, q_len=No
     process where a captured backward meets them. The same holds for qk_norm_rope and attention_kl.
     """
     scale = _diff_scale(scale, q1.shape[-1])
-    if torch.is_grad_enabled() and (q1.requires_grad or k1.requires_grad or q2.requires_grad or k2.requires_grad or
-                                    v.requires_grad or lam.requires_grad):
+    if _differentiated(q1, k1, q2, k2, v, lam):
         return _DiffAttention.apply(q1, k1, q2, k2, v, lam, scale, bool(causal), q_len, kv_len)
     return diff_fwd(q1, k1, q2, k2, v, lam, scale, causal, q_len, kv_len)

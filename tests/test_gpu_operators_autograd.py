@@ -1,0 +1,50 @@
+"""What autograd may ask of the operators around the divergence: tangents (refused), upstream gradients as graphs leave
+them."""
+import pytest
+import torch
+from torch.autograd import forward_ad as fw
+
+pytestmark = pytest.mark.gpu
+
+
+def norm_inputs(seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    mk = lambda *s: torch.randn(s, generator=gen, device="cuda")   # noqa: E731
+    return [mk(2, 7, 4, 64).bfloat16(), mk(2, 7, 2, 64).bfloat16(), 1 + 0.1 * mk(64), 1 + 0.1 * mk(64)]
+
+
+def diff_inputs(seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    mk = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()   # noqa: E731
+    return [mk(2, 4, 7, 64), mk(2, 2, 9, 64), mk(2, 4, 7, 64), mk(2, 2, 9, 64), mk(2, 2, 9, 96),
+            torch.rand(4, generator=gen, device="cuda")]
+
+
+@pytest.mark.parametrize("grad_mode", [True, False])
+@pytest.mark.parametrize("name", ["qk_norm_rope", "diff_attention"])
+def test_tangents_are_refused(gpu_lib, name, grad_mode):
+    """A dual input has requires_grad False; its tangent must not be dropped."""
+    call, inputs = getattr(gpu_lib, name), norm_inputs() if name == "qk_norm_rope" else diff_inputs()
+    plain = call(*inputs)
+    with fw.dual_level(), torch.set_grad_enabled(grad_mode):
+        for i, x in enumerate(inputs):
+            args = list(inputs)
+            args[i] = fw.make_dual(x, torch.ones_like(x))
+            with pytest.raises(RuntimeError):
+                call(*args)
+        same = call(*inputs)   # no tangents: as outside
+    for a, b in zip(*((x if isinstance(x, tuple) else (x,)) for x in (plain, same))):
+        assert torch.equal(a, b) and not b.requires_grad
+
+
+def test_a_table_that_requires_a_gradient_is_refused(gpu_lib):
+    q, k, wq, wk = norm_inputs()
+    table = gpu_lib.rope_table(7, 64)
+    plain = gpu_lib.qk_norm_rope(q, k, wq, wk, table)
+    table.requires_grad_(True)
+    with pytest.raises(ValueError):
+        gpu_lib.qk_norm_rope(q, k, wq, wk, table)
+    with torch.no_grad():
+        same = gpu_lib.qk_norm_rope(q, k, wq, wk, table)
+    for x in (same, gpu_lib.qk_norm_rope(q, k, wq, wk, table.detach())):
+        assert torch.equal(x[0], plain[0]) and torch.equal(x[1], plain[1])
