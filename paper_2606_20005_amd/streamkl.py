@@ -465,6 +465,12 @@ def _differentiated(*tensors):
     return False
 
 
+def _upstream(g):
+    """An upstream gradient as the kernels read it: contiguous, 16-byte aligned (a part of a concatenation's need not be)."""
+    g = g.contiguous()
+    return g.clone() if g.data_ptr() & 15 else g
+
+
 # --- norms of queries and keys with the position rotation -------------------------------------------------------------
 
 
@@ -655,7 +661,7 @@ class _QKNormRope(torch.autograd.Function):
         if gk is None and k is not None:
             heads = q.shape[2] if expand_k else k.shape[2]
             gk = torch.zeros((k.shape[0], heads, k.shape[1], k.shape[3]), dtype=torch.bfloat16, device=k.device)
-        gq, gk = (None if g is None else g.contiguous() for g in (gq, gk))
+        gq, gk = (None if g is None else _upstream(g) for g in (gq, gk))
         dq, dk, dwq, dwk = qk_norm_rope_bwd(q, k, gq, gk, wq, wk, table, eps, q_positions, k_positions, interleaved,
                                             expand_k, want_w=need[2] or need[3])
         return (dq if need[0] else None, dk if need[1] else None, dwq if need[2] else None, dwk if need[3] else None,
@@ -857,7 +863,7 @@ class _DiffAttention(torch.autograd.Function):
         want = tuple(n for n, need in zip(DIFF_GRADS, ctx.needs_input_grad) if need)
         if not want:
             return (None,) * 10
-        grads = diff_bwd(q1, k1, q2, k2, v, lam, dout.to(torch.bfloat16).contiguous(), *saved, scale, causal, q_len,
+        grads = diff_bwd(q1, k1, q2, k2, v, lam, _upstream(dout.to(torch.bfloat16)), *saved, scale, causal, q_len,
                          kv_len, want=want, grad_dtype=torch.bfloat16)
         return (*grads, None, None, None, None)
 

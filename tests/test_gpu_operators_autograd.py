@@ -48,3 +48,23 @@ def test_a_table_that_requires_a_gradient_is_refused(gpu_lib):
         same = gpu_lib.qk_norm_rope(q, k, wq, wk, table)
     for x in (same, gpu_lib.qk_norm_rope(q, k, wq, wk, table.detach())):
         assert torch.equal(x[0], plain[0]) and torch.equal(x[1], plain[1])
+
+
+@pytest.mark.parametrize("name", ["qk_norm_rope", "diff_attention"])
+@pytest.mark.parametrize("before", [1, 4, 8])
+def test_upstream_gradients_of_a_concatenation(gpu_lib, name, before):
+    """They are contiguous views that begin anywhere."""
+    inputs = [x.requires_grad_(True) for x in (norm_inputs() if name == "qk_norm_rope" else diff_inputs())]
+    outs = getattr(gpu_lib, name)(*inputs)
+    outs = outs if isinstance(outs, tuple) else (outs,)
+    pad = torch.zeros(before, dtype=torch.bfloat16, device="cuda")
+    joint = torch.cat([y for out in outs for y in (pad, out.flatten())])
+    g = torch.randn(joint.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).bfloat16()
+    got = torch.autograd.grad(joint, inputs, g, retain_graph=True)
+    parts, at = [], 0
+    for out in outs:
+        at += before
+        parts.append(g[at:at + out.numel()].view(out.shape).clone())
+        at += out.numel()
+    for a, b in zip(got, torch.autograd.grad(outs, inputs, parts)):
+        assert torch.equal(a, b)
