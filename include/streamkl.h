@@ -385,8 +385,9 @@ typedef struct {
  *             contiguous [N] shared by all sequences (*_pos_shared = 1) or
  *             [B, N]. NULL: keys stand at 0 .. N_K - 1 and queries are the
  *             last N_Q of these places (bottom-right alignment; N_Q <= N_K
- *             then, and N_Q = places 0 .. N_Q - 1 without keys). A position
- *             outside the table gives NaN in the rotated columns of its rows;
+ *             then), whatever k_pos says; without keys, at 0 .. N_Q - 1. With
+ *             rot > 0 these places have to be in the table. A position given
+ *             that is outside it gives NaN in the rotated columns of its rows;
  *             nothing is read there.
  *   k_copies  every key head is written this often in a row: yk has
  *             HK k_copies heads. With k_copies = H / HK it has one per query

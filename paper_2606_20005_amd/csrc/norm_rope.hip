@@ -463,6 +463,18 @@ int check_call(int B, int d, int dtype, float eps, const float* table, int n_pos
   return STREAMKL_OK;
 }
 
+// The places that rows without positions stand at, all of them in the table:
+// keys at 0 .. N_K - 1, queries at the last N_Q of these (without keys, at
+// 0 .. N_Q - 1).
+int check_places(bool has_q, bool has_k, bool keys_given, bool queries_given, int N_Q, int N_K, const void* q_pos,
+                 const void* k_pos, int rot, int n_pos) {
+  if (rot == 0) return STREAMKL_OK;
+  if (keys_given && queries_given && !q_pos && N_Q > N_K) return STREAMKL_ERR_INVALID_ARG;   // places before the first
+  if (has_k && !k_pos && N_K > n_pos) return STREAMKL_ERR_INVALID_ARG;
+  if (has_q && !q_pos && (keys_given ? N_K : N_Q) > n_pos) return STREAMKL_ERR_INVALID_ARG;
+  return STREAMKL_OK;
+}
+
 NrSide make_side(const streamkl_rows* x, bool present, int B, int N, int H, int copies, const float* w, const void* pos,
                  int pos_shared, int start, int d, int most_blocks) {
   NrSide s = {};
@@ -538,8 +550,8 @@ extern "C" int streamkl_qk_norm_rope_fwd(const streamkl_rows* q, const streamkl_
   bool has_q = false, has_k = false;
   if (st == STREAMKL_OK) st = check_side(q, B, N_Q, H, 1, dtype, wq, q_pos, pos64, yq, &has_q);
   if (st == STREAMKL_OK) st = check_side(k, B, N_K, HK, k_copies, dtype, wk, k_pos, pos64, yk, &has_k);
+  if (st == STREAMKL_OK) st = check_places(has_q, has_k, k, q, N_Q, N_K, q_pos, k_pos, rot, n_pos);
   if (st != STREAMKL_OK) return st;
-  if (rot > 0 && q && k && !q_pos && N_Q > N_K) return STREAMKL_ERR_INVALID_ARG;   // places before the first
   if (!has_q && !has_k) return STREAMKL_OK;
   NrArgs a = {};
   // without positions the queries are the last N_Q of the N_K places
@@ -587,8 +599,8 @@ extern "C" int streamkl_qk_norm_rope_bwd(const streamkl_rows* q, const streamkl_
   if (st == STREAMKL_OK && dy_dtype != STREAMKL_BF16 && dy_dtype != STREAMKL_F32) st = STREAMKL_ERR_INVALID_ARG;
   if (st == STREAMKL_OK) st = check_side(q, B, N_Q, H, 1, dtype, wq, q_pos, pos64, dxq, &has_q);
   if (st == STREAMKL_OK) st = check_side(k, B, N_K, HK, k_copies, dtype, wk, k_pos, pos64, dxk, &has_k);
+  if (st == STREAMKL_OK) st = check_places(has_q, has_k, k, q, N_Q, N_K, q_pos, k_pos, rot, n_pos);
   if (st != STREAMKL_OK) return st;
-  if (rot > 0 && q && k && !q_pos && N_Q > N_K) return STREAMKL_ERR_INVALID_ARG;   // places before the first
   if ((has_q && (!dyq || !aligned_to(dyq, 16))) || (has_k && (!dyk || !aligned_to(dyk, 16))))
     return STREAMKL_ERR_INVALID_ARG;
   if ((dwq && !aligned_to(dwq, 4)) || (dwk && !aligned_to(dwk, 4))) return STREAMKL_ERR_INVALID_ARG;

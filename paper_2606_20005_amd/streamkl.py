@@ -570,6 +570,10 @@ def _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k):
         raise ValueError("an extent does not fit 31 bits")
     if NQ > NK and table is not None and k is not None and q is not None and q_positions is None:
         raise ValueError("more queries than keys: their positions have to be given")
+    if (NQ > n_pos or NK > n_pos) and table is not None:   # the last places of rows without positions
+        for n, p, t, last in (("q", q_positions, q, NQ if k is None else NK), ("k", k_positions, k, NK)):
+            if p is None and t is not None and t.numel() and last > n_pos:
+                raise ValueError(f"{n} reaches position {last - 1}, the table holds {n_pos}")
     copies = 1
     if expand_k:
         if q is None or k is None or HK == 0 or H % HK:
@@ -679,8 +683,10 @@ def qk_norm_rope(q, k, wq=None, wk=None, table=None, *, eps=1e-6, q_positions=No
 
     wq, wk: float32 [d] or None (ones). table: rope_table(...), or None for the norm alone. q_positions, k_positions:
     int32 or int64 [N] or [B, N]; by default keys stand at 0 .. N_K - 1 and queries are the last N_Q of these places,
-    as everywhere in this library. A position outside the table gives NaN rows. interleaved: pairs (2j, 2j + 1) instead
-    of (j, j + rot_dim/2). expand_k: write every key head once per query head of its group, so that yk has H heads (the
+    as everywhere in this library. A side's default does not follow positions that are given for the other: with
+    k_positions alone, queries still stand at N_K - N_Q .. N_K - 1. Places by default have to be in the table; a
+    position given that is outside it gives NaN in the rotated columns. interleaved: pairs (2j, 2j + 1) instead of
+    (j, j + rot_dim/2). expand_k: write every key head once per query head of its group, so that yk has H heads (the
     gradients of the copies are added).
     """
     if _differentiated(q, k, wq, wk, table):

@@ -68,3 +68,19 @@ def test_upstream_gradients_of_a_concatenation(gpu_lib, name, before):
         at += out.numel()
     for a, b in zip(got, torch.autograd.grad(outs, inputs, parts)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("q_rows,k_rows,n_pos,given,fits", [
+    (7, 7, 6, "", False), (7, 7, 7, "", True), (2, 7, 6, "", False), (7, None, 6, "", False), (None, 7, 6, "", False),
+    (2, 7, 6, "k", False), (2, 7, 6, "q", False), (2, 7, 3, "qk", True), (7, 7, None, "", True)])
+def test_default_positions_have_to_be_in_the_table(gpu_lib, q_rows, k_rows, n_pos, given, fits):
+    q, k, wq, wk = norm_inputs()
+    q, k = (None if n is None else x[:, :n] for x, n in ((q, q_rows), (k, k_rows)))
+    table = None if n_pos is None else gpu_lib.rope_table(n_pos, 32)
+    opts = {n + "_positions": torch.arange(x.shape[1], device="cuda") % 3 for n, x in (("q", q), ("k", k)) if n in given}
+    if fits:
+        for y in gpu_lib.qk_norm_rope(q, k, wq, wk, table, **opts):
+            assert torch.isfinite(y).all()
+    else:
+        with pytest.raises(ValueError):
+            gpu_lib.qk_norm_rope(q, k, wq, wk, table, **opts)
