@@ -406,7 +406,9 @@ int streamkl_qk_norm_rope_fwd(const streamkl_rows* q, const streamkl_rows* k, in
 /*
  * Gradients of streamkl_qk_norm_rope_fwd, from its inputs alone.
  *   dyq, dyk  upstream gradients in the layout of yq, yk, bf16 or float32
- *             (dy_dtype); the gradients of a key head's copies are added.
+ *             (dy_dtype); the gradients of a key head's copies are added. Rows
+ *             at positions outside the table whose gradients are zero
+ *             (padding) have zero dxq, dxk and no part in dwq, dwk.
  *   dxq, dxk  contiguous [B, N_Q, H, d] and [B, N_K, HK, d] in the inputs'
  *             type, 16-byte aligned.
  *   dwq, dwk  float32 [d]; NULL: not wanted.

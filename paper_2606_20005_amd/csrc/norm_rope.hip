@@ -122,6 +122,7 @@ template <int TPR, int ROT>
 struct Place {
   int c, b, n, src;            // chunk, sequence, token, lane of the partner chunk
   bool live;                   // the token exists and the chunk lies inside the row
+  bool known;                  // its position is in the table, or nothing is rotated
   float co[8], si[8];          // of the own columns; si is 0 and co 1 where nothing is rotated
 
   __device__ __forceinline__ Place(const NrArgs& a, const NrSide& s, int group, int lane) {
@@ -133,6 +134,7 @@ struct Place {
     n = token ? t - b * s.N : 0;
     live = token && 8 * c < a.d;
     src = lane;
+    known = true;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       co[e] = 1.f;
@@ -148,7 +150,7 @@ struct Place {
         p = a.pos64 ? static_cast<const long long*>(s.pos)[i] : static_cast<const int*>(s.pos)[i];
       }
       // a position outside the table: NaN in the rotated columns, nothing is read
-      const bool known = p >= 0 && p < a.n_pos;
+      known = p >= 0 && p < a.n_pos;
       if (live && turned) {
         const float* row = a.table + (known ? p : 0) * a.rot;
         if constexpr (ROT == kRotHalf) {
@@ -280,6 +282,7 @@ __global__ void __launch_bounds__(kThreads) norm_rope_bwd_kernel(const NrArgs a)
     const int group = item / s.chunks, h0 = (item - group * s.chunks) * s.heads_per_item;
     const int h1 = min(h0 + s.heads_per_item, s.H);
     const Place<TPR, ROT> at(a, s, group, lane);
+    const bool strange = ROT != kRotNone && __builtin_amdgcn_ballot_w64(!at.known) != 0;
     const T* px = static_cast<const T*>(s.x) + (long long)at.b * s.sb + (long long)at.n * s.sn + 8 * at.c;
     const TG* pg = static_cast<const TG*>(s.dy) + 8 * at.c;
     pg += (long long)at.b * s.H * s.copies * hstride + (long long)at.n * a.d;
@@ -323,8 +326,15 @@ __global__ void __launch_bounds__(kThreads) norm_rope_bwd_kernel(const NrArgs a)
           for (int e = 0; e < 8; ++e) gp[e] = g[e ^ 1];
         }
         // the transposed rotation: the sine changes its sign
+        float turned[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = __builtin_fmaf(-at.si[e], gp[e], at.co[e] * g[e]);
+        for (int e = 0; e < 8; ++e) turned[e] = __builtin_fmaf(-at.si[e], gp[e], at.co[e] * g[e]);
+        if (strange) {   // a row outside the table that the loss does not reach (padding): no gradient, not 0 times NaN
+#pragma unroll
+          for (int e = 0; e < 8; ++e) turned[e] = !at.known && g[e] == 0.f && gp[e] == 0.f ? 0.f : turned[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = turned[e];
       }
       float ss = 0.f, hx = 0.f, hh[8];
 #pragma unroll

@@ -685,8 +685,8 @@ def qk_norm_rope(q, k, wq=None, wk=None, table=None, *, eps=1e-6, q_positions=No
     int32 or int64 [N] or [B, N]; by default keys stand at 0 .. N_K - 1 and queries are the last N_Q of these places,
     as everywhere in this library. A side's default does not follow positions that are given for the other: with
     k_positions alone, queries still stand at N_K - N_Q .. N_K - 1. Places by default have to be in the table; a
-    position given that is outside it gives NaN in the rotated columns. interleaved: pairs (2j, 2j + 1) instead of
-    (j, j + rot_dim/2). expand_k: write every key head once per query head of its group, so that yk has H heads (the
+    position given that is outside it gives NaN in the rotated columns, and no gradient where the loss does not reach
+    the row (padding). interleaved: pairs (2j, 2j + 1) instead of (j, j + rot_dim/2). expand_k: write every key head once per query head of its group, so that yk has H heads (the
     gradients of the copies are added).
     """
     if _differentiated(q, k, wq, wk, table):

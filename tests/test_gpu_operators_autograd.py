@@ -84,3 +84,30 @@ def test_default_positions_have_to_be_in_the_table(gpu_lib, q_rows, k_rows, n_po
     else:
         with pytest.raises(ValueError):
             gpu_lib.qk_norm_rope(q, k, wq, wk, table, **opts)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("expand_k", [False, True])
+def test_padding_outside_the_table_leaves_gradients_alone(gpu_lib, interleaved, expand_k):
+    """A padded batch whose padding has position -1 and no upstream gradient: the gradients of the rows before it."""
+    q, k, wq, wk = (x.requires_grad_(True) for x in norm_inputs())
+    table = gpu_lib.rope_table(16, 32)
+    at = torch.arange(7, dtype=torch.int32, device="cuda").repeat(2, 1)
+    at[1, 4:] = -1
+    opts = dict(interleaved=interleaved, expand_k=expand_k)
+    out = gpu_lib.qk_norm_rope(q, k, wq, wk, table, q_positions=at, k_positions=at, **opts)
+    assert torch.isnan(out[0][1, :, 4:, :32]).all() and torch.isfinite(out[0][1, :, :4]).all()
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    up = [torch.randn(y.shape, generator=gen, device="cuda").bfloat16() for y in out]
+    for u in up:
+        u[1, :, 4:] = 0
+    got = torch.autograd.grad(out, (q, k, wq, wk), up)
+    assert not got[0][1, 4:].any() and not got[1][1, 4:].any()
+    at[1, 4:] = 3   # inside the table, still no gradient
+    ref = torch.autograd.grad(gpu_lib.qk_norm_rope(q, k, wq, wk, table, q_positions=at, k_positions=at, **opts),
+                              (q, k, wq, wk), up)
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)
+    up[0][1, 2, 5, 1] = 1.0   # a row that the loss reaches: NaN, not a number that is wrong
+    out = gpu_lib.qk_norm_rope(q, k, wq, wk, table, q_positions=at.where(at != 3, -1), k_positions=at, **opts)
+    assert torch.isnan(torch.autograd.grad(out, (wq,), up)[0]).any()
