@@ -438,7 +438,9 @@ size_t streamkl_qk_norm_rope_bwd_workspace_bytes(int B, int H, int HK, int N_Q, 
  *             more than 4 GiB). H is a multiple of HK: groups of H / HK consecutive query heads share a key
  *             head, and their keys and values are streamed once for the group.
  *   d         a multiple of 32, 32 to 128;  dv a multiple of 32, 32 to 256.
- *   scale     2^-64 to 2^64 (usual: 1/sqrt(d)); the scaled logits must stay in the float32 range.
+ *   scale     2^-64 to 2^64 (usual: 1/sqrt(d)). Scaled logits must stay below 2^28: the exponent of a probability is a
+ *             float32 difference. The backward pass forms it from the log-sum-exp, so that probabilities there are off
+ *             by up to 2^-22 |LSE| of themselves (0.2% at 10^4).
  *   lam       float32 [H] on the device, any sign.
  *   q_len, kv_len  int32 [B] on the device, or NULL: sequence b has its first q_len[b] rows and kv_len[b] keys
  *             (values outside 0 .. N are clamped). Keys behind kv_len are not read, whatever they hold.
@@ -457,9 +459,10 @@ size_t streamkl_qk_norm_rope_bwd_workspace_bytes(int B, int H, int HK, int N_Q, 
  *   out2, lse1, lse2  what the backward pass needs: O_2 = P_2 V (layout of out) and the natural-log
  *             log-sum-exps [B, H, N_Q] of the two maps; each may be NULL.
  * Sums, maxima and accumulators are float32; P_t is rounded to bf16 as an operand of the product with V, O once at
- * the end. Keys that a row may see are expected finite, as are the rows: a non-finite value in a key row that the
- * causal mask hides from row i can reach it where both fall into one 32-key tile (0 x inf), never through kv_len
- * or q_len.
+ * the end. Inputs are expected finite. A non-finite value spoils every result that it takes part in, and results that
+ * the causal mask keeps apart from it (0 x inf) where the kernels work on both at once: a row j of v, and in the
+ * backward pass of k1 and k2, those of rows that stand up to 94 places before it (kv_len - q_len + i >= j - 94); a row
+ * of q1, q2 or dout those of keys up to 62 places behind it. Never through kv_len or q_len.
  */
 int streamkl_diff_fwd(const streamkl_rows* q1, const streamkl_rows* k1, const streamkl_rows* q2,
                       const streamkl_rows* k2, const streamkl_rows* v,
