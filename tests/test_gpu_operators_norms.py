@@ -82,3 +82,61 @@ def test_log_sum_exp_does_not_drift(gpu_lib, d, dv, NQ, splits):
         rms = float((lse.flatten().double() - ref).pow(2).mean().sqrt())
         print(f"lse {rms:.2e}", flush=True)
         assert rms <= 2.0 ** -21
+
+
+def partial_floats(sk, B, H, HK, NQ, NK, d, dv, causal):
+    """Floats of partial gradients in the backward's workspace; the sums for dlam at most added."""
+    return sk.diff_bwd_workspace_bytes(B, H, HK, NQ, NK, d, dv, causal) // 4 - B * H * -(-NQ // 32) * 128
+
+
+def check(sk, args, do, causal, q_len=None, kv_len=None):
+    """Outputs and gradients element by element, and in norm. Each is a sum of products of which one operand is rounded to
+    bf16 (2^-8 / sqrt(3) in norm), with the outputs' own rounding, or that of the outputs in D: three such, 2^-8."""
+    lens = [None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda") for x in (q_len, kv_len)]
+    saved = sk.diff_fwd(*args, None, causal, *lens, save=True)
+    got = sk.diff_bwd(*args, do, *saved, None, causal, *lens)
+    torch.cuda.synchronize()
+    plain = [n64(a) for a in args]
+    scale = plain[0].shape[-1] ** -0.5
+    ref, tol = oo.diff(*plain, scale, causal, q_len, kv_len)
+    grads, gtol = oo.diff_backward(*plain, scale, causal, n64(do), q_len, kv_len)
+    pairs = [("out", saved[0], ref["out"], tol["out"]), ("out2", saved[1], ref["out2"], tol["out2"])]
+    pairs += [(n, t, grads[n], gtol[n]) for n, t in zip(NAMES, got)]
+    for n, t, r, bound in pairs:
+        e = np.abs(n64(t) - r)
+        assert (e <= bound + 1e-30).all(), f"{n}: worst {np.nanmax(e / (bound + 1e-30)):.2f} bounds"
+        if n != "dlam":
+            norm = float(np.sqrt((e * e).sum()) / np.sqrt((r * r).sum()))
+            print(f"{n} {norm:.2e}", flush=True)
+            assert norm <= 2.0 ** -8, n
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,dv", [(64, 64), (64, 128), (96, 160), (128, 128), (64, 192), (128, 256)])
+@pytest.mark.parametrize("NK,kv_len", [(1000, None), (2011, [2011, 1203])])
+def test_query_gradients_from_ranges_of_keys(gpu_lib, d, dv, NK, kv_len, causal):
+    """Few rows against many keys; partials that are larger than the key-owned kernel's would be."""
+    B, H, HK, NQ = (1 if kv_len is None else 2), 4, 2, 100
+    floats = partial_floats(gpu_lib, B, H, HK, NQ, NK, d, dv, causal)
+    assert floats >= 2 * (2 * B * H * NQ * d) and floats < 2 * (B * HK * NK * (2 * d + dv))
+    args, do = make(B, H, HK, NQ, NK, d, dv, seed=d + dv)
+    check(gpu_lib, args, do, causal, None, kv_len)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,dv", [(32, 64), (64, 128), (96, 160), (128, 128), (96, 256), (128, 192), (128, 256)])
+@pytest.mark.parametrize("G,NQ,q_len", [(8, 300, None), (2, 1100, [1100, 770])])
+def test_key_gradients_from_ranges_of_rows(gpu_lib, d, dv, G, NQ, q_len, causal):
+    """Many rows, of several heads, against few keys: the key-owned kernel has several ranges, the other one (seven key
+    tiles)."""
+    B, NK = (1 if q_len is None else 2), 201
+    assert partial_floats(gpu_lib, B, G, 1, NQ, NK, d, dv, causal) >= 2 * (B * NK * (2 * d + dv))
+    args, do = make(B, G, 1, NQ, NK, d, dv, seed=d + dv)
+    check(gpu_lib, args, do, causal, q_len, None)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,dv", [(64, 64), (128, 128)])
+def test_square_maps_in_norm(gpu_lib, d, dv, causal):
+    args, do = make(1, 2, 2, 256, 256, d, dv, seed=d)
+    check(gpu_lib, args, do, causal)
