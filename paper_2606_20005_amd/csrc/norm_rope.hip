@@ -585,7 +585,7 @@ extern "C" int streamkl_qk_norm_rope_fwd(const streamkl_rows* q, const streamkl_
 }
 
 extern "C" size_t streamkl_qk_norm_rope_bwd_workspace_bytes(int B, int H, int HK, int N_Q, int N_K, int d) {
-  if (B < 0 || H < 0 || HK < 0 || N_Q < 0 || N_K < 0 || d < 32 || d > 256) return 0;
+  if (B < 0 || H < 0 || HK < 0 || N_Q < 0 || N_K < 0 || d < 32 || d > 256 || d % 32 != 0) return 0;
   if (!countable(B, N_Q, H) || !countable(B, N_K, HK)) return 0;
   NrSide q = {}, k = {};
   q.tokens = B * N_Q;

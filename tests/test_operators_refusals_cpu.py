@@ -37,3 +37,10 @@ def test_default_places_of_no_rows_and_without_a_rotation(sk):
     for rot in (0, 64):
         assert sk.lib.streamkl_qk_norm_rope_fwd(rows, rows, 0, 4, 2, 100, 100, 64, 0, FAKE, FAKE, 1e-6, FAKE, 8, rot, 0, None,
                                                 None, 0, 0, 0, 1, None, None, None) == 0
+
+
+def test_workspace_of_head_dims_that_are_refused(sk):
+    f = sk.lib.streamkl_qk_norm_rope_bwd_workspace_bytes
+    for d in (16, 40, 48, 250, 288):
+        assert f(2, 4, 2, 10, 10, d) == 0
+    assert f(2, 4, 2, 10, 10, 96) > 0
