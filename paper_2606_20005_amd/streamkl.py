@@ -618,7 +618,7 @@ def qk_norm_rope_bwd(q, k, dyq, dyk, wq=None, wk=None, table=None, eps=1e-6, q_p
     cfg = _prep_inputs(q, k, wq, wk, table, q_positions, k_positions, expand_k)
     dev, B, H, HK, NQ, NK, d, _, _, copies = cfg
     shapes = (None if q is None else (B, H, NQ, d), None if k is None else (B, HK * copies, NK, d))
-    kind = (dyq if q is not None else dyk).dtype
+    kind = getattr(dyq if q is not None else dyk, "dtype", None)
     for n, shape, t in zip(("dyq", "dyk"), shapes, (dyq, dyk)):
         if (shape is None) != (t is None):
             raise ValueError(f"{n} must be given exactly where {n[-1]} is")

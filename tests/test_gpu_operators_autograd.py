@@ -111,3 +111,11 @@ def test_padding_outside_the_table_leaves_gradients_alone(gpu_lib, interleaved, 
     up[0][1, 2, 5, 1] = 1.0   # a row that the loss reaches: NaN, not a number that is wrong
     out = gpu_lib.qk_norm_rope(q, k, wq, wk, table, q_positions=at.where(at != 3, -1), k_positions=at, **opts)
     assert torch.isnan(torch.autograd.grad(out, (wq,), up)[0]).any()
+
+
+def test_gradients_of_a_side_that_is_not_there_are_refused(gpu_lib):
+    q, k, wq, wk = norm_inputs()
+    yq, yk = gpu_lib.qk_norm_rope_fwd(q, k, wq, wk)
+    for args in ((q, k, None, yk), (q, k, yq, None), (q, None, yq, yk), (None, k, yq, yk), (q, None, None, None)):
+        with pytest.raises(ValueError):
+            gpu_lib.qk_norm_rope_bwd(*args, wq, wk)
