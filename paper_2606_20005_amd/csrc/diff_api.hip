@@ -125,11 +125,16 @@ double visible_share(int N_Q, int N_K, int causal) {
 // leaves the chip unevenly filled, the walk is cut into ranges whose partial
 // float32 gradients a further kernel adds up. The number of ranges is the one
 // with the least estimated time: rounds of resident workgroups times steps,
-// about 0.042 us an MFMA and resident wave of a SIMD (measured 0.038 to 0.048), and the
-// partials written and read back at 4 TB/s. Measured, us, one range and the
-// choice: dQ of 16 heads x 64 rows against 65536 keys, d 128/128, 2196 and 186;
-// dK dV of 4 x 12 heads x 1021 on 4 key heads, d 96/160 causal, 200 and 144;
-// both of 8 heads x 6007, d 128/128, 465 and 415, 811 and 643.
+// about 0.042 us an MFMA and resident wave of a SIMD, and the partials written and
+// read back at 4 TB/s. The estimate is that of the kernels with 32 rows (keys) a
+// wave (measured 0.038 to 0.048 us); where those with 16 run, with half of the rows
+// a block and two workgroups a CU, it only ranks the counts. Measured, us, with
+// the statistics and the joins, one range, the choice and the best of 1, 2, 3, 4,
+// 6, 8, 16 and 32: dQ of 16 heads x 64 rows against 65536 keys, d 128/128, 1591,
+// 172 and 163; dK dV of 4 x 12 heads x 1021 ragged rows on 4 key heads, d 96/160
+// causal, 110, 91 and 83; both of 8 heads x 6007, d 128/128, 404, 405 and 404, 522,
+// 510 and 509; of 6 heads x 3001 causal, 96/96, 83, 67 and 65, 103, 80 and 79; of 4
+// heads x 3001 causal on 2 key heads, 128/256, 100, 76 and 65, 526, 165 and 142.
 struct GradSplits {
   int q, k;
   size_t part_floats;

@@ -92,10 +92,6 @@ struct TileRows {
   }
 };
 
-// Staging of a tile of three matrices A, B (DA columns each) and C (DC
-// columns), 32 rows each, by direct-to-LDS loads of NT threads: stage layout
-// [A | B | C], every matrix in the swizzled layout of kl_common.hpp, or in
-// that of swz16 (K16).
 // Swizzle of a tile that is read as 16x16x32 operands: bijective in the 16
 // rows of a row read, whose service groups of 16 lanes are rows 0-3 and 12-15
 // at one chunk with rows 4-11 at the next (chunk c and c ^ 1), and the reverse;
@@ -109,6 +105,10 @@ __host__ __device__ constexpr int swz16(int r) {
   return CPR % 16 == 0 ? 4 * (r & 3) + low : 4 * ((r >> 1) & 1) + low;
 }
 
+// Staging of a tile of three matrices A, B (DA columns each) and C (DC
+// columns), 32 rows each, by direct-to-LDS loads of NT threads: stage layout
+// [A | B | C], every matrix in the swizzled layout of kl_common.hpp, or in
+// that of swz16 (K16).
 template <int DA, int DC, int NT, bool K16 = false>
 struct DiffDma {
   static constexpr int CA = lds_cols(DA) / 8, CC = lds_cols(DC) / 8;

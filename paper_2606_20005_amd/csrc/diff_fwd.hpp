@@ -33,7 +33,7 @@
 // chain by 3.0e-6. Tiles added apart, in float32 or 64 bits, took 1.5 to 2% longer
 // at d 128/256): with the rounded ones (two at a time by dot products, half of the
 // additions) the log-sum-exps, and with them the recomputed probabilities of
-// the backward pass and dlam, were off by up to 1e-3.
+// the backward pass, were off by up to 1e-3.
 //
 // splits > 1: blockIdx.y takes a contiguous range of the key tiles and leaves
 // unnormalised float32 sums and their reference in `part`; a second kernel

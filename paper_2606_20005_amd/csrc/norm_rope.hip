@@ -189,7 +189,7 @@ __device__ __forceinline__ void load_weight(const float* w, int c, bool live, fl
   }
 }
 
-// y = own values times `own` plus partner values times `other`.
+// The values that those of this lane are rotated with, from their raw chunk.
 template <typename T, int ROT>
 __device__ __forceinline__ void partner8(const Raw<T>& raw, const float (&x)[8], int src, float (&xp)[8]) {
   if constexpr (ROT == kRotHalf) {
