@@ -140,3 +140,28 @@ def test_key_gradients_from_ranges_of_rows(gpu_lib, d, dv, G, NQ, q_len, causal)
 def test_square_maps_in_norm(gpu_lib, d, dv, causal):
     args, do = make(1, 2, 2, 256, 256, d, dv, seed=d)
     check(gpu_lib, args, do, causal)
+
+
+# Terms g x r are off by a few roundings of 2^-24, r in common to a row; a lane adds up to about a hundred of them, 2048
+# partial rows follow in runs of 32 and 64. Independent roundings, relative to the root of the sum of the squares: below
+# sqrt(4 + 100 / 3) 2^-24 / sqrt(3) = 2.1e-7.
+@pytest.mark.parametrize("B,N,H,HK,d,rot,dtype", [(1, 4096, 32, 8, 128, 128, torch.bfloat16), (4, 1021, 12, 12, 96, 64, torch.float32),
+                                                  (1, 1, 1, 1, 64, 64, torch.float32), (2, 700, 3, 1, 256, 0, torch.float16)])
+def test_norm_weight_gradients_are_as_exact_as_their_terms(gpu_lib, B, N, H, HK, d, rot, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    mk = lambda *s: torch.randn(s, generator=gen, device="cuda")   # noqa: E731
+    q, k, w = mk(B, N, H, d).to(dtype), mk(B, N, HK, d).to(dtype), 1 + 0.2 * mk(2, d)
+    table = gpu_lib.rope_table(N, rot) if rot else None
+    dy = mk(B, H, N, d).bfloat16(), mk(B, HK, N, d).bfloat16()
+    got = gpu_lib.qk_norm_rope_bwd(q, k, *dy, w[0], w[1], table)
+    for x, g, dw in ((q, dy[0], got[2]), (k, dy[1], got[3])):
+        x, g = x.double(), g.double().transpose(1, 2)
+        if rot:
+            c, s = (t[None, :, None] for t in table.double().split(rot // 2, 1))
+            a, b = g[..., :rot // 2], g[..., rot // 2:rot]
+            g = torch.cat((a * c + b * s, b * c - a * s, g[..., rot:]), -1)
+        t = (g * x / torch.sqrt((x * x).mean(-1, keepdim=True) + 1e-6)).flatten(0, 2)
+        rel = (dw.double() - t.sum(0)) / t.square().sum(0).sqrt()
+        rms = float(rel.square().mean().sqrt())
+        print(f"dw {rms:.2e}", flush=True)
+        assert rms <= 2.0 ** -22
