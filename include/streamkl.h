@@ -459,7 +459,8 @@ size_t streamkl_qk_norm_rope_bwd_workspace_bytes(int B, int H, int HK, int N_Q, 
  *   out2, lse1, lse2  what the backward pass needs: O_2 = P_2 V (layout of out) and the natural-log
  *             log-sum-exps [B, H, N_Q] of the two maps; each may be NULL.
  * Sums, maxima and accumulators are float32; P_t is rounded to bf16 as an operand of the product with V, O once at
- * the end. Inputs are expected finite. A non-finite value spoils every result that it takes part in, and results that
+ * the end. Inputs are expected finite, values and upstream gradients below 2^40 in size (probabilities are summed up to
+ * 2^64 above their reference). A non-finite value spoils every result that it takes part in, and results that
  * the causal mask keeps apart from it (0 x inf) where the kernels work on both at once: a row j of v, and in the
  * backward pass of k1 and k2, those of rows that stand up to 94 places before it (kv_len - q_len + i >= j - 94); a row
  * of q1, q2 or dout those of keys up to 62 places behind it. Never through kv_len or q_len.

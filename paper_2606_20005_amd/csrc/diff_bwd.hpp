@@ -31,7 +31,11 @@
 //
 // Rounding: the logit gradients and P_1 - lam P_2 to bf16 as operands of the
 // second contraction (each term is off by at most 2^-8 of itself), gradients
-// once when they are written. D_t is formed from the bf16 outputs O and O_2.
+// once when they are written. D_t is formed from the bf16 outputs O and O_2, what
+// a layer keeps anyway (in float32 they would be twice the bytes to save and to
+// read): where a map is almost one key and dP - D cancels, that is the larger part
+// of a gradient's error, 1% in norm for N(0,1) rows at scale 1, d 32, 0.2% at scale
+// 1/sqrt(d).
 //
 // dlam can cancel to far below its terms P_2 dP, so it is held to what float32
 // gives each of them:

@@ -78,3 +78,25 @@ def test_logits_up_to_2_28(gpu_lib, d, dv, sign, splits):
     assert ((out.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2 * small).all()
     for lse, n in ((lse1, 100 if sign > 0 else 200), (lse2, 200)):
         assert ((lse.double() - (sign * top + math.log(n))).abs() <= 2.0 ** -22 * top).all()
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+def test_values_up_to_2_40_above_a_reference_that_stays(gpu_lib, splits):
+    """Logits that rise by just under 64 doublings after the first tile, which does not move the reference."""
+    args, _ = make(1, 2, 1, 40, 400, 64, 64)
+    q1, k1, q2, k2, v, _ = args
+    rise = 63.0 * math.log(2)
+    for q, k in ((q1, k1), (q2, k2)):
+        q.fill_(1.0)
+        k.fill_(0.0)
+        k[:, :, 32:].fill_(rise / 64)
+    v.mul_(2.0 ** 38)
+    out, out2, lse1, _ = gpu_lib.diff_fwd(*args, 1.0, False, splits=splits, save=True)
+    top = float(k1[0, 0, 32].double().sum())
+    w = torch.ones(400, dtype=torch.float64, device="cuda")
+    w[:32] = math.exp(-top)
+    mean = (w[:, None] * v[0, 0].double()).sum(0) / w.sum()
+    # equal probabilities above the first tile, whose rounding to bf16 is one factor, at most 2^-8; float32 sums
+    small = 2.0 ** -16 * v.double().abs().mean()
+    assert ((out2.double() - mean).abs() <= 2.0 ** -7 * mean.abs() + small).all()
+    assert ((lse1.double() - (top + math.log(float(w.sum())))).abs() <= 2.0 ** -18).all()
