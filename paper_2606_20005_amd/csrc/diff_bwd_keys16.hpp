@@ -4,9 +4,9 @@
 // 32 keys a wave, on the 16x16x32 MFMA. Accumulators and resident rows take
 // half the registers, so that two waves share a SIMD where 32 keys leave room
 // for one; a streamed operand serves half the MFMA work, so that LDS delivers
-// twice as much (47 and 51% of its cycles at d 64/128 and 128/128). One wave per SIMD issued its
+// twice as much (47 and 50% of its cycles at d 64/128 and 128/128). One wave per SIMD issued its
 // vector instructions and its MFMAs nearly one after the other (MFMAs busy
-// 31 to 32% of the cycles, 38 and 43 now). dK dV with 32 and 16 keys a wave, us: 8 heads x
+// 31 to 32% of the cycles, 37 and 43 now). dK dV with 32 and 16 keys a wave, us: 8 heads x
 // 6007, d 128/128, 629 and 511; 32 heads x 4096 causal, 64/128, 364 and 342; 16 heads x
 // 4096, 128/64, 398 and 357, 96/96, 359 and 339; 4 x 12 heads x 1021 ragged, 96/160, 112 and
 // 97. Where 32 keys leave room for two waves as well, they are ahead: 64/64, 226 and
