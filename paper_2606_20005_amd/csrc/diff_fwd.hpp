@@ -305,7 +305,7 @@ diff_fwd_kernel(const DiffArgs a) {
     const float f = l[x] > 0.f || l[x] != l[x] ? 1.f / l[x] : 0.f;   // 0 for rows that see nothing
     const float lam = in ? a.lam[row[x].h] : 0.f;
     if (lse && half == 0 && in)
-      lse[out_row(x)] = !ok || m[x] == kNegInf ? kNegInf : diff_lse(l[x], -nu[x]);
+      lse[out_row(x)] = !ok || l[x] == 0.f ? kNegInf : diff_lse(l[x], -nu[x]);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       // the wave of map 2 hands its block to the wave of map 1, lane by lane

@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kThreads) diff_merge_few_kernel(const DiffArgs
   if (lane < 2) {
     float* lse = lane ? a.lse2 : a.lse1;
     const float t = lane ? top[1] : top[0], l = lane ? sum[1] : sum[0];
-    if (lse) lse[row] = !ok || t == kNegInf ? kNegInf : diff_lse(l, t);
+    if (lse) lse[row] = !ok || l == 0.f ? kNegInf : diff_lse(l, t);
   }
 }
 
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kThreads) diff_merge_kernel(const DiffArgs a) 
   }
   if (tid < 2) {
     float* lse = tid ? a.lse2 : a.lse1;
-    if (lse) lse[row] = !ok || top[tid] == kNegInf ? kNegInf : diff_lse(total[tid], top[tid]);
+    if (lse) lse[row] = !ok || total[tid] == 0.f ? kNegInf : diff_lse(total[tid], top[tid]);
   }
 }
 

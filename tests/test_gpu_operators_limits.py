@@ -100,3 +100,20 @@ def test_values_up_to_2_40_above_a_reference_that_stays(gpu_lib, splits):
     small = 2.0 ** -16 * v.double().abs().mean()
     assert ((out2.double() - mean).abs() <= 2.0 ** -7 * mean.abs() + small).all()
     assert ((lse1.double() - (top + math.log(float(w.sum())))).abs() <= 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("splits,NQ", [(1, 70), (3, 70), (3, 2100)])
+def test_log_sum_exp_of_a_row_that_is_not_a_number(gpu_lib, splits, NQ):
+    """NaN, not the -inf of a row that sees no key."""
+    args, _ = make(1, 1, 1, NQ, 200, 64, 64)
+    kv_len = torch.tensor([150], dtype=torch.int32, device="cuda")
+    args[0][0, 0, 40] = float("nan")
+    args[2][0, 0, 41] = float("nan")
+    q_len = torch.tensor([45], dtype=torch.int32, device="cuda")
+    _, _, lse1, lse2 = gpu_lib.diff_fwd(*args, None, False, q_len, kv_len, splits=splits, save=True)
+    for lse, i in ((lse1, 40), (lse2, 41)):
+        assert torch.isnan(lse[0, 0, i]) and torch.isneginf(lse[0, 0, 45:]).all()
+        assert int(torch.isfinite(lse).sum()) == 44
+    q_len.fill_(NQ)
+    kv_len.fill_(0)
+    assert all(torch.isneginf(x).all() for x in gpu_lib.diff_fwd(*args, None, False, q_len, kv_len, splits=splits, save=True)[2:])
