@@ -686,8 +686,8 @@ def qk_norm_rope(q, k, wq=None, wk=None, table=None, *, eps=1e-6, q_positions=No
     as everywhere in this library. A side's default does not follow positions that are given for the other: with
     k_positions alone, queries still stand at N_K - N_Q .. N_K - 1. Places by default have to be in the table; a
     position given that is outside it gives NaN in the rotated columns, and no gradient where the loss does not reach
-    the row (padding). interleaved: pairs (2j, 2j + 1) instead of (j, j + rot_dim/2). expand_k: write every key head once per query head of its group, so that yk has H heads (the
-    gradients of the copies are added).
+    the row (padding). interleaved: pairs (2j, 2j + 1) instead of (j, j + rot_dim/2). expand_k: write every key head
+    once per query head of its group, so that yk has H heads (the gradients of the copies are added).
     """
     if _differentiated(q, k, wq, wk, table):
         if table is not None and table.requires_grad and torch.is_grad_enabled():
