@@ -504,6 +504,138 @@ int streamkl_diff_bwd(const streamkl_rows* q1, const streamkl_rows* k1, const st
    axis into ranges to fill the chip); 0 for invalid or unsupported extents. */
 size_t streamkl_diff_bwd_workspace_bytes(int B, int H, int HK, int N_Q, int N_K, int d, int dv, int causal);
 
+/*
+ * Operators on rows of logits
+ * ---------------------------
+ * What a distillation program does at the output of its models: the log
+ * probabilities, entropies and best tokens of a distribution over a vocabulary
+ * (streamkl_token_logprobs_*), and the divergence of a student's distribution
+ * from a teacher's best tokens (streamkl_topk_distill_*). The conventions above
+ * hold. All of these calls launch kernels only and record into a HIP graph;
+ * their results are reproducible bit for bit.
+ *
+ * B N rows of V logits: row n of sequence b begins at data + b sb + n sn (in
+ * elements) and is contiguous. data is aligned to its element type, the strides
+ * are >= 0 (rows of an odd vocabulary, a slice of a padded vocabulary, all
+ * positions but the last). The struct lies in host memory and is read before
+ * the call returns. V is at most 2^22 and B N at most 2^31 - 2^16, else
+ * STREAMKL_ERR_UNSUPPORTED.
+ *
+ * A logit of -inf has probability 0. A row of nothing else is empty: its
+ * log-sum-exp is -inf, its entropy, divergence and gradients are 0, its log
+ * probabilities -inf. Logits times scale have to stay finite in float32 where
+ * the logits are. A NaN or +inf spoils the results of its row (they are NaN; top
+ * ids are distinct, and -1 where no logit is left) and of no other.
+ */
+typedef struct {
+  const void* data;
+  long long sb, sn;
+  int B, N, V;
+  int dtype;          /* streamkl_dtype */
+} streamkl_logits;
+
+/*
+ * Log probabilities of given tokens, entropies and top alternatives. With
+ * z = scale x, lse = log sum_j exp z_j:
+ *   tokens    int32 (tokens64 = 0) or int64 (1), contiguous [B, N]; NULL: none.
+ *             A negative token is none (padding): logp = 0. One >= V gives NaN.
+ *   scale     2^-64 to 2^64 (an inverse temperature).
+ *   top       0 to 128, at most V: the `top` largest logits of each row in
+ *             descending order, the lowest index first among equal ones.
+ *   workspace device memory, 16-byte aligned, at least
+ *             streamkl_token_logprobs_workspace_bytes bytes (0 where the rows
+ *             fill the chip); contents ignored on entry, unspecified on return.
+ *             Calls that may overlap need one each, and so do captured graphs
+ *             whose replays may overlap.
+ *   logp      float32 [B, N]: z_tok - lse. NULL where tokens is.
+ *   entropy   float32 [B, N]: -sum_j p_j log p_j, p = exp(z - lse). NULL: not wanted.
+ *   lse       float32 [B, N]; lse_err: what its rounding left off, which keeps
+ *             the probabilities of a backward pass exact. Each may be NULL.
+ *   top_logp, top_ids  float32, int32 [B, N, top].
+ * Not all outputs may be NULL. Sums are float32, joined and finished in 64 bits.
+ */
+int streamkl_token_logprobs_fwd(const streamkl_logits* x, const void* tokens, int tokens64, float scale, int top,
+                                void* workspace, size_t workspace_bytes, float* logp, float* entropy, float* lse,
+                                float* lse_err, float* top_logp, int* top_ids, hipStream_t stream);
+
+/* Workspace bytes of streamkl_token_logprobs_fwd; 0 for invalid arguments too. */
+size_t streamkl_token_logprobs_workspace_bytes(int B, int N, int V, int dtype, int top);
+
+/*
+ * Gradients of logp, entropy and lse (top_logp has none):
+ *     dx_j = scale (dlogp ((j == tok) - p_j) + dlse p_j - dentropy p_j (log p_j + entropy)).
+ *   lse, lse_err, entropy  of the forward call (lse_err may be NULL: probabilities are then off by up to 2^-24 |lse| of
+ *             themselves; entropy is read only with dentropy).
+ *   dlogp, dentropy, dlse  float32 [B, N], each may be NULL (zero). dlogp of rows without a token is not read.
+ *   dx        rows of the element type of x at dx + b dx_sb + n dx_sn that do not overlap, each value rounded once. It may be
+ *             x itself, with its strides. Rows whose upstream gradients are all 0 get zeros, whatever x holds.
+ */
+int streamkl_token_logprobs_bwd(const streamkl_logits* x, const void* tokens, int tokens64, float scale, const float* lse,
+                                const float* lse_err, const float* entropy, const float* dlogp, const float* dentropy,
+                                const float* dlse, void* dx, long long dx_sb, long long dx_sn, hipStream_t stream);
+
+/*
+ * A teacher's best tokens, K of each row.
+ *   ids       int32 (ids64 = 0) or int64 (1), contiguous [B, N, K]. A negative id is no entry (lists of unequal length); one
+ *             >= V makes the row's results NaN.
+ *   values    contiguous [B, N, K] of type dtype. With rest = 1 natural log probabilities; with rest = 0 logits or log
+ *             probabilities, of which p = softmax(scale values) over the list is taken.
+ *   K         1 to 128, else STREAMKL_ERR_UNSUPPORTED.
+ *   rest      1: what the teacher holds outside the list is a bucket of its own (see below); scale has to be 1 then, the rest
+ *             of a distribution at another temperature is not known. 0: the list is all the teacher has.
+ */
+typedef struct {
+  const void* ids;
+  const void* values;
+  int K, ids64, dtype, rest;
+  float scale;
+} streamkl_teacher_list;
+
+/*
+ * Divergence of a student from a teacher's best tokens, per row. z = scale x, q_j = exp(z_j - lse) over all V tokens.
+ *   rest = 1: with p_k = exp(values_k), p_r = max(1 - sum_k p_k, 2^-24) (less is the rounding of the values) and q_r the
+ *             mass of all tokens that are not listed,
+ *                 STREAMKL_KL_FWD  L = sum_k p_k (log p_k - log q_k) + p_r (log p_r - log q_r)
+ *                 STREAMKL_KL_REV  L = sum_k q_k (log q_k - log p_k) + q_r (log q_r - log p_r).
+ *             q_r is summed over the tokens outside the list, not formed as 1 - sum q_k. Where nothing is outside (or only
+ *             logits of -inf), that bucket is left out. A token that is listed twice counts with both entries.
+ *   rest = 0: L = sum_k p_k (log p_k - log q_k), STREAMKL_KL_FWD only (STREAMKL_KL_REV: STREAMKL_ERR_UNSUPPORTED).
+ * A row without entries, and an empty row, has L = 0 and zero gradients. A listed token of probability 0 gives L = +inf, as
+ * the definition does (REV: a value of -inf does).
+ *   workspace as above, at least streamkl_topk_distill_workspace_bytes bytes.
+ *   loss      float32 [B, N].
+ *   stats     32 bytes a row, 8-byte aligned: what the backward pass reads.
+ */
+int streamkl_topk_distill_fwd(const streamkl_logits* x, const streamkl_teacher_list* teacher, float scale, int direction,
+                              void* workspace, size_t workspace_bytes, float* loss, void* stats, hipStream_t stream);
+
+/* Workspace bytes of streamkl_topk_distill_fwd and _step; 0 for invalid arguments too. */
+size_t streamkl_topk_distill_workspace_bytes(int B, int N, int V, int dtype, int rest);
+
+/*
+ * Gradient of sum over rows of g L with respect to x, g = dloss[row] factor dfactor[0].
+ *   dloss     float32 [B, N], or NULL: 1. dfactor: float32 [1] on the device, or NULL: 1.
+ *   done_if_one  1: dx already holds the gradient for dfactor[0] = 1 (streamkl_topk_distill_step wrote it), and is left as it
+ *             is where dfactor[0] is 1.
+ *   dx        as for streamkl_token_logprobs_bwd. Rows with g = 0 get zeros, whatever x holds.
+ */
+int streamkl_topk_distill_bwd(const streamkl_logits* x, const streamkl_teacher_list* teacher, float scale, int direction,
+                              const void* stats, const float* dloss, float factor, const float* dfactor, int done_if_one,
+                              void* dx, long long dx_sb, long long dx_sn, hipStream_t stream);
+
+/*
+ * Both in one: loss and stats of every row and the gradient of sum over rows of weight[row] factor L, for weights that are
+ * known beforehand (weight NULL: 1). Arguments as above.
+ */
+int streamkl_topk_distill_step(const streamkl_logits* x, const streamkl_teacher_list* teacher, float scale, int direction,
+                               void* workspace, size_t workspace_bytes, const float* weight, float factor, float* loss,
+                               void* stats, void* dx, long long dx_sb, long long dx_sn, hipStream_t stream);
+
+/* total[0] = factor sum over rows of weight[row] loss[row] (weight NULL: 1), in 64 bits, in a fixed order. Rows of weight 0
+   are left out, whatever their loss. */
+int streamkl_topk_distill_total(const float* loss, const float* weight, float factor, long long rows, float* total,
+                                hipStream_t stream);
+
 /* Static description of a status code. Never NULL. */
 const char* streamkl_strerror(int status);
 

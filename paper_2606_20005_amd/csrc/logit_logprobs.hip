@@ -1,0 +1,506 @@
+// Log probabilities of given tokens, entropies and top alternatives of rows of
+// logits (streamkl_token_logprobs_fwd, streamkl_token_logprobs_bwd).
+//
+// With z = s x one row, lse = log sum exp z and p = exp(z - lse),
+//   logp = z_tok - lse,   H = -sum p log p,   and the `top` largest z - lse.
+// Backward, for upstream gradients g (logp), h (H) and e (lse):
+//   dx_j = s [ g (j == tok) + p_j (e - g - h (log p_j + H)) ].
+//
+// Bound: HBM. A logit is read once (twice with a backward pass, and its
+// gradient written) with about 10 vector operations, 4 of the issue slots in
+// the exponential. A workgroup takes a row, or a part of one where rows are
+// few; the parts are joined by a second kernel.
+//
+// Alternatives. While a row streams by, the maximum of every 16 consecutive
+// logits (a group) goes to LDS and every thread keeps its own. The `top`-th
+// largest of 256 maxima over disjoint sets of logits is a bound that at least
+// `top` logits reach, and few more do; it is found by bisection in one wave.
+// Only the groups that reach it are read again, their logits that reach it are
+// ranked by counting, each against all. All of it is compared as keys of value
+// and place, so that equal logits rank by place and the outcome does not
+// depend on the order of arrival. Where too many groups reach the bound (rows
+// of equal logits), the `top` groups with the largest keys are found by
+// bisection over all groups instead: the alternatives lie in them, since each
+// group that a logit's own group ranks behind holds a logit that ranks before
+// it.
+#include "logit_rows.hpp"
+#include "streamkl.h"
+
+namespace streamkl {
+namespace {
+
+constexpr int kUnroll = 4;
+constexpr int kGroup = 16;                         // logits of a group
+constexpr int kMostGroups = 8448;                  // of a part: 135168 logits
+constexpr int kMostHits = 512, kMostCands = 2048;  // kMostTop groups hold at most kMostCands logits
+static_assert(kMostTop * kGroup <= kMostCands && kMostTop <= kMostHits, "");
+
+// The order of logits as numbers: larger for larger values, -0 as 0, 0 for a NaN.
+__device__ __forceinline__ u32 key_of(float x) {
+  const u32 b = __builtin_bit_cast(u32, x + 0.f);
+  return x != x ? 0u : b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(u32 k) {
+  return __builtin_bit_cast(float, k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
+}
+// Value, then place: a larger one ranks first.
+__device__ __forceinline__ u64 rank_key(u32 key, u32 place) { return ((u64)key << 32) | (u32)~place; }
+
+struct TopShared {
+  float group[kMostGroups];
+  u64 cand[kMostCands];
+  int hit[kMostHits];
+  u32 most[512];     // keys of the threads' maxima
+  int hits, cands, count[2];
+  u32 bound;
+};
+
+// The largest t with at least `top` of 256 keys >= t (or one that up to top / 8 more reach), by one wave. `most` holds
+// 512 keys or, padded with zeros, fewer.
+__device__ __forceinline__ u32 bound_of(const u32* most, int top) {
+  const int lane = threadIdx.x;
+  u32 k[4], lo = 0xffffffffu, hi = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u32 a = most[64 * i + lane], b = most[256 + 64 * i + lane];
+    k[i] = a > b ? a : b;
+    lo = k[i] < lo ? k[i] : lo;
+    hi = k[i] > hi ? k[i] : hi;
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const u32 l = (u32)__shfl_xor((int)lo, m), h = (u32)__shfl_xor((int)hi, m);
+    lo = l < lo ? l : lo;
+    hi = h > hi ? h : hi;
+  }
+  // all 256 reach lo; kMostTop <= 256
+  while (lo < hi) {
+    const u32 mid = lo + (hi - lo) / 2 + 1;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += __popcll(__ballot(k[i] >= mid));
+    if (n < top) {
+      hi = mid - 1;
+    } else {
+      lo = mid;
+      if (n <= top + top / 8) break;
+    }
+  }
+  return lo;
+}
+
+// How many groups satisfy `pred`, in every thread. All threads call it; `turn` counts the calls.
+template <int THREADS, typename P>
+__device__ int count_groups(TopShared& sh, int groups, int turn, P pred) {
+  int n = 0;
+  for (int b = 0; b < groups; b += THREADS) {
+    const int g = b + threadIdx.x;
+    n += __popcll(__ballot(g < groups && pred(g)));
+  }
+  if (threadIdx.x % 64 == 0) atomicAdd(&sh.count[turn & 1], n);
+  __syncthreads();
+  const int total = sh.count[turn & 1];
+  if (threadIdx.x == 0) sh.count[(turn + 1) & 1] = 0;
+  __syncthreads();
+  return total;
+}
+
+// The candidates of a part: keys of all its logits that can be among the `top` first, in sh.cand (sh.cands of them), the
+// first `top` among them for sure. group0 is the first group of the part.
+template <typename T, int THREADS>
+__device__ void find_candidates(TopShared& sh, const Row<T>& row, int group0, int groups, int top) {
+  const int tid = threadIdx.x;
+  __syncthreads();   // group maxima and thread maxima are written
+  if (tid < 64) {
+    const u32 t = bound_of(sh.most, top);
+    if (tid == 0) {
+      sh.bound = t ? t : 1u;   // 0 is for no logit
+      sh.hits = sh.cands = 0;
+      sh.count[0] = sh.count[1] = 0;
+    }
+  }
+  __syncthreads();
+  auto gather = [&](u32 bound, auto pred) {
+    for (int g = tid; g < groups; g += THREADS) {
+      if (pred(g, key_of(sh.group[g]))) {
+        const int at = atomicAdd(&sh.hits, 1);
+        if (at < kMostHits) sh.hit[at] = g;
+      }
+    }
+    __syncthreads();
+    const int hits = sh.hits;
+    if (hits <= kMostHits) {
+      for (int i = tid; i < hits * kGroup; i += THREADS) {
+        const int j = (group0 + sh.hit[i / kGroup]) * kGroup + i % kGroup - row.ph;
+        if (j >= 0 && j < row.V) {
+          const u32 k = key_of((float)row.row[j]);
+          if (k >= bound) {
+            const int at = atomicAdd(&sh.cands, 1);
+            if (at < kMostCands) sh.cand[at] = rank_key(k, (u32)j);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    return hits <= kMostHits && sh.cands <= kMostCands;
+  };
+  const u32 bound = sh.bound;
+  if (gather(bound, [&](int, u32 k) { return k >= bound; })) return;
+  // too many reach it: the first `top` groups by key, then by place
+  int turn = 0;
+  u32 lo = bound, hi = 0xffffffffu;   // more than `top` groups reach lo
+  while (lo < hi) {
+    const u32 mid = lo + (hi - lo) / 2 + 1;
+    if (count_groups<THREADS>(sh, groups, turn++, [&](int g) { return key_of(sh.group[g]) >= mid; }) < top)
+      hi = mid - 1;
+    else
+      lo = mid;
+  }
+  const u32 v = lo;
+  const int above = count_groups<THREADS>(sh, groups, turn++, [&](int g) { return key_of(sh.group[g]) > v; });
+  int g0 = 0, g1 = groups - 1;        // the last group of key v that is taken
+  while (g0 < g1) {
+    const int mid = g0 + (g1 - g0) / 2;
+    if (count_groups<THREADS>(sh, groups, turn++, [&](int g) { return g <= mid && key_of(sh.group[g]) == v; }) <
+        top - above)
+      g0 = mid + 1;
+    else
+      g1 = mid;
+  }
+  if (tid == 0) sh.hits = sh.cands = 0;
+  __syncthreads();
+  gather(v, [&](int g, u32 k) { return k > v || (k == v && g <= g0); });
+}
+
+// Ranks the candidates: f(rank, key) for the first `top`.
+template <int THREADS, typename F>
+__device__ __forceinline__ void rank_candidates(const TopShared& sh, int top, F f) {
+  const int n = sh.cands < kMostCands ? sh.cands : kMostCands;
+  for (int i = threadIdx.x; i < n; i += THREADS) {
+    const u64 k = sh.cand[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += sh.cand[j] > k;
+    if (rank < top) f(rank, k);
+  }
+}
+
+struct Part {
+  float r, l, a;
+};
+
+// What a row's sums come to. Log probabilities are formed from the distance to the reference: a log-sum-exp near the
+// type's lowest value would swallow them.
+struct RowEnd {
+  double r, log_l, scale;
+  bool empty;
+  __device__ __forceinline__ RowEnd(const Sums& s, float scale_)
+      : r((double)s.r), log_l(log((double)s.l)), scale((double)scale_), empty(s.l == 0.f) {}
+  __device__ __forceinline__ float logp(float x) const {
+    return empty ? kNegInf : (float)(scale * ((double)x - r) - log_l);
+  }
+};
+
+__device__ void finish_row(const LogprobArgs& a, int r, const Sums& sums, const RowEnd& end, const void* x, int dtype) {
+  const double base = end.scale * end.r;   // exact
+  const float lse = end.empty ? kNegInf : (float)(base + end.log_l);
+  if (a.lse) a.lse[r] = lse;
+  if (a.lse_err) a.lse_err[r] = end.empty ? 0.f : (float)((base - (double)lse) + end.log_l);
+  // in units of log 2: log2 l - a / l
+  if (a.entropy)
+    a.entropy[r] = end.empty ? 0.f : (float)(end.log_l - 0.69314718055994530942 * ((double)sums.a / (double)sums.l));
+  if (a.logp) {
+    const long long t = a.tokens64 ? static_cast<const long long*>(a.tokens)[r] : static_cast<const int*>(a.tokens)[r];
+    float v = 0.f;
+    if (t >= a.rows.V)
+      v = __builtin_nanf("");
+    else if (t >= 0)
+      v = end.logp(dtype == STREAMKL_F32   ? static_cast<const float*>(x)[t]
+                   : dtype == STREAMKL_F16 ? (float)static_cast<const _Float16*>(x)[t]
+                                           : (float)static_cast<const __bf16*>(x)[t]);
+    a.logp[r] = v;
+  }
+}
+
+__device__ __forceinline__ void write_top(const LogprobArgs& a, int r, int rank, u64 k, const RowEnd& end) {
+  const long long at = (long long)r * a.top + rank;
+  a.top_ids[at] = (int)~(u32)k;
+  a.top_logp[at] = end.logp(value_of((u32)(k >> 32)));
+}
+
+// Places of a row's list that no logit took (it holds a NaN).
+__device__ __forceinline__ void write_none(const LogprobArgs& a, int r, int rank) {
+  const long long at = (long long)r * a.top + rank;
+  a.top_ids[at] = -1;
+  a.top_logp[at] = __builtin_nanf("");
+}
+
+struct NoShared {};
+
+template <typename T, int THREADS, bool ENTROPY, bool TOP>
+__global__ void __launch_bounds__(THREADS)
+logprob_kernel(LogprobArgs a) {
+  __shared__ float red[3 * THREADS / 64];
+  __shared__ std::conditional_t<TOP, TopShared, NoShared> sh;
+  int r, s;
+  if (!grid_place((long long)a.rows.B * a.rows.N, a.plan.parts, &r, &s)) return;
+  const Row<T> row(a.rows, r);
+  const int c0 = s * a.plan.chunks, c1 = min(row.chunks, c0 + a.plan.chunks), tid = threadIdx.x;
+  const float c = a.scale * kLog2e, rise = kRise / c;
+  Sums sums;
+  float most = kNegInf;
+  each_turn<T, THREADS, kUnroll>(row, c0, c1, [&](int at, const u32x4(&raw)[kUnroll]) {
+    float f[kUnroll][kEpc<T>], mx[kUnroll];
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) {
+      unpack<T>(raw[j], f[j]);
+      mx[j] = max_of<T>(f[j]);
+    }
+    const float mm = vmax(vmax3(mx[0], mx[1], mx[2]), mx[3]);
+    sums.expect(mm, c, rise);
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j)
+#pragma unroll
+      for (int e = 0; e < kEpc<T>; ++e) sums.template add<ENTROPY>(f[j][e], c);
+    if constexpr (TOP) {
+      most = vmax(most, mm);
+      constexpr int CPG = kGroup / kEpc<T>;   // lanes that share a group
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) {
+        float g = vmax(mx[j], quad_swap<kXor1>(mx[j]));
+        if constexpr (CPG == 4) g = vmax(g, quad_swap<kXor2>(g));
+        const int ch = at + j * THREADS;
+        if (ch < c1 && tid % CPG == 0) sh.group[(ch - c0) / CPG] = g;
+      }
+    }
+  });
+  if constexpr (TOP) {
+    for (int i = tid; i < 512; i += THREADS) sh.most[i] = i == tid ? key_of(most) : 0u;
+  }
+  sums = block_join<THREADS>(sums, c, red);
+  const RowEnd end(sums, a.scale);
+  const int top = a.top;
+  if constexpr (TOP) {
+    constexpr int CPG = kGroup / kEpc<T>;
+    find_candidates<T, THREADS>(sh, row, c0 / CPG, (c1 - c0 + CPG - 1) / CPG, top);
+  }
+  if (a.plan.parts == 1) {
+    if (tid == 0) finish_row(a, r, sums, end, row.row, a.rows.dtype);
+    if constexpr (TOP) {
+      for (int i = sh.cands + tid; i < top; i += THREADS) write_none(a, r, i);
+      rank_candidates<THREADS>(sh, top, [&](int rank, u64 k) { write_top(a, r, rank, k, end); });
+    }
+  } else {
+    const long long i = (long long)r * a.plan.parts + s;
+    if (tid == 0) static_cast<Part*>(a.workspace)[i] = Part{sums.r, sums.l, sums.a};
+    if constexpr (TOP) {
+      const long long all = (long long)a.rows.B * a.rows.N * a.plan.parts;
+      u64* keys = reinterpret_cast<u64*>(static_cast<char*>(a.workspace) + (all * sizeof(Part) + 15) / 16 * 16) + i * top;
+      for (int q = sh.cands + tid; q < top; q += THREADS) keys[q] = 0;   // ranks behind any logit
+      rank_candidates<THREADS>(sh, top, [&](int rank, u64 k) { keys[rank] = k; });
+    }
+  }
+}
+
+// Joins the parts of a row: sums by one lane each, alternatives by ranking every key among the sorted lists of all parts.
+constexpr int kJoinThreads = 256;
+
+__global__ void __launch_bounds__(kJoinThreads)
+logprob_join_kernel(LogprobArgs a) {
+  extern __shared__ u64 keys[];   // [parts][top]
+  __shared__ u64 bound;
+  __shared__ float joined[2];
+  int r, s;
+  if (!grid_place((long long)a.rows.B * a.rows.N, 1, &r, &s)) return;
+  const int tid = threadIdx.x, parts = a.plan.parts, top = a.top;
+  const float c = a.scale * kLog2e;
+  if (tid < 64) {
+    Sums sums;
+    if (tid < parts) {
+      const Part p = static_cast<const Part*>(a.workspace)[(long long)r * parts + tid];
+      sums.r = p.r;
+      sums.l = p.l;
+      sums.a = p.a;
+    }
+    sums = wave_join(sums, c);
+    if (tid == 0) {
+      joined[0] = sums.r;
+      joined[1] = sums.l;
+      const int b = r / a.rows.N;
+      const long long at = b * a.rows.sb + (r - b * a.rows.N) * a.rows.sn;
+      const int size = a.rows.dtype == STREAMKL_F32 ? 4 : 2;
+      finish_row(a, r, sums, RowEnd(sums, a.scale), static_cast<const char*>(a.rows.x) + at * size, a.rows.dtype);
+    }
+  }
+  if (top == 0) return;
+  const long long all = (long long)a.rows.B * a.rows.N * parts;
+  const u64* from =
+      reinterpret_cast<const u64*>(static_cast<const char*>(a.workspace) + (all * sizeof(Part) + 15) / 16 * 16) +
+      (long long)r * parts * top;
+  const int n = parts * top;
+  for (int i = tid; i < n; i += kJoinThreads) keys[i] = from[i];
+  for (int i = tid; i < top; i += kJoinThreads) write_none(a, r, i);
+  __syncthreads();
+  if (tid == 0) {
+    // every part has `per` keys at or before its per-th, so that `top` keys rank at or before the last of these
+    const int per = (top + parts - 1) / parts;
+    u64 t = ~0ull;
+    for (int p = 0; p < parts; ++p) t = keys[p * top + per - 1] < t ? keys[p * top + per - 1] : t;
+    bound = t ? t : 1;
+  }
+  __syncthreads();
+  Sums sums;
+  sums.r = joined[0];
+  sums.l = joined[1];
+  const RowEnd end(sums, a.scale);
+  for (int i = tid; i < n; i += kJoinThreads) {
+    const u64 k = keys[i];
+    if (k < bound) continue;
+    int rank = 0;
+    for (int p = 0; p < parts && rank < top; ++p) {
+      int lo = 0, hi = top;   // keys of part p that rank before k
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (keys[p * top + mid] > k)
+          lo = mid + 1;
+        else
+          hi = mid;
+      }
+      rank += lo;
+    }
+    if (rank < top) write_top(a, r, rank, k, end);
+  }
+}
+
+// dx of a part of a row.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+logprob_grad_kernel(LogprobGradArgs a) {
+  int r, s;
+  if (!grid_place((long long)a.rows.B * a.rows.N, a.plan.parts, &r, &s)) return;
+  const Row<T> row(a.rows, r);
+  const int c0 = s * a.plan.chunks, c1 = min(row.chunks, c0 + a.plan.chunks);
+  const int b = r / a.rows.N;
+  T* const dx = static_cast<T*>(a.dx) + b * a.dsb + (r - b * a.rows.N) * a.dsn;
+  long long tok = -1;
+  if (a.tokens)
+    tok = a.tokens64 ? static_cast<const long long*>(a.tokens)[r] : static_cast<const int*>(a.tokens)[r];
+  const float g = a.dlogp && tok >= 0 ? a.dlogp[r] : 0.f;
+  const float h = a.dentropy ? a.dentropy[r] : 0.f, e = a.dlse ? a.dlse[r] : 0.f;
+  const float lse = a.lse[r];
+  float at = 0.f, p1 = 0.f, p2 = 0.f, hit = 0.f;   // dx_j = p_j (p1 + p2 u_j) + (j == tok) hit, p_j = 2^u_j
+  const bool none = (g == 0.f && h == 0.f && e == 0.f) || lse == kNegInf;
+  if (!none) {
+    const Exponent x(lse, a.lse_err ? a.lse_err[r] : 0.f, a.scale);
+    at = x.at;
+    // log p_j = ln 2 u_j + log f
+    const float H = h == 0.f ? 0.f : a.entropy[r];
+    p1 = a.scale * x.f * (e - g - h * (H + logf(x.f)));
+    p2 = -a.scale * x.f * h * kLn2;
+    hit = a.scale * g;
+    if (tok >= row.V) p1 = __builtin_nanf("");
+  }
+  const float c = a.scale * kLog2e;
+  const int tok_at = tok >= 0 && tok < row.V ? (int)tok + row.ph : -1;
+  const int tok_chunk = tok_at >= 0 ? tok_at / kEpc<T> : -1;
+  if (none) {
+    float z[kEpc<T>] = {};
+    for (int ch = c0 + threadIdx.x; ch < c1; ch += THREADS) store<T>(row, dx, ch, z);
+    return;
+  }
+  each_turn<T, THREADS, kUnroll>(row, c0, c1, [&](int first, const u32x4(&raw)[kUnroll]) {
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) {
+      const int ch = first + j * THREADS;
+      float f[kEpc<T>];
+      unpack<T>(raw[j], f);
+#pragma unroll
+      for (int i = 0; i < kEpc<T>; ++i) {
+        float u = (f[i] - at) * c;
+        u = u < kFloor ? kFloor : u;
+        f[i] = exp2_fast(u) * __builtin_fmaf(p2, u, p1);
+      }
+      if (ch == tok_chunk) {
+#pragma unroll
+        for (int i = 0; i < kEpc<T>; ++i) f[i] += i == tok_at % kEpc<T> ? hit : 0.f;
+      }
+      if (ch < c1) store<T>(row, dx, ch, f);
+    }
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------
+
+template <int THREADS, typename T>
+void run_fwd(const LogprobArgs& a, dim3 grid) {
+  if (a.top > 0) {
+    if (a.entropy)
+      logprob_kernel<T, THREADS, true, true><<<grid, dim3(THREADS), 0, a.stream>>>(a);
+    else
+      logprob_kernel<T, THREADS, false, true><<<grid, dim3(THREADS), 0, a.stream>>>(a);
+  } else if (a.entropy) {
+    logprob_kernel<T, THREADS, true, false><<<grid, dim3(THREADS), 0, a.stream>>>(a);
+  } else {
+    logprob_kernel<T, THREADS, false, false><<<grid, dim3(THREADS), 0, a.stream>>>(a);
+  }
+}
+
+}  // namespace
+
+LogitPlan logprob_plan(long long rows, int V, int dtype, int top) {
+  const int epc = dtype == STREAMKL_F32 ? 4 : 8, chunks = chunks_of(V, dtype);
+  // two workgroups a CU where that leaves a part 8192 logits; a part's group maxima have to fit
+  long long parts = rows ? 512 / rows : 1;
+  const long long useful = ((long long)V + 8191) / 8192;
+  if (parts > useful) parts = useful;
+  const long long least = top > 0 ? ((long long)chunks * epc + kMostGroups * kGroup - 1) / (kMostGroups * kGroup) : 1;
+  if (parts < least) parts = least;
+  if (parts < 1) parts = 1;
+  if (parts > kMostParts) parts = kMostParts;
+  LogitPlan p;
+  p.chunks = (int)((chunks + parts - 1) / parts + 3) / 4 * 4;
+  p.parts = (chunks + p.chunks - 1) / p.chunks;
+  p.threads = (long long)p.chunks * epc <= 16384 ? 256 : 512;
+  return p;
+}
+
+size_t logprob_workspace(long long rows, const LogitPlan& p, int top) {
+  if (p.parts <= 1) return 0;
+  const size_t all = (size_t)rows * p.parts;
+  return (all * sizeof(Part) + 15) / 16 * 16 + all * top * sizeof(u64);
+}
+
+hipError_t launch_logprob(const LogprobArgs& a) {
+  const long long rows = (long long)a.rows.B * a.rows.N;
+  const dim3 grid = logit_grid(rows * a.plan.parts);
+  by_type(a.rows.dtype, [&](auto t) {
+    if (a.plan.threads == 256)
+      run_fwd<256, decltype(t)>(a, grid);
+    else
+      run_fwd<512, decltype(t)>(a, grid);
+  });
+  if (a.plan.parts > 1)
+    logprob_join_kernel<<<logit_grid(rows), dim3(kJoinThreads), a.plan.parts * a.top * sizeof(u64), a.stream>>>(a);
+  return hipGetLastError();
+}
+
+LogitPlan logprob_grad_plan(long long rows, int V, int dtype) {
+  const int chunks = chunks_of(V, dtype);
+  const long long parts = ((long long)V + 32767) / 32768;
+  LogitPlan p;
+  p.chunks = (int)((chunks + parts - 1) / parts + 3) / 4 * 4;
+  p.parts = (chunks + p.chunks - 1) / p.chunks;
+  p.threads = 256;
+  return p;
+}
+
+hipError_t launch_logprob_grad(const LogprobGradArgs& a) {
+  const dim3 grid = logit_grid((long long)a.rows.B * a.rows.N * a.plan.parts);
+  by_type(a.rows.dtype, [&](auto t) {
+    logprob_grad_kernel<decltype(t), 256><<<grid, dim3(256), 0, a.stream>>>(a);
+  });
+  return hipGetLastError();
+}
+
+}  // namespace streamkl

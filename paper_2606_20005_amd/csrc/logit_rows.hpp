@@ -1,0 +1,301 @@
+// Rows of logits as the kernels of logit_logprobs.hip and logit_distill.hip
+// read them: 16-byte chunks, the running sums of a softmax, and how a
+// workgroup joins them.
+//
+// A row is V logits x at any element address (rows of an odd vocabulary begin
+// anywhere). It is read in aligned 16-byte chunks of EPC elements: chunk 0 is
+// the one that holds the first element, `ph` places into it. Chunks that lie
+// wholly in the row are loaded as they are, the two that may not be element by
+// element, so that nothing outside the row is read; places outside it hold
+// -inf, which adds nothing to any sum.
+//
+// Sums. With c = s log2(e) in float32, every lane keeps a reference r, one of
+// its logits, and
+//     l = sum 2^((x - r) c),      a = sum 2^((x - r) c) (x - r) c.
+// The sums are exact for any reference, so it is moved only when an exponent
+// passes kRise: terms stay below 2^kRise and a float32 sum of 2^24 of them far
+// from overflow. The difference comes first: it is exact, or nearly so, for
+// the logits that matter, and does not overflow for a row of the type's lowest
+// values (which is uniform). A logit of -inf has the power 0; for a its
+// exponent is taken as kFloor, where the power is 0 as well.
+#pragma once
+
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "kl_common.hpp"
+#include "logit_launch.hpp"
+#include "streamkl.h"
+
+namespace streamkl {
+
+typedef unsigned int u32;
+typedef unsigned long long u64;
+
+constexpr float kRise = 24.f;
+constexpr float kFloor = -1000.f;
+constexpr float kNoRef = -3.402823466e38f;   // reference of a lane that has seen nothing but -inf, or only this value
+
+// v_max_f32, v_max3_f32 without the instructions that quiet signalling NaN (a NaN loses against a number)
+__device__ __forceinline__ float vmax(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ float vmax3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// Lane l receives the value of lane l ^ 1 (kXor1), l ^ 2 (kXor2).
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E;
+template <int CTRL>
+__device__ __forceinline__ float quad_swap(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+
+// Elements of a type and of the chunks it comes in.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<__bf16> {
+  static constexpr u32 kNegInfBits = 0xFF80;
+};
+template <>
+struct Elem<_Float16> {
+  static constexpr u32 kNegInfBits = 0xFC00;
+};
+template <>
+struct Elem<float> {
+  static constexpr u32 kNegInfBits = 0xFF800000;
+};
+template <typename T>
+constexpr int kEpc = 16 / (int)sizeof(T);         // elements of a chunk
+
+template <typename T>
+__device__ __forceinline__ void unpack(const u32x4& raw, float (&f)[kEpc<T>]) {
+  typedef T TN __attribute__((ext_vector_type(kEpc<T>)));
+  const TN t = __builtin_bit_cast(TN, raw);
+#pragma unroll
+  for (int e = 0; e < kEpc<T>; ++e) f[e] = (float)t[e];
+}
+
+template <typename T>
+__device__ __forceinline__ u32x4 pack(const float (&f)[kEpc<T>]) {
+  typedef T TN __attribute__((ext_vector_type(kEpc<T>)));
+  TN t;
+#pragma unroll
+  for (int e = 0; e < kEpc<T>; ++e) t[e] = (T)f[e];
+  return __builtin_bit_cast(u32x4, t);
+}
+
+template <typename T>
+__device__ __forceinline__ float max_of(const float (&f)[kEpc<T>]) {
+  if constexpr (kEpc<T> == 8)
+    return vmax3(vmax3(f[0], f[1], f[2]), vmax3(f[3], f[4], f[5]), vmax(f[6], f[7]));
+  else
+    return vmax(vmax3(f[0], f[1], f[2]), f[3]);
+}
+
+// One row.
+template <typename T>
+struct Row {
+  const T* row;          // its first element
+  const u32x4* chunk;    // the chunk that holds it
+  int V, ph, chunks;     // elements, places of chunk 0 before the first one, chunks that hold elements
+
+  __device__ __forceinline__ Row(const LogitRows& a, int r) {
+    const int b = r / a.N;
+    row = static_cast<const T*>(a.x) + b * a.sb + (r - b * a.N) * a.sn;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row);
+    ph = (int)(at & 15) / (int)sizeof(T);
+    chunk = reinterpret_cast<const u32x4*>(at & ~(uintptr_t)15);
+    V = a.V;
+    chunks = (ph + V + kEpc<T> - 1) / kEpc<T>;
+  }
+  __device__ __forceinline__ bool whole(int c) const { return c * kEpc<T> >= ph && (c + 1) * kEpc<T> <= ph + V; }
+  // chunks c .. c + n - 1 lie wholly in the row
+  __device__ __forceinline__ bool whole(int c, int n) const {
+    return c * kEpc<T> >= ph && (long long)(c + n) * kEpc<T> <= ph + V;
+  }
+  // any chunk, -inf in the places outside the row and from chunk `end` on
+  __device__ __forceinline__ u32x4 load(int c, int end) const {
+    if (c < end && whole(c)) return chunk[c];
+    typedef T TN __attribute__((ext_vector_type(kEpc<T>)));
+    u32x4 raw;
+    const u32 fill = sizeof(T) == 4 ? Elem<T>::kNegInfBits : Elem<T>::kNegInfBits * 0x10001u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = fill;
+    if (c >= end) return raw;
+    TN t = __builtin_bit_cast(TN, raw);
+#pragma unroll
+    for (int e = 0; e < kEpc<T>; ++e) {
+      const int j = c * kEpc<T> + e - ph;
+      if (j >= 0 && j < V) t[e] = row[j];
+    }
+    return __builtin_bit_cast(u32x4, t);
+  }
+};
+
+// Chunks c0 .. c1 - 1 in turns of UNROLL per thread: f(chunk of this thread, raw), the chunks of a turn at once so that
+// their loads are in flight together. All threads take every turn.
+template <typename T, int THREADS, int UNROLL, typename F>
+__device__ __forceinline__ void each_turn(const Row<T>& row, int c0, int c1, F f) {
+  const int tid = threadIdx.x;
+  for (int b = c0; b < c1; b += THREADS * UNROLL) {
+    u32x4 raw[UNROLL];
+    if (b + THREADS * UNROLL <= c1 && row.whole(b, THREADS * UNROLL)) {
+#pragma unroll
+      for (int j = 0; j < UNROLL; ++j) raw[j] = row.chunk[b + j * THREADS + tid];
+    } else {
+#pragma unroll
+      for (int j = 0; j < UNROLL; ++j) raw[j] = row.load(b + j * THREADS + tid, c1);
+    }
+    f(b + tid, raw);
+  }
+}
+
+typedef u32x4 u32x4_any __attribute__((aligned(2)));   // a chunk at the address of any element
+
+// The places of a chunk of `row` in a row of gradients of any alignment (its elements begin at `to`).
+template <typename T>
+__device__ __forceinline__ void store(const Row<T>& row, T* to, int c, const float (&f)[kEpc<T>]) {
+  to += (long long)c * kEpc<T> - row.ph;
+  if (row.whole(c)) {
+    *reinterpret_cast<u32x4_any*>(to) = pack<T>(f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kEpc<T>; ++e) {
+      const int j = c * kEpc<T> + e - row.ph;
+      if (j >= 0 && j < row.V) to[e] = (T)f[e];
+    }
+  }
+}
+
+// Running sums of a lane (or, after joining, of a workgroup).
+struct Sums {
+  float r, l, a;
+
+  __device__ __forceinline__ Sums() : r(kNoRef), l(0.f), a(0.f) {}
+
+  __device__ __forceinline__ void move(float m, float c) {
+    const float d = vmax((r - m) * c, kFloor), w = exp2_fast(d);
+    a = w * __builtin_fmaf(l, d, a);
+    l *= w;
+    r = m;
+  }
+  // The largest logit of some that are to come: the reference is moved to it if it is more than `rise` above.
+  __device__ __forceinline__ void expect(float mx, float c, float rise) {
+    const bool up = mx > r + rise;
+    if (__any(up)) {
+      if (up) move(mx, c);
+    }
+  }
+  template <bool ENTROPY>
+  __device__ __forceinline__ void add(float x, float c) {
+    float u = (x - r) * c;
+    if constexpr (ENTROPY) {
+      u = u < kFloor ? kFloor : u;   // keeps a NaN, which a maximum would drop
+      const float e = exp2_fast(u);
+      l += e;
+      a = __builtin_fmaf(e, u, a);
+    } else {
+      l += exp2_fast(u);
+    }
+  }
+  __device__ __forceinline__ void join(const Sums& o, float c) {
+    const float m = fmaxf(r, o.r);
+    const float d0 = vmax((r - m) * c, kFloor), d1 = vmax((o.r - m) * c, kFloor);
+    const float w0 = exp2_fast(d0), w1 = exp2_fast(d1);
+    a = w0 * __builtin_fmaf(l, d0, a) + w1 * __builtin_fmaf(o.l, d1, o.a);
+    l = w0 * l + w1 * o.l;
+    r = m;
+  }
+};
+
+// The sums of all lanes of a wave, in every lane.
+__device__ __forceinline__ Sums wave_join(Sums s, float c) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    Sums o;
+    o.r = __shfl_xor(s.r, m);
+    o.l = __shfl_xor(s.l, m);
+    o.a = __shfl_xor(s.a, m);
+    s.join(o, c);
+  }
+  return s;
+}
+
+// The sums of a workgroup, in every thread. `red` holds 3 * THREADS / 64 floats and may be written again after the next
+// barrier.
+template <int THREADS>
+__device__ __forceinline__ Sums block_join(Sums s, float c, float* red) {
+  s = wave_join(s, c);
+  if constexpr (THREADS > 64) {
+    constexpr int W = THREADS / 64;
+    const int w = threadIdx.x / 64;
+    if (threadIdx.x % 64 == 0) {
+      red[3 * w] = s.r;
+      red[3 * w + 1] = s.l;
+      red[3 * w + 2] = s.a;
+    }
+    __syncthreads();
+    Sums t;
+    t.r = red[0];
+    t.l = red[1];
+    t.a = red[2];
+    for (int i = 1; i < W; ++i) {
+      Sums o;
+      o.r = red[3 * i];
+      o.l = red[3 * i + 1];
+      o.a = red[3 * i + 2];
+      t.join(o, c);
+    }
+    s = t;
+  }
+  return s;
+}
+
+// exp(s x - lse) = 2^((x - at) c) f: what a log-sum-exp is for a kernel that forms probabilities, given as its float32
+// value and what the rounding left off.
+struct Exponent {
+  float at, f;
+  __device__ __forceinline__ Exponent(float lse, float err, float scale) {
+    at = (float)((double)lse / (double)scale);
+    f = (float)exp(((double)scale * (double)at - (double)lse) - (double)err);   // the product is exact
+  }
+};
+
+// A row of the grid: workgroup i of rows x parts, of which row r and part s.
+__device__ __forceinline__ bool grid_place(long long rows, int parts, int* r, int* s) {
+  const long long i = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+  if (i >= rows * parts) return false;
+  *r = (int)(i / parts);
+  *s = (int)(i - (long long)*r * parts);
+  return true;
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+// The most chunks that a row of any alignment has.
+inline int chunks_of(int V, int dtype) {
+  const int epc = dtype == STREAMKL_F32 ? 4 : 8;
+  return (V + epc - 1 + epc - 1) / epc;
+}
+
+// f(element) with a value of the type
+template <typename F>
+inline void by_type(int dtype, F f) {
+  if (dtype == STREAMKL_F32)
+    f(float{});
+  else if (dtype == STREAMKL_F16)
+    f(_Float16{});
+  else
+    f(__bf16{});
+}
+
+}  // namespace streamkl

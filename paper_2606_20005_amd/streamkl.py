@@ -15,6 +15,12 @@ The operators around it:
     yq, yk = qk_norm_rope(q, k, wq, wk, rope_table(n, rot))           # projections -> normed, rotated, head-major
     loss = attention_kl_proj(q1, k1, q2, k2, QKPrep(...), QKPrep(...), causal=True).mean()
     out = diff_attention(q1, k1, q2, k2, v, lam, causal=True)         # (softmax map 1 - lam * softmax map 2) v
+
+The operators on rows of logits:
+
+    scores = token_logprobs(logits, tokens, top=20)                   # logp, entropy, lse, top_logp, top_ids
+    best = token_logprobs(teacher_logits, top=64)
+    loss = topk_distill_loss(student_logits, best.top_ids, best.top_logp)
 """
 from __future__ import annotations
 
@@ -40,7 +46,10 @@ ENTRY_POINTS = ("streamkl_fwd", "streamkl_bwd", "streamkl_bwd_ex", "streamkl_bwd
                 "streamkl_fwd_act", "streamkl_bwd_act", "streamkl_bwd_grads", "streamkl_strerror", "streamkl_version",
                 "streamkl_supported_head_dim", "streamkl_qk_norm_rope_fwd", "streamkl_qk_norm_rope_bwd",
                 "streamkl_qk_norm_rope_bwd_workspace_bytes", "streamkl_diff_fwd", "streamkl_diff_fwd_split_count",
-                "streamkl_diff_fwd_workspace_bytes", "streamkl_diff_bwd", "streamkl_diff_bwd_workspace_bytes")
+                "streamkl_diff_fwd_workspace_bytes", "streamkl_diff_bwd", "streamkl_diff_bwd_workspace_bytes",
+                "streamkl_token_logprobs_fwd", "streamkl_token_logprobs_workspace_bytes", "streamkl_token_logprobs_bwd",
+                "streamkl_topk_distill_fwd", "streamkl_topk_distill_workspace_bytes", "streamkl_topk_distill_bwd",
+                "streamkl_topk_distill_step", "streamkl_topk_distill_total")
 _MAX_INT = 0x7fffffff   # the ABI's extents; ctypes would cut a larger one silently
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
@@ -49,6 +58,18 @@ class _Rows(ctypes.Structure):
     """streamkl_rows: a [batch, head, row] arrangement of contiguous rows."""
     _fields_ = [("data", ctypes.c_void_p), ("sb", ctypes.c_longlong), ("sh", ctypes.c_longlong),
                 ("sn", ctypes.c_longlong)]
+
+
+class _Logits(ctypes.Structure):
+    """streamkl_logits: B N rows of V logits."""
+    _fields_ = [("data", ctypes.c_void_p), ("sb", ctypes.c_longlong), ("sn", ctypes.c_longlong), ("B", ctypes.c_int),
+                ("N", ctypes.c_int), ("V", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class _TeacherList(ctypes.Structure):
+    """streamkl_teacher_list: a teacher's best tokens."""
+    _fields_ = [("ids", ctypes.c_void_p), ("values", ctypes.c_void_p), ("K", ctypes.c_int), ("ids64", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("rest", ctypes.c_int), ("scale", ctypes.c_float)]
 
 
 def _load():
@@ -104,6 +125,23 @@ def _load():
     lib.streamkl_diff_bwd.restype = i
     lib.streamkl_diff_bwd_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
     lib.streamkl_diff_bwd_workspace_bytes.restype = sz
+    logits, teacher, ll = ctypes.POINTER(_Logits), ctypes.POINTER(_TeacherList), ctypes.c_longlong
+    lib.streamkl_token_logprobs_fwd.argtypes = [logits, vp, i, f, i, vp, sz, vp, vp, vp, vp, vp, vp, vp]
+    lib.streamkl_token_logprobs_fwd.restype = i
+    lib.streamkl_token_logprobs_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.streamkl_token_logprobs_workspace_bytes.restype = sz
+    lib.streamkl_token_logprobs_bwd.argtypes = [logits, vp, i, f, vp, vp, vp, vp, vp, vp, vp, ll, ll, vp]
+    lib.streamkl_token_logprobs_bwd.restype = i
+    lib.streamkl_topk_distill_fwd.argtypes = [logits, teacher, f, i, vp, sz, vp, vp, vp]
+    lib.streamkl_topk_distill_fwd.restype = i
+    lib.streamkl_topk_distill_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.streamkl_topk_distill_workspace_bytes.restype = sz
+    lib.streamkl_topk_distill_bwd.argtypes = [logits, teacher, f, i, vp, vp, f, vp, i, vp, ll, ll, vp]
+    lib.streamkl_topk_distill_bwd.restype = i
+    lib.streamkl_topk_distill_step.argtypes = [logits, teacher, f, i, vp, sz, vp, f, vp, vp, vp, ll, ll, vp]
+    lib.streamkl_topk_distill_step.restype = i
+    lib.streamkl_topk_distill_total.argtypes = [vp, vp, f, ll, vp, vp]
+    lib.streamkl_topk_distill_total.restype = i
     lib.streamkl_strerror.argtypes = [i]
     lib.streamkl_strerror.restype = ctypes.c_char_p
     lib.streamkl_version.argtypes = []
@@ -894,3 +932,353 @@ def diff_attention(q1, k1, q2, k2, v, lam, *, scale=None, causal=False, q_len=No
     if _differentiated(q1, k1, q2, k2, v, lam):
         return _DiffAttention.apply(q1, k1, q2, k2, v, lam, scale, bool(causal), q_len, kv_len)
     return diff_fwd(q1, k1, q2, k2, v, lam, scale, causal, q_len, kv_len)
+
+
+# --- rows of logits: log probabilities, entropies, best tokens --------------------------------------------------------
+
+
+class TokenLogprobs(typing.NamedTuple):
+    """What token_logprobs returns; None where not asked for."""
+    logp: torch.Tensor | None
+    entropy: torch.Tensor | None
+    lse: torch.Tensor
+    top_logp: torch.Tensor | None
+    top_ids: torch.Tensor | None
+
+
+def _logit_error(t, name):
+    """What is wrong with a tensor of logits."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        return ValueError(f"{name} must be a GPU tensor")
+    if t.dtype not in DTYPES:
+        return ValueError(f"{name} must be bfloat16, float16 or float32, got {t.dtype}")
+    if t.dim() not in (2, 3):
+        return ValueError(f"{name} must be a [N, V] or [B, N, V] tensor, got {tuple(t.shape)}")
+    return ValueError(f"{name} must be contiguous along its last axis")
+
+
+def _logits(t, name="logits"):
+    """A tensor of logits as a streamkl_logits: (device, shape of its rows, V, streamkl_logits)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in DTYPES and t.dim() in (2, 3)):
+        raise _logit_error(t, name)
+    shape, st = t.shape, t.stride()
+    V = shape[-1]
+    if st[-1] != 1 and V != 1:
+        raise _logit_error(t, name)
+    B, N = (1, shape[0]) if len(shape) == 2 else shape[:2]
+    if B > _MAX_INT or N > _MAX_INT or V > _MAX_INT:
+        raise ValueError("an extent does not fit 31 bits")
+    # the stride of an extent of one says nothing
+    sb = st[0] if len(shape) == 3 and B > 1 else 0
+    return t.device, shape[:-1], V, _Logits(t.data_ptr(), sb, st[-2] if N > 1 else 0, B, N, V, DTYPES[t.dtype])
+
+
+def _ints(t, shape, dev, name):
+    if not (isinstance(t, torch.Tensor) and t.dtype in (torch.int32, torch.int64) and t.shape == shape and
+            t.is_contiguous() and t.device == dev):
+        raise ValueError(f"{name} must be a contiguous int32 or int64 tensor of shape {tuple(shape)} on {dev}")
+    return int(t.dtype is torch.int64)
+
+
+def _row_floats(t, shape, dev, name):
+    if t is not None and not (isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.shape == shape and
+                              t.is_contiguous() and t.device == dev):
+        raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on {dev}")
+    return t
+
+
+def _grad_rows(out, logits):
+    """A tensor for the gradient of the logits, new or the caller's: (tensor, strides between sequences and rows)."""
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    elif not (isinstance(out, torch.Tensor) and out.dtype == logits.dtype and out.shape == logits.shape and
+              out.device == logits.device):
+        raise ValueError(f"out must be a {logits.dtype} tensor of shape {tuple(logits.shape)} on {logits.device}")
+    _, _, _, rows = _logits(out, "out")
+    return out, rows.sb, rows.sn
+
+
+def token_logprobs_workspace_bytes(B, N, V, dtype, top=0) -> int:
+    """streamkl_token_logprobs_workspace_bytes."""
+    return int(lib.streamkl_token_logprobs_workspace_bytes(int(B), int(N), int(V), DTYPES[dtype], int(top)))
+
+
+def token_logprobs_fwd(logits, tokens=None, scale=1.0, top=0, entropy=True, save=False, workspace=None):
+    """streamkl_token_logprobs_fwd: TokenLogprobs, with ``save`` also lse_err, which token_logprobs_bwd takes. See
+    token_logprobs. The workspace (16-byte aligned) is allocated here unless given."""
+    dev, shape, V, rows = _logits(logits)
+    tokens64 = 0 if tokens is None else _ints(tokens, shape, dev, "tokens")
+    top = int(top)
+    if not 0 <= top <= V:
+        raise ValueError(f"top must be 0 to the vocabulary's {V}, got {top}")
+    row = lambda dtype=torch.float32, last=(): torch.empty((*shape, *last), dtype=dtype, device=dev)   # noqa: E731
+    lse = row()
+    logp, ent, err = (row() if want else None for want in (tokens is not None, entropy, save))
+    top_logp, top_ids = (row(last=(top,)), row(torch.int32, (top,))) if top else (None, None)
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = _workspace(workspace, dev)
+    elif top <= 128:
+        ws_bytes = lib.streamkl_token_logprobs_workspace_bytes(rows.B, rows.N, V, rows.dtype, top)
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    with _on(dev):
+        st = lib.streamkl_token_logprobs_fwd(rows, _p(tokens), tokens64, float(scale), top, _p(workspace), ws_bytes,
+                                             _p(logp), _p(ent), _p(lse), _p(err), _p(top_logp), _p(top_ids), _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_token_logprobs_fwd")
+    y = TokenLogprobs(logp, ent, lse, top_logp, top_ids)
+    return (y, err) if save else y
+
+
+def token_logprobs_bwd(logits, tokens, lse, lse_err=None, entropy=None, dlogp=None, dentropy=None, dlse=None, scale=1.0,
+                       out=None):
+    """streamkl_token_logprobs_bwd: the gradient of the logits, in their type. lse, lse_err and entropy are those of
+    token_logprobs_fwd(..., save=True). ``out`` may be a tensor of the logits' shape and type with rows that do not
+    overlap, the logits themselves among them."""
+    dev, shape, _, rows = _logits(logits)
+    tokens64 = 0 if tokens is None else _ints(tokens, shape, dev, "tokens")
+    if lse is None:
+        raise ValueError("lse is missing")
+    args = [_p(_row_floats(t, shape, dev, n)) for n, t in
+            (("lse", lse), ("lse_err", lse_err), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy),
+             ("dlse", dlse))]
+    if dlogp is not None and tokens is None:
+        raise ValueError("dlogp given without tokens")
+    if dentropy is not None and entropy is None:
+        raise ValueError("dentropy given without entropy")
+    out, sb, sn = _grad_rows(out, logits)
+    with _on(dev):
+        st = lib.streamkl_token_logprobs_bwd(rows, _p(tokens), tokens64, float(scale), *args, _p(out), sb, sn,
+                                             _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_token_logprobs_bwd")
+    return out
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, scale, top, entropy):
+        y, err = token_logprobs_fwd(logits, tokens, scale, top, entropy, save=True)
+        ctx.save_for_backward(logits, tokens, y.lse, err, y.entropy)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        if top:
+            ctx.mark_non_differentiable(y.top_logp, y.top_ids)
+        return tuple(y)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogp, dentropy, dlse, _top, _ids):
+        logits, tokens, lse, err, entropy = ctx.saved_tensors
+        up = [None if g is None else g.to(torch.float32).contiguous() for g in (dlogp, dentropy, dlse)]
+        if all(g is None for g in up):
+            return (None,) * 5
+        return (token_logprobs_bwd(logits, tokens, lse, err, entropy, *up, ctx.scale), None, None, None, None)
+
+
+def token_logprobs(logits, tokens=None, *, scale=1.0, top=0, entropy=True):
+    """Log probabilities of given tokens under softmax(scale logits), with entropies and the best tokens; differentiable.
+
+    logits [N, V] or [B, N, V] in bfloat16, float16 or float32, rows anywhere in memory (a vocabulary of any size, a slice
+    of a padded one, logits[:, :-1]). tokens: int32 or int64 [N] or [B, N], or None; a negative token is none (padding)
+    and has logp 0, one outside the vocabulary NaN. scale: an inverse temperature. top: 0 to 128.
+
+    Returns TokenLogprobs: logp, entropy (nats; None unless ``entropy``) and lse = log sum exp(scale logits), float32 of
+    the tokens' shape; top_logp (float32) and top_ids (int32) [..., top], descending, the lowest index first among equal
+    logits. Gradients flow through logp, entropy and lse in the logits' type. Logits of -inf have probability 0; a row
+    of nothing else has lse -inf, entropy 0 and no gradient.
+    """
+    if _differentiated(logits):
+        return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, float(scale), int(top), bool(entropy)))
+    return token_logprobs_fwd(logits, tokens, scale, top, entropy)
+
+
+# --- distillation from a teacher's best tokens ------------------------------------------------------------------------
+
+
+def _distill_inputs(logits, ids, teacher, s1, s2, rest, direction):
+    """Checked arguments of the distillation calls: (device, shape of the rows, arguments that all calls begin with)."""
+    dev, shape, V, rows = _logits(logits)
+    if not (isinstance(ids, torch.Tensor) and ids.dim() == logits.dim()):
+        raise ValueError(f"ids must be a tensor of shape {(*shape, 'K')}")
+    lists = (*shape, ids.shape[-1])
+    ids64 = _ints(ids, lists, dev, "ids")
+    if not (isinstance(teacher, torch.Tensor) and teacher.dtype in DTYPES and teacher.shape == lists and
+            teacher.is_contiguous() and teacher.device == dev):
+        raise ValueError(f"teacher must be a contiguous bfloat16, float16 or float32 tensor of shape {lists} on {dev}")
+    d = _direction(direction)
+    if rest and s1 != 1.0:
+        raise ValueError("s1 must be 1 with a rest: that of a distribution at another temperature is not known")
+    if d == REV and not rest:
+        raise ValueError("the reverse direction needs a rest: a student's tokens outside the list have no teacher")
+    listed = _TeacherList(ids.data_ptr(), teacher.data_ptr(), lists[-1], ids64, DTYPES[teacher.dtype], int(bool(rest)),
+                          float(s1))
+    return dev, shape, (rows, listed, float(s2), d)
+
+
+def topk_distill_workspace_bytes(B, N, V, dtype, rest=True) -> int:
+    """streamkl_topk_distill_workspace_bytes."""
+    return int(lib.streamkl_topk_distill_workspace_bytes(int(B), int(N), int(V), DTYPES[dtype], int(bool(rest))))
+
+
+def _distill_workspace(workspace, dev, args):
+    if workspace is not None:
+        return workspace, _workspace(workspace, dev)
+    rows, listed = args[:2]
+    n = lib.streamkl_topk_distill_workspace_bytes(rows.B, rows.N, rows.V, rows.dtype, listed.rest)
+    return (torch.empty(n, dtype=torch.uint8, device=dev) if n else None), n
+
+
+def _distill_stats(stats, shape, dev):
+    if not (isinstance(stats, torch.Tensor) and stats.dtype is torch.float64 and stats.shape == (*shape, 4) and
+            stats.is_contiguous() and stats.device == dev):
+        raise ValueError(f"stats must be a contiguous float64 tensor of shape {(*shape, 4)} on {dev}")
+    return stats
+
+
+def topk_distill_fwd(logits, ids, teacher, s1=1.0, s2=1.0, rest=True, direction=FWD, workspace=None):
+    """streamkl_topk_distill_fwd: (loss, stats), float32 of the rows' shape and what topk_distill_bwd needs (float64
+    [..., 4]). See topk_distill. The workspace (16-byte aligned) is allocated here unless given."""
+    dev, shape, args = _distill_inputs(logits, ids, teacher, s1, s2, rest, direction)
+    loss = torch.empty(shape, dtype=torch.float32, device=dev)
+    stats = torch.empty((*shape, 4), dtype=torch.float64, device=dev)
+    workspace, ws_bytes = _distill_workspace(workspace, dev, args)
+    with _on(dev):
+        st = lib.streamkl_topk_distill_fwd(*args, _p(workspace), ws_bytes, _p(loss), _p(stats), _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_topk_distill_fwd")
+    return loss, stats
+
+
+def topk_distill_bwd(logits, ids, teacher, stats, dloss=None, s1=1.0, s2=1.0, rest=True, direction=FWD, factor=1.0,
+                     dfactor=None, done_if_one=False, out=None):
+    """streamkl_topk_distill_bwd: the gradient of the logits, in their type, for the upstream gradients
+    dloss (float32 of the rows' shape, None: ones) times factor times dfactor (a float32 tensor of one element, None: 1).
+    done_if_one: ``out`` already holds it for dfactor 1 (topk_distill_step) and is left alone then. ``out`` may be a
+    tensor of the logits' shape and type with rows that do not overlap, the logits themselves among them."""
+    dev, shape, args = _distill_inputs(logits, ids, teacher, s1, s2, rest, direction)
+    _distill_stats(stats, shape, dev)
+    _row_floats(dloss, shape, dev, "dloss")
+    if dfactor is not None and not (dfactor.dtype is torch.float32 and dfactor.numel() == 1 and dfactor.device == dev):
+        raise ValueError(f"dfactor must be a float32 tensor of one element on {dev}")
+    if done_if_one and (out is None or dfactor is None):
+        raise ValueError("done_if_one needs out and dfactor")
+    out, sb, sn = _grad_rows(out, logits)
+    with _on(dev):
+        st = lib.streamkl_topk_distill_bwd(*args, _p(stats), _p(dloss), float(factor), _p(dfactor),
+                                           int(bool(done_if_one)), _p(out), sb, sn, _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_topk_distill_bwd")
+    return out
+
+
+def topk_distill_step(logits, ids, teacher, weight=None, s1=1.0, s2=1.0, rest=True, direction=FWD, factor=1.0, out=None,
+                      workspace=None):
+    """streamkl_topk_distill_step: (loss, stats, dlogits), the rows' losses with the gradient of
+    sum(weight * factor * loss). weight: float32 of the rows' shape, None: ones. Others as in topk_distill_fwd and
+    topk_distill_bwd."""
+    dev, shape, args = _distill_inputs(logits, ids, teacher, s1, s2, rest, direction)
+    _row_floats(weight, shape, dev, "weight")
+    loss = torch.empty(shape, dtype=torch.float32, device=dev)
+    stats = torch.empty((*shape, 4), dtype=torch.float64, device=dev)
+    workspace, ws_bytes = _distill_workspace(workspace, dev, args)
+    out, sb, sn = _grad_rows(out, logits)
+    with _on(dev):
+        st = lib.streamkl_topk_distill_step(*args, _p(workspace), ws_bytes, _p(weight), float(factor), _p(loss),
+                                            _p(stats), _p(out), sb, sn, _stream(dev))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_topk_distill_step")
+    return loss, stats, out
+
+
+def _distill_total(loss, weight, factor):
+    total = torch.empty((), dtype=torch.float32, device=loss.device)
+    with _on(loss.device):
+        st = lib.streamkl_topk_distill_total(_p(loss), _p(weight), factor, loss.numel(), _p(total), _stream(loss.device))
+    if st != OK:
+        raise StreamKLError(st, "streamkl_topk_distill_total")
+    return total
+
+
+class _TopkDistill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, teacher, opts):
+        loss, stats = topk_distill_fwd(logits, ids, teacher, *opts)
+        ctx.save_for_backward(logits, ids, teacher, stats)
+        ctx.opts = opts
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        logits, ids, teacher, stats = ctx.saved_tensors
+        return (topk_distill_bwd(logits, ids, teacher, stats, dloss.to(torch.float32).contiguous(), *ctx.opts),
+                None, None, None)
+
+
+class _TopkDistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, teacher, weight, factor, opts):
+        loss, stats, grad = topk_distill_step(logits, ids, teacher, weight, *opts, factor)
+        ctx.save_for_backward(logits, ids, teacher, weight, stats)
+        ctx.cfg = (factor, opts)
+        ctx.grad = grad   # for an upstream gradient of 1
+        return _distill_total(loss, weight, factor)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g):
+        logits, ids, teacher, weight, stats = ctx.saved_tensors
+        factor, opts = ctx.cfg
+        # the first backward pass hands the gradient over; a later one through a retained graph forms it again
+        out, ctx.grad = ctx.grad, None
+        return (topk_distill_bwd(logits, ids, teacher, stats, weight, *opts, factor, g.to(torch.float32), out is not None,
+                                 out), None, None, None, None, None)
+
+
+def _no_gradient(**tensors):
+    if torch.is_grad_enabled():
+        for n, t in tensors.items():
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{n} takes no gradient: pass it detached")
+
+
+def topk_distill(logits, ids, teacher, *, s1=1.0, s2=1.0, rest=True, direction="fwd"):
+    """Per-row divergence of a student, softmax(s2 logits) over the vocabulary, from a teacher's best tokens;
+    differentiable in the logits.
+
+    logits [N, V] or [B, N, V] as token_logprobs takes them. ids (int32 or int64) and teacher (float32, bfloat16 or
+    float16) [..., K], K up to 128: the teacher's tokens of every row and their values, such as top_ids and top_logp of
+    token_logprobs. A negative id is no entry: lists may be of unequal length, a row without entries has no loss.
+
+    rest=True: the values are natural log probabilities, and the mass outside the list is one bucket of both
+    distributions. direction "fwd" is KL(teacher || student), "rev" KL(student || teacher), as in attention_kl.
+    rest=False: the list is all the teacher has, softmax(s1 teacher) over it; "fwd" only.
+
+    Returns float32 losses of the rows' shape; the gradient comes in the logits' type. For a weighted sum of the rows
+    topk_distill_loss is faster: it reads the logits once.
+    """
+    opts = (s1, s2, rest, direction)
+    if _differentiated(logits, teacher):
+        _no_gradient(teacher=teacher)
+        return _TopkDistill.apply(logits, ids, teacher, opts)
+    return topk_distill_fwd(logits, ids, teacher, *opts)[0]
+
+
+def topk_distill_loss(logits, ids, teacher, weight=None, *, s1=1.0, s2=1.0, rest=True, direction="fwd"):
+    """sum(weight * topk_distill(logits, ids, teacher, ...)), a scalar; weight float32 of the rows' shape, or None for the
+    mean over all rows. Rows of weight 0 (padding) are left out, whatever they hold.
+
+    The weights are known before the losses, so the gradient is formed with them, in the forward call where the logits
+    require one. The backward pass hands it over; for an upstream gradient other than 1 (a loss scale) it forms the
+    gradient anew, rounded once.
+    """
+    opts = (s1, s2, rest, direction)
+    rows = logits.numel() // logits.shape[-1] if isinstance(logits, torch.Tensor) and logits.numel() else 0
+    factor = 1.0 if weight is not None else 1.0 / max(rows, 1)
+    if _differentiated(logits, teacher, weight):
+        _no_gradient(teacher=teacher, weight=weight)
+        return _TopkDistillLoss.apply(logits, ids, teacher, weight, factor, opts)
+    loss = topk_distill_fwd(logits, ids, teacher, *opts)[0]
+    return _distill_total(loss, _row_floats(weight, loss.shape, loss.device, "weight"), factor)
