@@ -6,10 +6,10 @@ distill / distill_grad: divergence from a teacher's best tokens (streamkl_topk_d
 Rows are [R, V]. Every function also returns how far a computation may be from it that holds sums and exponents in
 float32, U = 2^-24 a rounding, and rounds each result once to its type (the caller's part). A probability is
 exp2((x - r) c): the difference, the product and c are each off by U of themselves, which the exponential turns into
-3 U |z - r| of the term, and the exponential by 2 U. A reference r is within 24 ln 2 < 17 of the largest logit it has
+3 U |z - r| of the term, and the exponential by 2 U. A reference r is within 4 ln 2 < 3 of the largest logit it has
 seen. A lane adds at most V / 64 terms one after the other, and some 20 more roundings join them. So a sum of
 exponentials, relative, and with it its logarithm, absolute, is off by at most
-    SUM = U (3 (D + 17) + 22 + V / 64),    D = sum_j p_j |z_j - max z|.
+    SUM = U (3 (D + 3) + 22 + V / 64),    D = sum_j p_j |z_j - max z|.
 """
 import numpy as np
 
@@ -30,7 +30,7 @@ def _softmax(x, scale):
         p = np.where(total > 0, e / total, 0.0)
         d = np.where(p > 0, p * np.abs(z - safe), 0.0).sum(-1)
         lp = np.where(total > 0, (z - safe) - np.log(total), -np.inf)
-    return lp, p, lse[:, 0], U * (3 * (d + 17) + 22 + x.shape[-1] / 64)
+    return lp, p, lse[:, 0], U * (3 * (d + 3) + 22 + x.shape[-1] / 64)
 
 
 def _entropy_terms(p, lp):
@@ -42,9 +42,9 @@ def token_logprobs(x, tokens, scale, top):
     R, V = x.shape
     lp, p, lse, err = _softmax(x, scale)
     ent = -_entropy_terms(p, lp).sum(-1)
-    wide = np.abs(_entropy_terms(p, lp)).sum(-1) + 17
+    wide = np.abs(_entropy_terms(p, lp)).sum(-1) + 3
     out = {"lse": (lse, err + U * np.where(np.isfinite(lse), np.abs(lse), 0)),
-           # l and a are both off by err of sum p |log p|, of logits relative to a reference up to 17 away
+           # l and a are both off by err of sum p |log p|, of logits relative to a reference up to 3 away
            "entropy": (ent, err * (2 + 2 * wide) + U * np.abs(ent))}
     if tokens is not None:
         t = np.asarray(tokens)
@@ -73,7 +73,7 @@ def token_logprobs_grad(x, tokens, scale, dlogp, dent, dlse):
     size = p * (np.abs(col(e)) + np.abs(col(g)) + np.abs(col(h)) * (np.abs(lp) + np.abs(col(ent))))
     # p is off by 3 U |z - lse| and a few roundings, log p by 3 U |z - lse|, lse and the entropy by their own error
     rel = U * (3 * np.abs(lp) + 10) + col(err)
-    bound = size * rel + p * np.abs(col(h)) * (rel + col(err * (2 + 2 * (np.abs(_entropy_terms(p, lp)).sum(-1) + 17))))
+    bound = size * rel + p * np.abs(col(h)) * (rel + col(err * (2 + 2 * (np.abs(_entropy_terms(p, lp)).sum(-1) + 3))))
     if tokens is not None:
         t = np.asarray(tokens)
         rows = np.nonzero((t >= 0) & (t < V) & ~np.isneginf(lse))[0]
@@ -106,7 +106,7 @@ def _row(z, ids, t, s1, rest, reverse):
     if others:
         zr = z[outside]
         er = np.exp(zr - zr.max())
-        err_r = U * (3 * (np.where(er > 0, er * np.where(er > 0, zr.max() - zr, 0.0), 0.0).sum() / er.sum() + 17) + 22 + V / 64)
+        err_r = U * (3 * (np.where(er > 0, er * np.where(er > 0, zr.max() - zr, 0.0), 0.0).sum() / er.sum() + 3) + 22 + V / 64)
         lqr = lz[outside].max() + np.log(er.sum())
         qr = np.exp(lqr)
     else:

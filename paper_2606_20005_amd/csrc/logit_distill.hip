@@ -256,10 +256,7 @@ distill_kernel(DistillArgs a) {
 #pragma unroll
       for (int j = 0; j < kUnroll; ++j) mx[j] = max_of<T>(f[j]);
       sums.expect(vmax(vmax3(mx[0], mx[1], mx[2]), mx[3]), c, rise);
-#pragma unroll
-      for (int j = 0; j < kUnroll; ++j)
-#pragma unroll
-        for (int e = 0; e < kEpc<T>; ++e) sums.template add<false>(f[j][e], c);
+    sums.template add<false>(f, c);
     });
   }
   sums = block_join<THREADS>(sums, c, red);

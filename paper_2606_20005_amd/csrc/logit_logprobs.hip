@@ -257,10 +257,7 @@ logprob_kernel(LogprobArgs a) {
     }
     const float mm = vmax(vmax3(mx[0], mx[1], mx[2]), mx[3]);
     sums.expect(mm, c, rise);
-#pragma unroll
-    for (int j = 0; j < kUnroll; ++j)
-#pragma unroll
-      for (int e = 0; e < kEpc<T>; ++e) sums.template add<ENTROPY>(f[j][e], c);
+    sums.template add<ENTROPY>(f, c);
     if constexpr (TOP) {
       most = vmax(most, mm);
       constexpr int CPG = kGroup / kEpc<T>;   // lanes that share a group
