@@ -247,6 +247,7 @@ extern "C" int streamkl_topk_distill_step(const streamkl_logits* x, const stream
   a.dx = dx;
   a.dsb = dx_sb;
   a.dsn = dx_sn;
+  if (distill_step_fits((long long)x->B * x->N, x->V, x->dtype)) return status(launch_distill_step(a));
   st = status(launch_distill(a));
   if (st != STREAMKL_OK) return st;
   a.plan = back;

@@ -1,0 +1,199 @@
+// Loss and gradient of a distillation step in one kernel
+// (streamkl_topk_distill_step); logit_distill.hpp has the mathematics.
+//
+// The upstream gradients are known beforehand, so a workgroup that has the sums
+// of a row can write its gradient at once, and it still holds the row: a thread
+// keeps HELD chunks of 16 bytes in registers, THREADS * HELD of them a
+// workgroup (half of a CU's registers at 1024 * 16, 131072 logits of 2 bytes).
+// Chunks beyond that are read again, out of the cache as a rule. So a logit is
+// read once and its gradient written, where a forward and a backward pass read
+// it twice: two thirds of the bytes.
+//
+// All loads of a row are issued before its list is read; the teacher's side is
+// formed by one wave while they are on their way. Whole chunks only are held;
+// the elements of the one or two that are not (rows begin anywhere) are one
+// each in the first threads.
+//
+// The gradient of a listed logit is written by the thread that has written its
+// chunk, after it: a wave's stores to one place arrive in order, so no barrier
+// has to wait for them. Every thread finds its entries in a chained list in LDS.
+#include "logit_distill.hpp"
+
+namespace streamkl {
+namespace {
+
+constexpr int kTurn = 2;   // chunks that are summed at once
+
+struct Upshot {
+  float at, w;   // gradients outside the list: w 2^((x - at) c)
+  int zero;      // no gradient
+};
+
+template <typename T, int THREADS, int HELD, bool REST, int WAVES>
+__global__ void __launch_bounds__(THREADS, WAVES)
+distill_step_kernel(DistillArgs a) {
+  constexpr int E = kEpc<T>;
+  __shared__ float red[3 * THREADS / 64];
+  __shared__ List list;
+  __shared__ Upshot up;
+  __shared__ int head[THREADS];        // a thread's last entry, -1: none; the one before it in next
+  __shared__ int next[kMostList];
+  extern __shared__ u32 marks[];       // REST: a byte per chunk, a bit per listed logit
+  int r, s;
+  if (!grid_place((long long)a.rows.B * a.rows.N, 1, &r, &s)) return;
+  const Row<T> row(a.rows, r);
+  const int tid = threadIdx.x, V = row.V, ph = row.ph;
+  // whole chunks c0 .. c1 - 1, elements before and behind them
+  const int before = ph ? min(V, E - ph) : 0, c0 = ph ? 1 : 0, c1 = max(c0, (ph + V) / E);
+  const int behind = max(before, c1 * E - ph);
+  const int mine = tid < E ? (tid < before ? tid : -1) : tid < 2 * E && behind + tid - E < V ? behind + tid - E : -1;
+  u32x4 held[HELD];
+  if (c0 < c1) {
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) held[j] = row.chunk[min(c0 + j * THREADS + tid, c1 - 1)];
+  } else {
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) held[j] = u32x4{0, 0, 0, 0};
+  }
+  float edge = mine >= 0 ? (float)row.row[mine] : kNegInf;
+  if (tid == 0) list.some = list.bad = list.twice = 0;
+  head[tid] = -1;
+  if constexpr (REST)
+    for (int i = tid; 4 * i < row.chunks; i += THREADS) marks[i] = 0;
+  __syncthreads();
+  read_list<T, THREADS>(a, r, row.row, list, [&](int k, int id) {
+    const int at = id + ph, ch = at / E;
+    if (REST) atomicOr(&marks[ch / 4], 1u << (8 * (ch % 4) + at % E));
+    const int owner = id < before ? id : id >= behind ? E + id - behind : (ch - c0) % THREADS;
+    next[k] = atomicExch(&head[owner], k);
+  });
+  __syncthreads();
+  T* const dx = static_cast<T*>(a.dx) + (r / a.rows.N) * a.dsb + (r % a.rows.N) * a.dsn;
+  if (list.some) {
+    if (tid < 64) teacher_side(a, list);
+    const unsigned char* const mark = reinterpret_cast<const unsigned char*>(marks);
+    const float c = a.s2 * kLog2e, rise = kRise / c;
+    Sums sums;
+    // kTurn chunks of this thread, the first one ch, the others THREADS apart; those from c1 on are none
+    auto sum = [&](int ch, const u32x4(&raw)[kTurn], bool all) {
+      float f[kTurn][E], mx[kTurn];
+      u32 m[kTurn], any = 0;
+#pragma unroll
+      for (int j = 0; j < kTurn; ++j) {
+        const bool there = all || ch + j * THREADS < c1;
+        m[j] = there ? (REST ? mark[ch + j * THREADS] : 0) : (1u << E) - 1;
+        any |= m[j];
+        unpack<T>(raw[j], f[j]);
+      }
+      if ((REST || !all) && __any(any != 0)) {
+#pragma unroll
+        for (int j = 0; j < kTurn; ++j)
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[j][e] = (m[j] >> e) & 1 ? kNegInf : f[j][e];
+      }
+#pragma unroll
+      for (int j = 0; j < kTurn; ++j) mx[j] = max_of<T>(f[j]);
+      sums.expect(vmax(mx[0], mx[1]), c, rise);
+      sums.template add<false>(f, c);
+    };
+#pragma unroll
+    for (int j = 0; j < HELD; j += kTurn) {
+      const int first = c0 + j * THREADS;
+      if (first < c1) {
+        const u32x4 raw[kTurn] = {held[j], held[j + 1]};
+        sum(first + tid, raw, first + kTurn * THREADS <= c1);
+      }
+    }
+    for (int first = c0 + HELD * THREADS; first < c1; first += kTurn * THREADS) {
+      u32x4 raw[kTurn];
+#pragma unroll
+      for (int j = 0; j < kTurn; ++j) raw[j] = row.chunk[min(first + j * THREADS + tid, c1 - 1)];
+      sum(first + tid, raw, first + kTurn * THREADS <= c1);
+    }
+    {
+      const int at = mine + ph;
+      const bool listed = REST && mine >= 0 && (mark[at / E] >> (at % E)) & 1;
+      const float f[1][1] = {{listed ? kNegInf : edge}};
+      sums.expect(f[0][0], c, rise);
+      sums.template add<false>(f, c);
+    }
+    sums = block_join<THREADS>(sums, c, red);
+    if (tid < 64) {
+      float loss;
+      const DistillStats st = finish_row(a, sums, list, &loss);
+      const float g = upstream(a, r);
+      listed_gradients(a, st, g, list);
+      if (tid == 0) {
+        a.loss[r] = loss;
+        a.stats[r] = st;
+        up = Upshot{st.r, (float)((double)a.s2 * (double)g * st.rest), g == 0.f || st.lse == (double)kNegInf};
+      }
+    }
+    __syncthreads();
+    if (!up.zero) {
+      const float at = up.at, w = up.w;
+      auto put = [&](int ch, const u32x4& raw) {
+        float f[E];
+        unpack<T>(raw, f);
+#pragma unroll
+        for (int i = 0; i < E; ++i) f[i] = exp2_fast((f[i] - at) * c) * w;
+        if (ch < c1) *reinterpret_cast<u32x4_any*>(dx + ((long long)ch * E - ph)) = pack<T>(f);
+      };
+#pragma unroll
+      for (int j = 0; j < HELD; ++j)
+        if (c0 + j * THREADS < c1) put(c0 + j * THREADS + tid, held[j]);
+      for (int first = c0 + HELD * THREADS; first < c1; first += kTurn * THREADS) {
+        u32x4 raw[kTurn];
+#pragma unroll
+        for (int j = 0; j < kTurn; ++j) raw[j] = row.chunk[min(first + j * THREADS + tid, c1 - 1)];
+#pragma unroll
+        for (int j = 0; j < kTurn; ++j) put(first + j * THREADS + tid, raw[j]);
+      }
+      if (mine >= 0) dx[mine] = (T)(exp2_fast((edge - at) * c) * w);
+      for (int k = head[tid]; k >= 0; k = next[k]) dx[list.id[k]] = (T)list.value[k];
+      return;
+    }
+  } else if (tid == 0) {
+    a.loss[r] = 0.f;
+    a.stats[r] = DistillStats{0.f, 0.f, (double)kNegInf, 0.0, 0.0};
+  }
+  for (int ch = c0 + tid; ch < c1; ch += THREADS)
+    *reinterpret_cast<u32x4_any*>(dx + ((long long)ch * E - ph)) = u32x4{0, 0, 0, 0};
+  if (mine >= 0) dx[mine] = (T)0.f;
+}
+
+template <typename T, int THREADS, int HELD>
+void run(const DistillArgs& a) {
+  // waves a SIMD that the registers held leave room for
+  constexpr int waves = HELD <= 4 ? 6 : 4;
+  const long long rows = (long long)a.rows.B * a.rows.N;
+  if (a.rest)
+    distill_step_kernel<T, THREADS, HELD, true, waves>
+        <<<logit_grid(rows), dim3(THREADS), (size_t)(chunks_of(a.rows.V, a.rows.dtype) + 3) / 4 * 4, a.stream>>>(a);
+  else
+    distill_step_kernel<T, THREADS, HELD, false, waves><<<logit_grid(rows), dim3(THREADS), 0, a.stream>>>(a);
+}
+
+}  // namespace
+
+bool distill_step_fits(long long rows, int V, int dtype) {
+  return rows >= 128 && chunks_of(V, dtype) <= kMostMarks;
+}
+
+hipError_t launch_distill_step(const DistillArgs& a) {
+  const int chunks = chunks_of(a.rows.V, a.rows.dtype);
+  by_type(a.rows.dtype, [&](auto t) {
+    using T = decltype(t);
+    if (chunks <= 1024)
+      run<T, 256, 4>(a);
+    else if (chunks <= 4096)
+      run<T, 256, 16>(a);
+    else if (chunks <= 8192)
+      run<T, 512, 16>(a);
+    else
+      run<T, 1024, 16>(a);
+  });
+  return hipGetLastError();
+}
+
+}  // namespace streamkl

@@ -98,6 +98,9 @@ size_t distill_workspace(long long rows, const LogitPlan& p);
 hipError_t launch_distill(const DistillArgs& a);
 LogitPlan distill_grad_plan(long long rows, int V, int dtype);
 hipError_t launch_distill_grad(const DistillArgs& a);
+// Loss and gradient in one kernel, for sizes that it holds.
+bool distill_step_fits(long long rows, int V, int dtype);
+hipError_t launch_distill_step(const DistillArgs& a);
 hipError_t launch_weighted_sum(const float* loss, const float* weight, float factor, long long rows, float* total,
                                hipStream_t stream);
 

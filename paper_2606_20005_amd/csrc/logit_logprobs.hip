@@ -46,8 +46,9 @@ __device__ __forceinline__ float value_of(u32 k) {
 // Value, then place: a larger one ranks first.
 __device__ __forceinline__ u64 rank_key(u32 key, u32 place) { return ((u64)key << 32) | (u32)~place; }
 
+template <typename T>
 struct TopShared {
-  float group[kMostGroups];
+  T group[kMostGroups];   // their maxima, which are logits
   u64 cand[kMostCands];
   int hit[kMostHits];
   u32 most[512];     // keys of the threads' maxima
@@ -90,8 +91,8 @@ __device__ __forceinline__ u32 bound_of(const u32* most, int top) {
 }
 
 // How many groups satisfy `pred`, in every thread. All threads call it; `turn` counts the calls.
-template <int THREADS, typename P>
-__device__ int count_groups(TopShared& sh, int groups, int turn, P pred) {
+template <typename T, int THREADS, typename P>
+__device__ int count_groups(TopShared<T>& sh, int groups, int turn, P pred) {
   int n = 0;
   for (int b = 0; b < groups; b += THREADS) {
     const int g = b + threadIdx.x;
@@ -108,7 +109,7 @@ __device__ int count_groups(TopShared& sh, int groups, int turn, P pred) {
 // The candidates of a part: keys of all its logits that can be among the `top` first, in sh.cand (sh.cands of them), the
 // first `top` among them for sure. group0 is the first group of the part.
 template <typename T, int THREADS>
-__device__ void find_candidates(TopShared& sh, const Row<T>& row, int group0, int groups, int top) {
+__device__ void find_candidates(TopShared<T>& sh, const Row<T>& row, int group0, int groups, int top) {
   const int tid = threadIdx.x;
   __syncthreads();   // group maxima and thread maxima are written
   if (tid < 64) {
@@ -122,7 +123,7 @@ __device__ void find_candidates(TopShared& sh, const Row<T>& row, int group0, in
   __syncthreads();
   auto gather = [&](u32 bound, auto pred) {
     for (int g = tid; g < groups; g += THREADS) {
-      if (pred(g, key_of(sh.group[g]))) {
+      if (pred(g, key_of((float)sh.group[g]))) {
         const int at = atomicAdd(&sh.hits, 1);
         if (at < kMostHits) sh.hit[at] = g;
       }
@@ -151,17 +152,17 @@ __device__ void find_candidates(TopShared& sh, const Row<T>& row, int group0, in
   u32 lo = bound, hi = 0xffffffffu;   // more than `top` groups reach lo
   while (lo < hi) {
     const u32 mid = lo + (hi - lo) / 2 + 1;
-    if (count_groups<THREADS>(sh, groups, turn++, [&](int g) { return key_of(sh.group[g]) >= mid; }) < top)
+    if (count_groups<T, THREADS>(sh, groups, turn++, [&](int g) { return key_of((float)sh.group[g]) >= mid; }) < top)
       hi = mid - 1;
     else
       lo = mid;
   }
   const u32 v = lo;
-  const int above = count_groups<THREADS>(sh, groups, turn++, [&](int g) { return key_of(sh.group[g]) > v; });
+  const int above = count_groups<T, THREADS>(sh, groups, turn++, [&](int g) { return key_of((float)sh.group[g]) > v; });
   int g0 = 0, g1 = groups - 1;        // the last group of key v that is taken
   while (g0 < g1) {
     const int mid = g0 + (g1 - g0) / 2;
-    if (count_groups<THREADS>(sh, groups, turn++, [&](int g) { return g <= mid && key_of(sh.group[g]) == v; }) <
+    if (count_groups<T, THREADS>(sh, groups, turn++, [&](int g) { return g <= mid && key_of((float)sh.group[g]) == v; }) <
         top - above)
       g0 = mid + 1;
     else
@@ -173,8 +174,8 @@ __device__ void find_candidates(TopShared& sh, const Row<T>& row, int group0, in
 }
 
 // Ranks the candidates: f(rank, key) for the first `top`.
-template <int THREADS, typename F>
-__device__ __forceinline__ void rank_candidates(const TopShared& sh, int top, F f) {
+template <typename T, int THREADS, typename F>
+__device__ __forceinline__ void rank_candidates(const TopShared<T>& sh, int top, F f) {
   const int n = sh.cands < kMostCands ? sh.cands : kMostCands;
   for (int i = threadIdx.x; i < n; i += THREADS) {
     const u64 k = sh.cand[i];
@@ -194,7 +195,7 @@ struct RowEnd {
   double r, log_l, scale;
   bool empty;
   __device__ __forceinline__ RowEnd(const Sums& s, float scale_)
-      : r((double)s.r), log_l(log((double)s.l)), scale((double)scale_), empty(s.l == 0.f) {}
+      : r((double)s.r), log_l(log_of((double)s.l)), scale((double)scale_), empty(s.l == 0.f) {}
   __device__ __forceinline__ float logp(float x) const {
     return empty ? kNegInf : (float)(scale * ((double)x - r) - log_l);
   }
@@ -237,10 +238,10 @@ __device__ __forceinline__ void write_none(const LogprobArgs& a, int r, int rank
 struct NoShared {};
 
 template <typename T, int THREADS, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 8)
 logprob_kernel(LogprobArgs a) {
   __shared__ float red[3 * THREADS / 64];
-  __shared__ std::conditional_t<TOP, TopShared, NoShared> sh;
+  __shared__ std::conditional_t<TOP, TopShared<T>, NoShared> sh;
   int r, s;
   if (!grid_place((long long)a.rows.B * a.rows.N, a.plan.parts, &r, &s)) return;
   const Row<T> row(a.rows, r);
@@ -256,8 +257,6 @@ logprob_kernel(LogprobArgs a) {
       mx[j] = max_of<T>(f[j]);
     }
     const float mm = vmax(vmax3(mx[0], mx[1], mx[2]), mx[3]);
-    sums.expect(mm, c, rise);
-    sums.template add<ENTROPY>(f, c);
     if constexpr (TOP) {
       most = vmax(most, mm);
       constexpr int CPG = kGroup / kEpc<T>;   // lanes that share a group
@@ -266,9 +265,11 @@ logprob_kernel(LogprobArgs a) {
         float g = vmax(mx[j], quad_swap<kXor1>(mx[j]));
         if constexpr (CPG == 4) g = vmax(g, quad_swap<kXor2>(g));
         const int ch = at + j * THREADS;
-        if (ch < c1 && tid % CPG == 0) sh.group[(ch - c0) / CPG] = g;
+        if (ch < c1 && tid % CPG == 0) sh.group[(ch - c0) / CPG] = (T)g;
       }
     }
+    sums.expect(mm, c, rise);
+    sums.template add<ENTROPY>(f, c);
   });
   if constexpr (TOP) {
     for (int i = tid; i < 512; i += THREADS) sh.most[i] = i == tid ? key_of(most) : 0u;
@@ -284,7 +285,7 @@ logprob_kernel(LogprobArgs a) {
     if (tid == 0) finish_row(a, r, sums, end, row.row, a.rows.dtype);
     if constexpr (TOP) {
       for (int i = sh.cands + tid; i < top; i += THREADS) write_none(a, r, i);
-      rank_candidates<THREADS>(sh, top, [&](int rank, u64 k) { write_top(a, r, rank, k, end); });
+      rank_candidates<T, THREADS>(sh, top, [&](int rank, u64 k) { write_top(a, r, rank, k, end); });
     }
   } else {
     const long long i = (long long)r * a.plan.parts + s;
@@ -293,7 +294,7 @@ logprob_kernel(LogprobArgs a) {
       const long long all = (long long)a.rows.B * a.rows.N * a.plan.parts;
       u64* keys = reinterpret_cast<u64*>(static_cast<char*>(a.workspace) + (all * sizeof(Part) + 15) / 16 * 16) + i * top;
       for (int q = sh.cands + tid; q < top; q += THREADS) keys[q] = 0;   // ranks behind any logit
-      rank_candidates<THREADS>(sh, top, [&](int rank, u64 k) { keys[rank] = k; });
+      rank_candidates<T, THREADS>(sh, top, [&](int rank, u64 k) { keys[rank] = k; });
     }
   }
 }

@@ -157,7 +157,7 @@ __device__ __forceinline__ void each_turn(const Row<T>& row, int c0, int c1, F f
   }
 }
 
-typedef u32x4 u32x4_any __attribute__((aligned(2)));   // a chunk at the address of any element
+typedef u32x4 u32x4_any __attribute__((aligned(2), may_alias));   // a chunk at the address of any element
 
 // The places of a chunk of `row` in a row of gradients of any alignment (its elements begin at `to`).
 template <typename T>
@@ -200,15 +200,9 @@ struct Sums {
     float ls[4] = {}, as[4] = {};
 #pragma unroll
     for (int i = 0; i < N * E; ++i) {
-      float u = (f[i / E][i % E] - r) * c;
-      if constexpr (ENTROPY) {
-        u = u < kFloor ? kFloor : u;   // keeps a NaN, which a maximum would drop
-        const float e = exp2_fast(u);
-        ls[i % 4] += e;
-        as[i % 4] = __builtin_fmaf(e, u, as[i % 4]);
-      } else {
-        ls[i % 4] += exp2_fast(u);
-      }
+      const float u = (f[i / E][i % E] - r) * c, e = exp2_fast(u);
+      ls[i % 4] += e;
+      if constexpr (ENTROPY) as[i % 4] = __builtin_fmaf(e, vmax(u, kFloor), as[i % 4]);   // a NaN stays in e
     }
     l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
     if constexpr (ENTROPY) a += (as[0] + as[1]) + (as[2] + as[3]);
@@ -264,6 +258,17 @@ __device__ __forceinline__ Sums block_join(Sums s, float c, float* red) {
     s = t;
   }
   return s;
+}
+
+// log v for v > 0, off by about 2^-25: the logarithm of a number near 1, and the exponent in 64 bits.
+__device__ __forceinline__ double log_of(double v) {
+  int e;
+  double m = frexp(v, &e);
+  if (m < 0.70710678118654752) {
+    m *= 2.0;
+    --e;
+  }
+  return (double)e * 0.69314718055994530942 + (double)logf((float)m);
 }
 
 // exp(s x - lse) = 2^((x - at) c) f: what a log-sum-exp is for a kernel that forms probabilities, given as its float32
