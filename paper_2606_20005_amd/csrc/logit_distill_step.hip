@@ -137,7 +137,7 @@ distill_step_kernel(DistillArgs a) {
         unpack<T>(raw, f);
 #pragma unroll
         for (int i = 0; i < E; ++i) f[i] = exp2_fast((f[i] - at) * c) * w;
-        if (ch < c1) *reinterpret_cast<u32x4_any*>(dx + ((long long)ch * E - ph)) = pack<T>(f);
+        if (ch < c1) store_chunk(dx + ((long long)ch * E - ph), pack<T>(f));
       };
 #pragma unroll
       for (int j = 0; j < HELD; ++j)
@@ -158,7 +158,7 @@ distill_step_kernel(DistillArgs a) {
     a.stats[r] = DistillStats{0.f, 0.f, (double)kNegInf, 0.0, 0.0};
   }
   for (int ch = c0 + tid; ch < c1; ch += THREADS)
-    *reinterpret_cast<u32x4_any*>(dx + ((long long)ch * E - ph)) = u32x4{0, 0, 0, 0};
+    store_chunk(dx + ((long long)ch * E - ph), u32x4{0, 0, 0, 0});
   if (mine >= 0) dx[mine] = (T)0.f;
 }
 
@@ -188,10 +188,8 @@ hipError_t launch_distill_step(const DistillArgs& a) {
       run<T, 256, 4>(a);
     else if (chunks <= 4096)
       run<T, 256, 16>(a);
-    else if (chunks <= 8192)
-      run<T, 512, 16>(a);
     else
-      run<T, 1024, 16>(a);
+      run<T, 512, 16>(a);
   });
   return hipGetLastError();
 }

@@ -375,6 +375,7 @@ __global__ void __launch_bounds__(THREADS)
 logprob_grad_kernel(LogprobGradArgs a) {
   int r, s;
   if (!grid_place((long long)a.rows.B * a.rows.N, a.plan.parts, &r, &s)) return;
+  r = a.rows.B * a.rows.N - 1 - r;   // the last rows first: the forward pass left them in the cache
   const Row<T> row(a.rows, r);
   const int c0 = s * a.plan.chunks, c1 = min(row.chunks, c0 + a.plan.chunks);
   const int b = r / a.rows.N;

@@ -159,12 +159,18 @@ __device__ __forceinline__ void each_turn(const Row<T>& row, int c0, int c1, F f
 
 typedef u32x4 u32x4_any __attribute__((aligned(2), may_alias));   // a chunk at the address of any element
 
+// Gradients go past the caches, which are left to the logits that are read again.
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* to, const u32x4& v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any*>(to));
+}
+
 // The places of a chunk of `row` in a row of gradients of any alignment (its elements begin at `to`).
 template <typename T>
 __device__ __forceinline__ void store(const Row<T>& row, T* to, int c, const float (&f)[kEpc<T>]) {
   to += (long long)c * kEpc<T> - row.ph;
   if (row.whole(c)) {
-    *reinterpret_cast<u32x4_any*>(to) = pack<T>(f);
+    store_chunk(to, pack<T>(f));
   } else {
 #pragma unroll
     for (int e = 0; e < kEpc<T>; ++e) {
