@@ -109,12 +109,7 @@ distill_join_kernel(DistillArgs a) {
 
 // dx of a part of a row.
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS, 8)
-distill_grad_kernel(DistillArgs a) {
-  __shared__ List list;
-  if (a.done_if_one && *a.dfactor == 1.f) return;
-  int r, s;
-  if (!grid_place((long long)a.rows.B * a.rows.N, a.plan.parts, &r, &s)) return;
+__device__ __forceinline__ void part_gradients(const DistillArgs& a, int r, int s, List& list) {
   r = a.rows.B * a.rows.N - 1 - r;   // the last rows first: the forward pass left them in the cache
   const Row<T> row(a.rows, r);
   const int c0 = s * a.plan.chunks, c1 = min(row.chunks, c0 + a.plan.chunks), tid = threadIdx.x;
@@ -127,6 +122,7 @@ distill_grad_kernel(DistillArgs a) {
     for (int ch = c0 + tid; ch < c1; ch += THREADS) store<T>(row, dx, ch, z);
     return;
   }
+  __syncthreads();   // the list of the part before is done with
   // dx may be x: the listed logits of a part are read before it writes, those of other parts are read but not used
   if (tid == 0) list.some = list.bad = list.twice = 0;
   __syncthreads();
@@ -156,16 +152,44 @@ distill_grad_kernel(DistillArgs a) {
   }
 }
 
+// One part a workgroup; FEW, where there may be nothing to do: few workgroups that take several (65536 that only look at the
+// factor took 15 us).
+constexpr int kFewWorkgroups = 2048;
+
+template <typename T, int THREADS, bool FEW>
+__global__ void __launch_bounds__(THREADS, FEW ? 4 : 8)
+distill_grad_kernel(DistillArgs a) {
+  __shared__ List list;
+  int r, s;
+  if constexpr (!FEW) {
+    if (grid_place((long long)a.rows.B * a.rows.N, a.plan.parts, &r, &s)) part_gradients<T, THREADS>(a, r, s, list);
+  } else {
+    if (*a.dfactor == 1.f) return;
+    const long long n = (long long)a.rows.B * a.rows.N * a.plan.parts;
+    for (long long i = blockIdx.x; i < n; i += gridDim.x)
+      part_gradients<T, THREADS>(a, (int)(i / a.plan.parts), (int)(i % a.plan.parts), list);
+  }
+}
+
 // total = sum of weight factor loss over the rows whose weight is not 0, by one workgroup.
 constexpr int kSumThreads = 1024;
 
 __global__ void __launch_bounds__(kSumThreads)
 weighted_sum_kernel(const float* loss, const float* weight, float factor, long long rows, float* total) {
   __shared__ double red[kSumThreads / 64];
+  // eight loads of each in flight
+  constexpr int ahead = 8;
   double v = 0.0;
-  for (long long i = threadIdx.x; i < rows; i += kSumThreads) {
-    const float w = weight ? weight[i] : 1.f;
-    v += w == 0.f ? 0.0 : (double)w * (double)loss[i];
+  for (long long i = threadIdx.x; i < rows; i += ahead * kSumThreads) {
+    float w[ahead], l[ahead];
+#pragma unroll
+    for (int u = 0; u < ahead; ++u) {
+      const long long at = i + u * kSumThreads;
+      w[u] = at < rows ? (weight ? weight[at] : 1.f) : 0.f;
+      l[u] = at < rows ? loss[at] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < ahead; ++u) v += w[u] == 0.f ? 0.0 : (double)w[u] * (double)l[u];
   }
   v = wave_sum(v);
   if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
@@ -231,9 +255,13 @@ LogitPlan distill_grad_plan(long long rows, int V, int dtype) {
 }
 
 hipError_t launch_distill_grad(const DistillArgs& a) {
-  const dim3 grid = logit_grid((long long)a.rows.B * a.rows.N * a.plan.parts);
+  const long long n = (long long)a.rows.B * a.rows.N * a.plan.parts;
   by_type(a.rows.dtype, [&](auto t) {
-    distill_grad_kernel<decltype(t), 256><<<grid, dim3(256), 0, a.stream>>>(a);
+    if (a.done_if_one)
+      distill_grad_kernel<decltype(t), 256, true>
+          <<<dim3((unsigned)(n < kFewWorkgroups ? n : kFewWorkgroups)), dim3(256), 0, a.stream>>>(a);
+    else
+      distill_grad_kernel<decltype(t), 256, false><<<logit_grid(n), dim3(256), 0, a.stream>>>(a);
   });
   return hipGetLastError();
 }

@@ -201,7 +201,22 @@ struct RowEnd {
   }
 };
 
-__device__ void finish_row(const LogprobArgs& a, int r, const Sums& sums, const RowEnd& end, const void* x, int dtype) {
+// A row's token and its logit.
+struct Token {
+  long long id;
+  float x;
+  __device__ __forceinline__ Token(const LogprobArgs& a, int r, const void* row) : id(-1), x(0.f) {
+    if (!a.logp) return;
+    id = a.tokens64 ? static_cast<const long long*>(a.tokens)[r] : static_cast<const int*>(a.tokens)[r];
+    if (id < 0 || id >= a.rows.V) return;
+    x = a.rows.dtype == STREAMKL_F32   ? static_cast<const float*>(row)[id]
+        : a.rows.dtype == STREAMKL_F16 ? (float)static_cast<const _Float16*>(row)[id]
+                                       : (float)static_cast<const __bf16*>(row)[id];
+  }
+};
+
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int r, const Sums& sums, const RowEnd& end,
+                                           const Token& token) {
   const double base = end.scale * end.r;   // exact
   const float lse = end.empty ? kNegInf : (float)(base + end.log_l);
   if (a.lse) a.lse[r] = lse;
@@ -209,17 +224,7 @@ __device__ void finish_row(const LogprobArgs& a, int r, const Sums& sums, const 
   // in units of log 2: log2 l - a / l
   if (a.entropy)
     a.entropy[r] = end.empty ? 0.f : (float)(end.log_l - 0.69314718055994530942 * ((double)sums.a / (double)sums.l));
-  if (a.logp) {
-    const long long t = a.tokens64 ? static_cast<const long long*>(a.tokens)[r] : static_cast<const int*>(a.tokens)[r];
-    float v = 0.f;
-    if (t >= a.rows.V)
-      v = __builtin_nanf("");
-    else if (t >= 0)
-      v = end.logp(dtype == STREAMKL_F32   ? static_cast<const float*>(x)[t]
-                   : dtype == STREAMKL_F16 ? (float)static_cast<const _Float16*>(x)[t]
-                                           : (float)static_cast<const __bf16*>(x)[t]);
-    a.logp[r] = v;
-  }
+  if (a.logp) a.logp[r] = token.id < 0 ? 0.f : token.id >= a.rows.V ? __builtin_nanf("") : end.logp(token.x);
 }
 
 __device__ __forceinline__ void write_top(const LogprobArgs& a, int r, int rank, u64 k, const RowEnd& end) {
@@ -282,7 +287,7 @@ logprob_kernel(LogprobArgs a) {
     find_candidates<T, THREADS>(sh, row, c0 / CPG, (c1 - c0 + CPG - 1) / CPG, top);
   }
   if (a.plan.parts == 1) {
-    if (tid == 0) finish_row(a, r, sums, end, row.row, a.rows.dtype);
+    if (tid == 0) finish_row(a, r, sums, end, Token(a, r, row.row));
     if constexpr (TOP) {
       for (int i = sh.cands + tid; i < top; i += THREADS) write_none(a, r, i);
       rank_candidates<T, THREADS>(sh, top, [&](int rank, u64 k) { write_top(a, r, rank, k, end); });
@@ -299,60 +304,84 @@ logprob_kernel(LogprobArgs a) {
   }
 }
 
-// Joins the parts of a row: sums by one lane each, alternatives by ranking every key among the sorted lists of all parts.
-constexpr int kJoinThreads = 256;
+// Joins the parts of a row. Sums by one lane a part. Every part has sorted keys, `per` of them at or before its per-th, so
+// that `top` keys rank at or before the last of these: only keys up to there are looked at, and each is ranked against all
+// others of them (or, where they are many, among the sorted lists). Everything is on its way before anything is waited for:
+// the kernel is latency (16 rows of 16 parts, 20 alternatives: 18 us with the bound by one thread and a search in every
+// list, 6 us so).
+constexpr int kJoinThreads = 256, kJoinCands = 512;
 
 __global__ void __launch_bounds__(kJoinThreads)
 logprob_join_kernel(LogprobArgs a) {
   extern __shared__ u64 keys[];   // [parts][top]
+  __shared__ u64 cand[kJoinCands];
   __shared__ u64 bound;
   __shared__ float joined[2];
+  __shared__ int cands;
   int r, s;
   if (!grid_place((long long)a.rows.B * a.rows.N, 1, &r, &s)) return;
-  const int tid = threadIdx.x, parts = a.plan.parts, top = a.top;
+  const int tid = threadIdx.x, parts = a.plan.parts, top = a.top, n = parts * top;
   const float c = a.scale * kLog2e;
+  const long long all = (long long)a.rows.B * a.rows.N * parts;
+  const u64* const from =
+      reinterpret_cast<const u64*>(static_cast<const char*>(a.workspace) + (all * sizeof(Part) + 15) / 16 * 16) +
+      (long long)r * n;
   if (tid < 64) {
+    const int b = r / a.rows.N;
+    const long long at = b * a.rows.sb + (r - b * a.rows.N) * a.rows.sn;
     Sums sums;
+    u64 least = ~0ull;
     if (tid < parts) {
       const Part p = static_cast<const Part*>(a.workspace)[(long long)r * parts + tid];
       sums.r = p.r;
       sums.l = p.l;
       sums.a = p.a;
+      if (top) least = from[tid * top + (top + parts - 1) / parts - 1];
+    }
+    const Token token(a, r, static_cast<const char*>(a.rows.x) + at * (a.rows.dtype == STREAMKL_F32 ? 4 : 2));
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const u64 o = (u64)__shfl_xor((long long)least, m);
+      least = o < least ? o : least;
     }
     sums = wave_join(sums, c);
     if (tid == 0) {
       joined[0] = sums.r;
       joined[1] = sums.l;
-      const int b = r / a.rows.N;
-      const long long at = b * a.rows.sb + (r - b * a.rows.N) * a.rows.sn;
-      const int size = a.rows.dtype == STREAMKL_F32 ? 4 : 2;
-      finish_row(a, r, sums, RowEnd(sums, a.scale), static_cast<const char*>(a.rows.x) + at * size, a.rows.dtype);
+      bound = least ? least : 1;
+      cands = 0;
+      finish_row(a, r, sums, RowEnd(sums, a.scale), token);
     }
   }
   if (top == 0) return;
-  const long long all = (long long)a.rows.B * a.rows.N * parts;
-  const u64* from =
-      reinterpret_cast<const u64*>(static_cast<const char*>(a.workspace) + (all * sizeof(Part) + 15) / 16 * 16) +
-      (long long)r * parts * top;
-  const int n = parts * top;
   for (int i = tid; i < n; i += kJoinThreads) keys[i] = from[i];
   for (int i = tid; i < top; i += kJoinThreads) write_none(a, r, i);
   __syncthreads();
-  if (tid == 0) {
-    // every part has `per` keys at or before its per-th, so that `top` keys rank at or before the last of these
-    const int per = (top + parts - 1) / parts;
-    u64 t = ~0ull;
-    for (int p = 0; p < parts; ++p) t = keys[p * top + per - 1] < t ? keys[p * top + per - 1] : t;
-    bound = t ? t : 1;
+  const u64 first = bound;
+  for (int i = tid; i < n; i += kJoinThreads) {
+    if (keys[i] >= first) {
+      const int at = atomicAdd(&cands, 1);
+      if (at < kJoinCands) cand[at] = keys[i];
+    }
   }
   __syncthreads();
   Sums sums;
   sums.r = joined[0];
   sums.l = joined[1];
   const RowEnd end(sums, a.scale);
+  if (cands <= kJoinCands) {
+    const int m = cands;
+    for (int i = tid; i < m; i += kJoinThreads) {
+      const u64 k = cand[i];
+      int rank = 0;
+      for (int j = 0; j < m; ++j) rank += cand[j] > k;
+      if (rank < top) write_top(a, r, rank, k, end);
+    }
+    return;
+  }
   for (int i = tid; i < n; i += kJoinThreads) {
     const u64 k = keys[i];
-    if (k < bound) continue;
+    if (k < first) continue;
     int rank = 0;
     for (int p = 0; p < parts && rank < top; ++p) {
       int lo = 0, hi = top;   // keys of part p that rank before k
