@@ -92,7 +92,7 @@ extern "C" size_t streamkl_token_logprobs_workspace_bytes(int B, int N, int V, i
   if (B < 0 || N < 0 || V < 1 || V > kMostVocab || !known_type(dtype) || top < 0 || top > kMostTop || top > V) return 0;
   const long long rows = (long long)B * N;
   if (rows > kMostRows) return 0;
-  return logprob_workspace(rows, logprob_plan(rows, V, dtype, top), top);
+  return logprob_workspace(rows, logprob_plan(rows, V, dtype == STREAMKL_F32, top), top);
 }
 
 extern "C" int streamkl_token_logprobs_fwd(const streamkl_logits* x, const void* tokens, int tokens64, float scale, int top,
@@ -113,7 +113,7 @@ extern "C" int streamkl_token_logprobs_fwd(const streamkl_logits* x, const void*
   LogprobArgs a = {};
   a.rows = rows_of(x);
   const long long rows = (long long)x->B * x->N;
-  a.plan = logprob_plan(rows, x->V, x->dtype, top);
+  a.plan = logprob_plan(rows, x->V, x->dtype == STREAMKL_F32, top);
   if (!countable(x->B, x->N, a.plan.parts)) return STREAMKL_ERR_UNSUPPORTED;
   st = check_workspace(workspace, workspace_bytes, logprob_workspace(rows, a.plan, top));
   if (st != STREAMKL_OK) return st;
@@ -148,7 +148,7 @@ extern "C" int streamkl_token_logprobs_bwd(const streamkl_logits* x, const void*
     if (!aligned_to(p, 4)) return STREAMKL_ERR_INVALID_ARG;
   LogprobGradArgs a = {};
   a.rows = rows_of(x);
-  a.plan = logprob_grad_plan((long long)x->B * x->N, x->V, x->dtype);
+  a.plan = grad_plan(x->V, x->dtype == STREAMKL_F32);
   if (!countable(x->B, x->N, a.plan.parts)) return STREAMKL_ERR_UNSUPPORTED;
   a.tokens = tokens;
   a.tokens64 = tokens64;
@@ -170,7 +170,7 @@ extern "C" size_t streamkl_topk_distill_workspace_bytes(int B, int N, int V, int
   if (B < 0 || N < 0 || V < 1 || V > kMostVocab || !known_type(dtype)) return 0;
   const long long rows = (long long)B * N;
   if (rows > kMostRows) return 0;
-  return distill_workspace(rows, distill_plan(rows, V, dtype, rest));
+  return distill_workspace(rows, distill_plan(rows, V, dtype == STREAMKL_F32, rest != 0));
 }
 
 namespace {
@@ -185,7 +185,7 @@ int distill_forward(const streamkl_logits* x, const streamkl_teacher_list* t, fl
   if (!loss || !aligned_to(loss, 4) || !stats || !aligned_to(stats, 8)) return STREAMKL_ERR_INVALID_ARG;
   *a = distill_args(x, t, scale, direction, stream);
   const long long rows = (long long)x->B * x->N;
-  a->plan = distill_plan(rows, x->V, x->dtype, t->rest);
+  a->plan = distill_plan(rows, x->V, x->dtype == STREAMKL_F32, t->rest != 0);
   if (!countable(x->B, x->N, a->plan.parts)) return STREAMKL_ERR_UNSUPPORTED;
   a->workspace = workspace;
   a->loss = loss;
@@ -217,7 +217,7 @@ extern "C" int streamkl_topk_distill_bwd(const streamkl_logits* x, const streamk
   if (st != STREAMKL_OK) return st;
   if (!stats || !aligned_to(stats, 8) || !aligned_to(dloss, 4) || !aligned_to(dfactor, 4)) return STREAMKL_ERR_INVALID_ARG;
   DistillArgs a = distill_args(x, t, scale, direction, stream);
-  a.plan = distill_grad_plan((long long)x->B * x->N, x->V, x->dtype);
+  a.plan = grad_plan(x->V, x->dtype == STREAMKL_F32);
   if (!countable(x->B, x->N, a.plan.parts)) return STREAMKL_ERR_UNSUPPORTED;
   a.stats = const_cast<DistillStats*>(static_cast<const DistillStats*>(stats));
   a.weight = dloss;
@@ -240,14 +240,14 @@ extern "C" int streamkl_topk_distill_step(const streamkl_logits* x, const stream
   st = check_grads(x, dx, dx_sb, dx_sn);
   if (st != STREAMKL_OK) return st;
   if (!aligned_to(weight, 4)) return STREAMKL_ERR_INVALID_ARG;
-  const LogitPlan back = distill_grad_plan((long long)x->B * x->N, x->V, x->dtype);
+  const LogitPlan back = grad_plan(x->V, x->dtype == STREAMKL_F32);
   if (!countable(x->B, x->N, back.parts)) return STREAMKL_ERR_UNSUPPORTED;
   a.weight = weight;
   a.factor = factor;
   a.dx = dx;
   a.dsb = dx_sb;
   a.dsn = dx_sn;
-  if (distill_step_fits((long long)x->B * x->N, x->V, x->dtype)) return status(launch_distill_step(a));
+  if (distill_step_fits((long long)x->B * x->N, x->V, x->dtype == STREAMKL_F32)) return status(launch_distill_step(a));
   st = status(launch_distill(a));
   if (st != STREAMKL_OK) return st;
   a.plan = back;

@@ -11,10 +11,6 @@ namespace {
 
 constexpr int kUnroll = 4;
 
-struct Part {
-  float r, l;
-};
-
 template <typename T, int THREADS, bool REST>
 __global__ void __launch_bounds__(THREADS, 8)
 distill_kernel(DistillArgs a) {
@@ -74,7 +70,7 @@ distill_kernel(DistillArgs a) {
       }
     }
   } else if (tid == 0) {
-    static_cast<Part*>(a.workspace)[(long long)r * a.plan.parts + s] = Part{sums.r, sums.l};
+    static_cast<DistillPart*>(a.workspace)[(long long)r * a.plan.parts + s] = DistillPart{sums.r, sums.l};
   }
 }
 
@@ -90,7 +86,7 @@ distill_join_kernel(DistillArgs a) {
   __syncthreads();
   Sums sums;
   if ((int)threadIdx.x < a.plan.parts) {
-    const Part p = static_cast<const Part*>(a.workspace)[(long long)r * a.plan.parts + threadIdx.x];
+    const DistillPart p = static_cast<const DistillPart*>(a.workspace)[(long long)r * a.plan.parts + threadIdx.x];
     sums.r = p.r;
     sums.l = p.l;
   }
@@ -211,26 +207,6 @@ void run_fwd(const DistillArgs& a, dim3 grid) {
 
 }  // namespace
 
-LogitPlan distill_plan(long long rows, int V, int dtype, int rest) {
-  const int epc = dtype == STREAMKL_F32 ? 4 : 8, chunks = chunks_of(V, dtype);
-  long long parts = rows ? 512 / rows : 1;
-  const long long useful = ((long long)V + 8191) / 8192;
-  if (parts > useful) parts = useful;
-  const long long least = rest ? (chunks + kMostMarks - 1) / kMostMarks : 1;
-  if (parts < least) parts = least;
-  if (parts < 1) parts = 1;
-  if (parts > kMostParts) parts = kMostParts;
-  LogitPlan p;
-  p.chunks = (int)((chunks + parts - 1) / parts + 3) / 4 * 4;
-  p.parts = (chunks + p.chunks - 1) / p.chunks;
-  p.threads = (long long)p.chunks * epc <= 16384 ? 256 : 512;
-  return p;
-}
-
-size_t distill_workspace(long long rows, const LogitPlan& p) {
-  return p.parts <= 1 ? 0 : (size_t)rows * p.parts * sizeof(Part);
-}
-
 hipError_t launch_distill(const DistillArgs& a) {
   const long long rows = (long long)a.rows.B * a.rows.N;
   const dim3 grid = logit_grid(rows * a.plan.parts);
@@ -242,16 +218,6 @@ hipError_t launch_distill(const DistillArgs& a) {
     if (a.plan.parts > 1) distill_join_kernel<decltype(t)><<<logit_grid(rows), dim3(64), 0, a.stream>>>(a);
   });
   return hipGetLastError();
-}
-
-LogitPlan distill_grad_plan(long long rows, int V, int dtype) {
-  const int chunks = chunks_of(V, dtype);
-  const long long parts = ((long long)V + 32767) / 32768;
-  LogitPlan p;
-  p.chunks = (int)((chunks + parts - 1) / parts + 3) / 4 * 4;
-  p.parts = (chunks + p.chunks - 1) / p.chunks;
-  p.threads = 256;
-  return p;
 }
 
 hipError_t launch_distill_grad(const DistillArgs& a) {

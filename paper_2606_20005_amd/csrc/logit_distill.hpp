@@ -35,7 +35,6 @@
 
 namespace streamkl {
 
-constexpr int kMostMarks = 33792;        // chunks of a part
 constexpr double kLeastRest = 0x1p-24;   // of the teacher's mass outside its list: less is the rounding of its t_k
 static_assert(kMostList == 128, "a wave holds a list in two entries a lane");
 

@@ -169,19 +169,15 @@ void run(const DistillArgs& a) {
   const long long rows = (long long)a.rows.B * a.rows.N;
   if (a.rest)
     distill_step_kernel<T, THREADS, HELD, true, waves>
-        <<<logit_grid(rows), dim3(THREADS), (size_t)(chunks_of(a.rows.V, a.rows.dtype) + 3) / 4 * 4, a.stream>>>(a);
+        <<<logit_grid(rows), dim3(THREADS), (size_t)(chunks_of(a.rows.V, a.rows.dtype == STREAMKL_F32) + 3) / 4 * 4, a.stream>>>(a);
   else
     distill_step_kernel<T, THREADS, HELD, false, waves><<<logit_grid(rows), dim3(THREADS), 0, a.stream>>>(a);
 }
 
 }  // namespace
 
-bool distill_step_fits(long long rows, int V, int dtype) {
-  return rows >= 128 && chunks_of(V, dtype) <= kMostMarks;
-}
-
 hipError_t launch_distill_step(const DistillArgs& a) {
-  const int chunks = chunks_of(a.rows.V, a.rows.dtype);
+  const int chunks = chunks_of(a.rows.V, a.rows.dtype == STREAMKL_F32);
   by_type(a.rows.dtype, [&](auto t) {
     using T = decltype(t);
     if (chunks <= 1024)

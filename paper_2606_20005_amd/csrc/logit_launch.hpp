@@ -25,6 +25,78 @@ struct LogitPlan {
   int threads, parts, chunks;
 };
 
+constexpr int kGroup = 16;             // logits of a group, whose maximum is kept
+constexpr int kMostGroups = 8448;      // of a part with alternatives: 135168 logits
+constexpr int kMostMarks = 33792;      // chunks of a part with marks
+
+// The most 16-byte chunks that a row of any alignment has.
+inline int chunks_of(int V, bool f32) {
+  const int epc = f32 ? 4 : 8;
+  return (V + epc - 1 + epc - 1) / epc;
+}
+
+// A row in parts of a multiple of 4 chunks.
+inline LogitPlan cut(int chunks, long long parts) {
+  LogitPlan p;
+  p.chunks = (int)((chunks + parts - 1) / parts + 3) / 4 * 4;
+  p.parts = (chunks + p.chunks - 1) / p.chunks;
+  p.threads = 256;
+  return p;
+}
+
+// Forward passes: a workgroup a row; two a CU where rows are fewer, as long as a part has 8192 logits, and no more chunks
+// in a part than its workgroup's LDS has room for.
+inline LogitPlan forward_plan(long long rows, int V, bool f32, int most_chunks) {
+  const int epc = f32 ? 4 : 8, chunks = chunks_of(V, f32);
+  long long parts = rows ? 512 / rows : 1;
+  const long long useful = ((long long)V + 8191) / 8192, least = ((long long)chunks + most_chunks - 1) / most_chunks;
+  if (parts > useful) parts = useful;
+  if (parts < least) parts = least;
+  if (parts < 1) parts = 1;
+  if (parts > kMostParts) parts = kMostParts;
+  LogitPlan p = cut(chunks, parts);
+  if ((long long)p.chunks * epc > 16384) p.threads = 512;
+  return p;
+}
+
+inline LogitPlan logprob_plan(long long rows, int V, bool f32, int top) {
+  return forward_plan(rows, V, f32, top > 0 ? kMostGroups * kGroup / (f32 ? 4 : 8) : 1 << 30);
+}
+
+inline LogitPlan distill_plan(long long rows, int V, bool f32, bool rest) {
+  return forward_plan(rows, V, f32, rest ? kMostMarks : 1 << 30);
+}
+
+// Backward passes: parts of at most 32768 logits.
+inline LogitPlan grad_plan(int V, bool f32) { return cut(chunks_of(V, f32), ((long long)V + 32767) / 32768); }
+
+// The sums of a part.
+struct LogprobPart {
+  float r, l, a;
+};
+struct DistillPart {
+  float r, l;
+};
+
+// Sums of all parts, then their keys.
+__host__ __device__ inline size_t logprob_part_bytes(long long rows, const LogitPlan& p) {
+  return ((size_t)rows * p.parts * sizeof(LogprobPart) + 15) / 16 * 16;
+}
+inline size_t logprob_workspace(long long rows, const LogitPlan& p, int top) {
+  return p.parts <= 1 ? 0 : logprob_part_bytes(rows, p) + (size_t)rows * p.parts * top * 8;
+}
+inline size_t distill_workspace(long long rows, const LogitPlan& p) {
+  return p.parts <= 1 ? 0 : (size_t)rows * p.parts * sizeof(DistillPart);
+}
+
+// Whether a distillation step runs as one kernel, a workgroup a row, or as a forward and a backward pass in parts: for few
+// long rows parts fill the chip (one kernel and three, us: 4096 logits, 1 row 8.8 and 12.7; 32000, 1 row 15.5 and 19.4;
+// 128000, 16 rows 25 and 21, 64 rows 25.8 both, 128 rows 28 and 34; 262144, 128 rows 61 and 49, 256 rows 68 and 81).
+inline bool distill_step_fits(long long rows, int V, bool f32) {
+  const int chunks = chunks_of(V, f32);
+  return chunks <= kMostMarks && (chunks <= 8192 || rows * 128 >= chunks);
+}
+
 // A grid of n workgroups: an axis holds less than 2^32 threads.
 inline dim3 logit_grid(long long n) {
   constexpr long long most = 1 << 21;
@@ -87,19 +159,12 @@ struct DistillArgs {
   hipStream_t stream;
 };
 
-LogitPlan logprob_plan(long long rows, int V, int dtype, int top);
-size_t logprob_workspace(long long rows, const LogitPlan& p, int top);
 hipError_t launch_logprob(const LogprobArgs& a);
-LogitPlan logprob_grad_plan(long long rows, int V, int dtype);
 hipError_t launch_logprob_grad(const LogprobGradArgs& a);
 
-LogitPlan distill_plan(long long rows, int V, int dtype, int rest);
-size_t distill_workspace(long long rows, const LogitPlan& p);
 hipError_t launch_distill(const DistillArgs& a);
-LogitPlan distill_grad_plan(long long rows, int V, int dtype);
 hipError_t launch_distill_grad(const DistillArgs& a);
 // Loss and gradient in one kernel, for sizes that it holds.
-bool distill_step_fits(long long rows, int V, int dtype);
 hipError_t launch_distill_step(const DistillArgs& a);
 hipError_t launch_weighted_sum(const float* loss, const float* weight, float factor, long long rows, float* total,
                                hipStream_t stream);

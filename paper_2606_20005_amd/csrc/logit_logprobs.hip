@@ -30,8 +30,6 @@ namespace streamkl {
 namespace {
 
 constexpr int kUnroll = 4;
-constexpr int kGroup = 16;                         // logits of a group
-constexpr int kMostGroups = 8448;                  // of a part: 135168 logits
 constexpr int kMostHits = 512, kMostCands = 2048;  // kMostTop groups hold at most kMostCands logits
 static_assert(kMostTop * kGroup <= kMostCands && kMostTop <= kMostHits, "");
 
@@ -185,10 +183,6 @@ __device__ __forceinline__ void rank_candidates(const TopShared<T>& sh, int top,
   }
 }
 
-struct Part {
-  float r, l, a;
-};
-
 // What a row's sums come to. Log probabilities are formed from the distance to the reference: a log-sum-exp near the
 // type's lowest value would swallow them.
 struct RowEnd {
@@ -294,10 +288,10 @@ logprob_kernel(LogprobArgs a) {
     }
   } else {
     const long long i = (long long)r * a.plan.parts + s;
-    if (tid == 0) static_cast<Part*>(a.workspace)[i] = Part{sums.r, sums.l, sums.a};
+    if (tid == 0) static_cast<LogprobPart*>(a.workspace)[i] = LogprobPart{sums.r, sums.l, sums.a};
     if constexpr (TOP) {
-      const long long all = (long long)a.rows.B * a.rows.N * a.plan.parts;
-      u64* keys = reinterpret_cast<u64*>(static_cast<char*>(a.workspace) + (all * sizeof(Part) + 15) / 16 * 16) + i * top;
+      u64* keys = reinterpret_cast<u64*>(static_cast<char*>(a.workspace) +
+                                         logprob_part_bytes((long long)a.rows.B * a.rows.N, a.plan)) + i * top;
       for (int q = sh.cands + tid; q < top; q += THREADS) keys[q] = 0;   // ranks behind any logit
       rank_candidates<T, THREADS>(sh, top, [&](int rank, u64 k) { keys[rank] = k; });
     }
@@ -322,9 +316,9 @@ logprob_join_kernel(LogprobArgs a) {
   if (!grid_place((long long)a.rows.B * a.rows.N, 1, &r, &s)) return;
   const int tid = threadIdx.x, parts = a.plan.parts, top = a.top, n = parts * top;
   const float c = a.scale * kLog2e;
-  const long long all = (long long)a.rows.B * a.rows.N * parts;
   const u64* const from =
-      reinterpret_cast<const u64*>(static_cast<const char*>(a.workspace) + (all * sizeof(Part) + 15) / 16 * 16) +
+      reinterpret_cast<const u64*>(static_cast<const char*>(a.workspace) +
+                                   logprob_part_bytes((long long)a.rows.B * a.rows.N, a.plan)) +
       (long long)r * n;
   if (tid < 64) {
     const int b = r / a.rows.N;
@@ -332,7 +326,7 @@ logprob_join_kernel(LogprobArgs a) {
     Sums sums;
     u64 least = ~0ull;
     if (tid < parts) {
-      const Part p = static_cast<const Part*>(a.workspace)[(long long)r * parts + tid];
+      const LogprobPart p = static_cast<const LogprobPart*>(a.workspace)[(long long)r * parts + tid];
       sums.r = p.r;
       sums.l = p.l;
       sums.a = p.a;
@@ -476,29 +470,6 @@ void run_fwd(const LogprobArgs& a, dim3 grid) {
 
 }  // namespace
 
-LogitPlan logprob_plan(long long rows, int V, int dtype, int top) {
-  const int epc = dtype == STREAMKL_F32 ? 4 : 8, chunks = chunks_of(V, dtype);
-  // two workgroups a CU where that leaves a part 8192 logits; a part's group maxima have to fit
-  long long parts = rows ? 512 / rows : 1;
-  const long long useful = ((long long)V + 8191) / 8192;
-  if (parts > useful) parts = useful;
-  const long long least = top > 0 ? ((long long)chunks * epc + kMostGroups * kGroup - 1) / (kMostGroups * kGroup) : 1;
-  if (parts < least) parts = least;
-  if (parts < 1) parts = 1;
-  if (parts > kMostParts) parts = kMostParts;
-  LogitPlan p;
-  p.chunks = (int)((chunks + parts - 1) / parts + 3) / 4 * 4;
-  p.parts = (chunks + p.chunks - 1) / p.chunks;
-  p.threads = (long long)p.chunks * epc <= 16384 ? 256 : 512;
-  return p;
-}
-
-size_t logprob_workspace(long long rows, const LogitPlan& p, int top) {
-  if (p.parts <= 1) return 0;
-  const size_t all = (size_t)rows * p.parts;
-  return (all * sizeof(Part) + 15) / 16 * 16 + all * top * sizeof(u64);
-}
-
 hipError_t launch_logprob(const LogprobArgs& a) {
   const long long rows = (long long)a.rows.B * a.rows.N;
   const dim3 grid = logit_grid(rows * a.plan.parts);
@@ -511,16 +482,6 @@ hipError_t launch_logprob(const LogprobArgs& a) {
   if (a.plan.parts > 1)
     logprob_join_kernel<<<logit_grid(rows), dim3(kJoinThreads), a.plan.parts * a.top * sizeof(u64), a.stream>>>(a);
   return hipGetLastError();
-}
-
-LogitPlan logprob_grad_plan(long long rows, int V, int dtype) {
-  const int chunks = chunks_of(V, dtype);
-  const long long parts = ((long long)V + 32767) / 32768;
-  LogitPlan p;
-  p.chunks = (int)((chunks + parts - 1) / parts + 3) / 4 * 4;
-  p.parts = (chunks + p.chunks - 1) / p.chunks;
-  p.threads = 256;
-  return p;
 }
 
 hipError_t launch_logprob_grad(const LogprobGradArgs& a) {

@@ -300,12 +300,6 @@ __device__ __forceinline__ bool grid_place(long long rows, int parts, int* r, in
 // Host side
 // ---------------------------------------------------------------------------
 
-// The most chunks that a row of any alignment has.
-inline int chunks_of(int V, int dtype) {
-  const int epc = dtype == STREAMKL_F32 ? 4 : 8;
-  return (V + epc - 1 + epc - 1) / epc;
-}
-
 // f(element) with a value of the type
 template <typename F>
 inline void by_type(int dtype, F f) {

@@ -1011,10 +1011,14 @@ def token_logprobs_fwd(logits, tokens=None, scale=1.0, top=0, entropy=True, save
     top = int(top)
     if not 0 <= top <= V:
         raise ValueError(f"top must be 0 to the vocabulary's {V}, got {top}")
-    row = lambda dtype=torch.float32, last=(): torch.empty((*shape, *last), dtype=dtype, device=dev)   # noqa: E731
-    lse = row()
-    logp, ent, err = (row() if want else None for want in (tokens is not None, entropy, save))
-    top_logp, top_ids = (row(last=(top,)), row(torch.int32, (top,))) if top else (None, None)
+    # the rows' numbers from one allocation (1.5 us each)
+    want = (True, tokens is not None, bool(entropy), save)
+    made = iter(torch.empty((sum(want), *shape), dtype=torch.float32, device=dev).unbind(0))
+    lse, logp, ent, err = (next(made) if w else None for w in want)
+    top_logp = top_ids = None
+    if top:
+        top_logp = torch.empty((*shape, top), dtype=torch.float32, device=dev)
+        top_ids = torch.empty((*shape, top), dtype=torch.int32, device=dev)
     ws_bytes = 0
     if workspace is not None:
         ws_bytes = _workspace(workspace, dev)
