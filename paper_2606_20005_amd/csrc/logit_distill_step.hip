@@ -2,12 +2,19 @@
 // (streamkl_topk_distill_step); logit_distill.hpp has the mathematics.
 //
 // The upstream gradients are known beforehand, so a workgroup that has the sums
-// of a row can write its gradient at once, and it still holds the row: a thread
-// keeps HELD chunks of 16 bytes in registers, THREADS * HELD of them a
-// workgroup (half of a CU's registers at 1024 * 16, 131072 logits of 2 bytes).
-// Chunks beyond that are read again, out of the cache as a rule. So a logit is
-// read once and its gradient written, where a forward and a backward pass read
-// it twice: two thirds of the bytes.
+// of a row can write its gradient at once, and it still holds (much of) the
+// row: a thread keeps HELD chunks of 16 bytes in registers. Chunks beyond that
+// are read again out of the cache, the last ones first. So a logit is read from
+// memory once and its gradient written, where a forward and a backward pass
+// read it twice: two thirds of the bytes. Bound: HBM.
+//
+// A CU holds two workgroups of 512 threads, 8192 chunks each, so that one reads
+// while the other finishes its row or writes. At 8192 x 128000 bf16, 64 entries
+// (4.2 GB, 807 us at the rate of a large copy): 828 us; in two passes 1279 us;
+// one workgroup of 1024 threads that holds the whole row 1024 us; four of 256
+// 960 us; 512 threads of 8 chunks 873 us; gradients kept in the caches 932 us;
+// the chunks read again first to last 868 us. At 8192 x 262144 (three quarters
+// read again, 1652 us) 1813 us.
 //
 // All loads of a row are issued before its list is read; the teacher's side is
 // formed by one wave while they are on their way. Whole chunks only are held;
@@ -104,11 +111,16 @@ distill_step_kernel(DistillArgs a) {
         sum(first + tid, raw, first + kTurn * THREADS <= c1);
       }
     }
-    for (int first = c0 + HELD * THREADS; first < c1; first += kTurn * THREADS) {
-      u32x4 raw[kTurn];
+    constexpr int ahead = 4;   // turns whose loads are in flight
+    for (int first = c0 + HELD * THREADS; first < c1; first += ahead * kTurn * THREADS) {
+      u32x4 raw[ahead][kTurn];
 #pragma unroll
-      for (int j = 0; j < kTurn; ++j) raw[j] = row.chunk[min(first + j * THREADS + tid, c1 - 1)];
-      sum(first + tid, raw, first + kTurn * THREADS <= c1);
+      for (int j = 0; j < ahead * kTurn; ++j) raw[j / kTurn][j % kTurn] = row.chunk[min(first + j * THREADS + tid, c1 - 1)];
+#pragma unroll
+      for (int h = 0; h < ahead; ++h) {
+        const int at = first + h * kTurn * THREADS;
+        if (at < c1) sum(at + tid, raw[h], at + kTurn * THREADS <= c1);
+      }
     }
     {
       const int at = mine + ph;
@@ -139,16 +151,20 @@ distill_step_kernel(DistillArgs a) {
         for (int i = 0; i < E; ++i) f[i] = exp2_fast((f[i] - at) * c) * w;
         if (ch < c1) store_chunk(dx + ((long long)ch * E - ph), pack<T>(f));
       };
+      // the chunks that were read last first: they are in the nearest cache
+      constexpr int back = 8;
+      const int held_to = c0 + HELD * THREADS, turns = (c1 - held_to + back * THREADS - 1) / (back * THREADS);
+      for (int t = turns - 1; t >= 0; --t) {
+        const int first = held_to + t * back * THREADS;
+        u32x4 raw[back];
+#pragma unroll
+        for (int j = back - 1; j >= 0; --j) raw[j] = row.chunk[min(first + j * THREADS + tid, c1 - 1)];
+#pragma unroll
+        for (int j = back - 1; j >= 0; --j) put(first + j * THREADS + tid, raw[j]);
+      }
 #pragma unroll
       for (int j = 0; j < HELD; ++j)
         if (c0 + j * THREADS < c1) put(c0 + j * THREADS + tid, held[j]);
-      for (int first = c0 + HELD * THREADS; first < c1; first += kTurn * THREADS) {
-        u32x4 raw[kTurn];
-#pragma unroll
-        for (int j = 0; j < kTurn; ++j) raw[j] = row.chunk[min(first + j * THREADS + tid, c1 - 1)];
-#pragma unroll
-        for (int j = 0; j < kTurn; ++j) put(first + j * THREADS + tid, raw[j]);
-      }
       if (mine >= 0) dx[mine] = (T)(exp2_fast((edge - at) * c) * w);
       for (int k = head[tid]; k >= 0; k = next[k]) dx[list.id[k]] = (T)list.value[k];
       return;
