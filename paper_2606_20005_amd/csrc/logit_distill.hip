@@ -34,27 +34,19 @@ distill_kernel(DistillArgs a) {
   Sums sums;
   if (list.some) {   // a row without a list has no loss, whatever its logits
     const unsigned char* const mark = reinterpret_cast<const unsigned char*>(marks);
-    each_turn<T, THREADS, kUnroll>(row, c0, c1, [&](int at, const u32x4(&raw)[kUnroll]) {
-      float f[kUnroll][kEpc<T>], mx[kUnroll];
-      u32 m[kUnroll] = {}, any = 0;
+    each_turn<T, THREADS, kUnroll, true>(row, c0, c1, [&](int at, const auto& turn) {
+      constexpr int N = std::decay_t<decltype(turn)>::N;
+      float f[N][kEpc<T>], mx[N];
 #pragma unroll
-      for (int j = 0; j < kUnroll; ++j) {
+      for (int j = 0; j < N; ++j) {
+        unpack<T>(turn.raw[j], f[j]);
         if constexpr (REST) {
           const int ch = at + j * THREADS;
-          m[j] = ch < c1 ? mark[ch - c0] : 0;
-          any |= m[j];
+          leave_out(f[j], ch < c1 ? mark[ch - c0] : 0u);
         }
-        unpack<T>(raw[j], f[j]);
+        mx[j] = max_of<T>(f[j]);
       }
-      if (REST && __any(any != 0)) {
-#pragma unroll
-        for (int j = 0; j < kUnroll; ++j)
-#pragma unroll
-          for (int e = 0; e < kEpc<T>; ++e) f[j][e] = (m[j] >> e) & 1 ? kNegInf : f[j][e];
-      }
-#pragma unroll
-      for (int j = 0; j < kUnroll; ++j) mx[j] = max_of<T>(f[j]);
-      sums.expect(vmax(vmax3(mx[0], mx[1], mx[2]), mx[3]), c, rise);
+      sums.expect(max_all(mx), c, rise);
       sums.template add<false>(f, c);
     });
   }
@@ -94,7 +86,7 @@ distill_join_kernel(DistillArgs a) {
   __syncthreads();
   teacher_side(a, list);
   __syncthreads();
-  sums = wave_join(sums, a.s2 * kLog2e);
+  sums = lanes_join<64>(sums, a.s2 * kLog2e);
   float loss;
   const DistillStats st = finish_row(a, sums, list, &loss);
   if (threadIdx.x == 0) {
@@ -130,12 +122,12 @@ __device__ __forceinline__ void part_gradients(const DistillArgs& a, int r, int 
     listed_gradients(a, st, g, list);
   }
   const float c = a.s2 * kLog2e, at = st.r, w = (float)((double)a.s2 * (double)g * st.rest);
-  each_turn<T, THREADS, kUnroll>(row, c0, c1, [&](int first, const u32x4(&raw)[kUnroll]) {
+  each_turn<T, THREADS, kUnroll, false>(row, c0, c1, [&](int first, const auto& turn) {
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
+    for (int j = 0; j < std::decay_t<decltype(turn)>::N; ++j) {
       const int ch = first + j * THREADS;
       float f[kEpc<T>];
-      unpack<T>(raw[j], f);
+      unpack<T>(turn.raw[j], f);
 #pragma unroll
       for (int i = 0; i < kEpc<T>; ++i) f[i] = exp2_fast((f[i] - at) * c) * w;
       if (ch < c1) store<T>(row, dx, ch, f);

@@ -84,23 +84,19 @@ distill_step_kernel(DistillArgs a) {
     // kTurn chunks of this thread, the first one ch, the others THREADS apart; those from c1 on are none
     auto sum = [&](int ch, const u32x4(&raw)[kTurn], bool all) {
       float f[kTurn][E], mx[kTurn];
-      u32 m[kTurn], any = 0;
 #pragma unroll
       for (int j = 0; j < kTurn; ++j) {
         const bool there = all || ch + j * THREADS < c1;
-        m[j] = there ? (REST ? mark[ch + j * THREADS] : 0) : (1u << E) - 1;
-        any |= m[j];
         unpack<T>(raw[j], f[j]);
+        if constexpr (REST) {
+          leave_out(f[j], there ? mark[ch + j * THREADS] : (1u << E) - 1);
+        } else if (!all) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[j][e] = there ? f[j][e] : kNegInf;
+        }
+        mx[j] = max_of<T>(f[j]);
       }
-      if ((REST || !all) && __any(any != 0)) {
-#pragma unroll
-        for (int j = 0; j < kTurn; ++j)
-#pragma unroll
-          for (int e = 0; e < E; ++e) f[j][e] = (m[j] >> e) & 1 ? kNegInf : f[j][e];
-      }
-#pragma unroll
-      for (int j = 0; j < kTurn; ++j) mx[j] = max_of<T>(f[j]);
-      sums.expect(vmax(mx[0], mx[1]), c, rise);
+      sums.expect(max_all(mx), c, rise);
       sums.template add<false>(f, c);
     };
 #pragma unroll

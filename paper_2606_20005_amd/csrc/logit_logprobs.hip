@@ -248,19 +248,20 @@ logprob_kernel(LogprobArgs a) {
   const float c = a.scale * kLog2e, rise = kRise / c;
   Sums sums;
   float most = kNegInf;
-  each_turn<T, THREADS, kUnroll>(row, c0, c1, [&](int at, const u32x4(&raw)[kUnroll]) {
-    float f[kUnroll][kEpc<T>], mx[kUnroll];
+  each_turn<T, THREADS, kUnroll, true>(row, c0, c1, [&](int at, const auto& turn) {
+    constexpr int N = std::decay_t<decltype(turn)>::N;
+    float f[N][kEpc<T>], mx[N];
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      unpack<T>(raw[j], f[j]);
+    for (int j = 0; j < N; ++j) {
+      unpack<T>(turn.raw[j], f[j]);
       mx[j] = max_of<T>(f[j]);
     }
-    const float mm = vmax(vmax3(mx[0], mx[1], mx[2]), mx[3]);
+    const float mm = max_all(mx);
     if constexpr (TOP) {
       most = vmax(most, mm);
       constexpr int CPG = kGroup / kEpc<T>;   // lanes that share a group
 #pragma unroll
-      for (int j = 0; j < kUnroll; ++j) {
+      for (int j = 0; j < N; ++j) {
         float g = vmax(mx[j], quad_swap<kXor1>(mx[j]));
         if constexpr (CPG == 4) g = vmax(g, quad_swap<kXor2>(g));
         const int ch = at + j * THREADS;
@@ -338,7 +339,7 @@ logprob_join_kernel(LogprobArgs a) {
       const u64 o = (u64)__shfl_xor((long long)least, m);
       least = o < least ? o : least;
     }
-    sums = wave_join(sums, c);
+    sums = lanes_join<64>(sums, c);
     if (tid == 0) {
       joined[0] = sums.r;
       joined[1] = sums.l;
@@ -429,12 +430,12 @@ logprob_grad_kernel(LogprobGradArgs a) {
     for (int ch = c0 + threadIdx.x; ch < c1; ch += THREADS) store<T>(row, dx, ch, z);
     return;
   }
-  each_turn<T, THREADS, kUnroll>(row, c0, c1, [&](int first, const u32x4(&raw)[kUnroll]) {
+  each_turn<T, THREADS, kUnroll, false>(row, c0, c1, [&](int first, const auto& turn) {
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
+    for (int j = 0; j < std::decay_t<decltype(turn)>::N; ++j) {
       const int ch = first + j * THREADS;
       float f[kEpc<T>];
-      unpack<T>(raw[j], f);
+      unpack<T>(turn.raw[j], f);
 #pragma unroll
       for (int i = 0; i < kEpc<T>; ++i) {
         float u = (f[i] - at) * c;

@@ -159,3 +159,22 @@ def test_the_largest_vocabulary(gpu_lib, R, dtype):
     half = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}[dtype]
     assert abs(float(loss[-1]) - value[0]) <= bound[0]
     assert (np.abs(np64(dx[-1]) - g[0]) <= gb[0] + half * np.abs(g[0])).all()
+
+
+def test_more_rows_than_an_axis_of_the_grid(gpu_lib):
+    R, V = (1 << 21) + 5, 9
+    x = torch.zeros((R, V), device="cuda")
+    x[-5:] = normal(5, V, seed=12)
+    t = torch.full((R,), 3, dtype=torch.int32, device="cuda")
+    y, err = gpu_lib.token_logprobs_fwd(x, t, top=2, save=True)
+    small = gpu_lib.token_logprobs(x[-5:].clone(), t[:5], top=2)
+    for a, b in zip(y, small):
+        assert torch.equal(a[-5:], b)
+    up = torch.ones(R, device="cuda")
+    dx = gpu_lib.token_logprobs_bwd(x, t, y.lse, err, dlogp=up)
+    ref, bound = lo.token_logprobs_grad(np64(x[-5:]), np.full(5, 3), 1.0, np.ones(5), None, None)
+    assert (np.abs(np64(dx[-5:]) - ref) <= bound + 2.0 ** -24 * np.abs(ref)).all() and torch.equal(dx[0], dx[1 << 21])
+    ids, v = y.top_ids, y.top_logp
+    loss, _, g = gpu_lib.topk_distill_step(x, ids, v)
+    few, _, h = gpu_lib.topk_distill_step(x[-5:].clone(), ids[-5:].clone(), v[-5:].clone())
+    assert torch.equal(loss[-5:], few) and torch.equal(g[-5:], h) and torch.equal(g[0], g[1 << 21])
