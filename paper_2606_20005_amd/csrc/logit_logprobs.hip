@@ -262,8 +262,8 @@ logprob_kernel(LogprobArgs a) {
       constexpr int CPG = kGroup / kEpc<T>;   // lanes that share a group
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        float g = vmax(mx[j], quad_swap<kXor1>(mx[j]));
-        if constexpr (CPG == 4) g = vmax(g, quad_swap<kXor2>(g));
+        float g = vmax_xor1(mx[j]);
+        if constexpr (CPG == 4) g = vmax_xor2(g);
         const int ch = at + j * THREADS;
         if (ch < c1 && tid % CPG == 0) sh.group[(ch - c0) / CPG] = (T)g;
       }

@@ -37,7 +37,9 @@ constexpr float kRise = 4.f;
 constexpr float kFloor = -1000.f;
 constexpr float kNoRef = -3.402823466e38f;   // reference of a lane that has seen nothing but -inf, or only this value
 
-// v_max_f32, v_max3_f32 without the instructions that quiet signalling NaN (a NaN loses against a number)
+// v_max_f32, v_max3_f32 without the instructions that quiet signalling NaN (a NaN loses against a number). The compiler does
+// not see vector instructions in these: what it inserts waits for between two of its own must not follow one or precede it.
+// So their operands come from no transcendental instruction, and their results go into no cross-lane operand of another.
 __device__ __forceinline__ float vmax(float a, float b) {
   float r;
   asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
@@ -49,11 +51,17 @@ __device__ __forceinline__ float vmax3(float a, float b, float c) {
   return r;
 }
 
-// Lane l receives the value of lane l ^ 1 (kXor1), l ^ 2 (kXor2).
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E;
-template <int CTRL>
-__device__ __forceinline__ float quad_swap(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+// max of a lane's value and that of lane l ^ 1, l ^ 2. A cross-lane operand may be read two wait states after a vector
+// instruction has written it; s_nop 1 is these two.
+__device__ __forceinline__ float vmax_xor1(float v) {
+  float r;
+  asm("s_nop 1\n\tv_max_f32_dpp %0, %1, %1 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf" : "=v"(r) : "v"(v));
+  return r;
+}
+__device__ __forceinline__ float vmax_xor2(float v) {
+  float r;
+  asm("s_nop 1\n\tv_max_f32_dpp %0, %1, %1 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf" : "=v"(r) : "v"(v));
+  return r;
 }
 
 // Elements of a type and of the chunks it comes in.
@@ -237,7 +245,12 @@ struct Sums {
   }
 };
 
-// The sums of every WIDTH lanes, in each of them.
+__device__ __forceinline__ float first_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
+// The sums of the first WIDTH lanes of a wave, those of other WIDTH lanes being the same where WIDTH < 64, in every lane. It
+// is the first lane's result: those of the others may be off by a rounding, where a product is fused into one addend.
 template <int WIDTH>
 __device__ __forceinline__ Sums lanes_join(Sums s, float c) {
   float m = s.r;
@@ -249,6 +262,9 @@ __device__ __forceinline__ Sums lanes_join(Sums s, float c) {
     s.l += __shfl_xor(s.l, i);
     s.a += __shfl_xor(s.a, i);
   }
+  s.r = first_lane(s.r);
+  s.l = first_lane(s.l);
+  s.a = first_lane(s.a);
   return s;
 }
 
