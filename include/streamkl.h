@@ -601,7 +601,8 @@ typedef struct {
  *             logits of -inf), that bucket is left out. A token that is listed twice counts with both entries.
  *   rest = 0: L = sum_k p_k (log p_k - log q_k), STREAMKL_KL_FWD only (STREAMKL_KL_REV: STREAMKL_ERR_UNSUPPORTED).
  * A row without entries, and an empty row, has L = 0 and zero gradients. A listed token of probability 0 gives L = +inf, as
- * the definition does (REV: a value of -inf does).
+ * the definition does; in STREAMKL_KL_REV a value of -inf does, and the row's gradients are not finite then. With rest = 0 a
+ * list of nothing but -inf is no distribution: NaN.
  *   workspace as above, at least streamkl_topk_distill_workspace_bytes bytes.
  *   loss      float32 [B, N].
  *   stats     32 bytes a row, 8-byte aligned: what the backward pass reads.
