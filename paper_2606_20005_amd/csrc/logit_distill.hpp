@@ -228,7 +228,7 @@ __device__ __forceinline__ DistillStats finish_row(const DistillArgs& a, const S
 __device__ __forceinline__ void listed_gradients(const DistillArgs& a, const DistillStats& st, float g, List& list) {
   const int lane = threadIdx.x & 63;
   const double s2 = (double)a.s2;
-  double v[2];
+  double base[2], v[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int k = lane + 64 * i;
@@ -238,14 +238,17 @@ __device__ __forceinline__ void listed_gradients(const DistillArgs& a, const Dis
     // what the entry adds to its token: forward -p, reverse q (r + 1)
     const double add = a.reverse ? (q == 0.0 ? 0.0 : q * (lq - list.lp[k] + 1.0)) : -(double)list.p[k];
     list.add[k] = (float)add;
-    v[i] = (a.reverse ? (q == 0.0 ? 0.0 : -q * st.total) : q * st.total) + add;
+    base[i] = a.reverse ? (q == 0.0 ? 0.0 : -q * st.total) : q * st.total;
+    v[i] = base[i] + add;
   }
   wave_fence();
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int k = lane + 64 * i, id = list.id[k];
-    if (list.twice && id >= 0)
-      for (int j = 0; j < a.K; ++j) v[i] += list.id[j] == id && j != k ? (double)list.add[j] : 0.0;
+    if (list.twice && id >= 0) {   // the entries of one token all come to the same value: any of them may be written last
+      v[i] = base[i];
+      for (int j = 0; j < a.K; ++j) v[i] += list.id[j] == id ? (double)list.add[j] : 0.0;
+    }
     list.value[k] = (float)(v[i] * (s2 * (double)g));
   }
 }

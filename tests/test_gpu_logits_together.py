@@ -59,6 +59,22 @@ def test_results_are_reproducible(gpu_lib, B, N, V):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("direction", ["fwd", "rev"])
+@pytest.mark.parametrize("R", [3, 500])
+def test_a_token_with_many_entries_is_reproducible(gpu_lib, R, direction):
+    """Whichever of its entries is written last."""
+    V, K = 70001, 96
+    x = normal(R, V, seed=14)
+    ids = torch.randint(0, 9, (R, K), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) * 7001
+    t = torch.log_softmax(normal(R, K + 1, seed=15), -1)[:, :K].contiguous()
+    loss, stats, first = gpu_lib.topk_distill_step(x, ids, t, direction=direction)
+    back = gpu_lib.topk_distill_bwd(x, ids, t, stats, direction=direction)
+    for _ in range(8):
+        again = gpu_lib.topk_distill_step(x, ids, t, direction=direction)
+        assert torch.equal(again[0], loss) and torch.equal(again[2], first)
+        assert torch.equal(gpu_lib.topk_distill_bwd(x, ids, t, stats, direction=direction), back)
+
+
 @pytest.mark.parametrize("B,N,V", [(1, 2, 60001), (2, 100, 3001)])
 def test_captured_and_replayed(gpu_lib, B, N, V):
     """Two graphs with workspaces of their own, replayed with eager work and other inputs in between."""
