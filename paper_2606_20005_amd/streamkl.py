@@ -1275,8 +1275,8 @@ def topk_distill_loss(logits, ids, teacher, weight=None, *, s1=1.0, s2=1.0, rest
     mean over all rows. Rows of weight 0 (padding) are left out, whatever they hold.
 
     The weights are known before the losses, so the gradient is formed with them, in the forward call where the logits
-    require one. The backward pass hands it over; for an upstream gradient other than 1 (a loss scale) it forms the
-    gradient anew, rounded once.
+    require one (memory of the logits' size from there on). The backward pass hands it over; for an upstream gradient
+    other than 1 (a loss scale) it forms the gradient anew, rounded once. Under torch.no_grad() only the loss is formed.
     """
     opts = (s1, s2, rest, direction)
     rows = logits.numel() // logits.shape[-1] if isinstance(logits, torch.Tensor) and logits.numel() else 0
