@@ -926,7 +926,8 @@ def diff_attention(q1, k1, q2, k2, v, lam, *, scale=None, causal=False, q_len=No
 
     To capture a training step into a HIP graph, capture it while no eager graph of the same leaves is alive (drop the
     warm-up's outputs first): autograd's accumulation nodes of an eager graph belong to its stream, and torch ends the
-    process where a captured backward meets them. The same holds for qk_norm_rope and attention_kl.
+    process where a captured backward meets them. The same holds for the other autograd
+    functions here.
     """
     scale = _diff_scale(scale, q1.shape[-1])
     if _differentiated(q1, k1, q2, k2, v, lam):
