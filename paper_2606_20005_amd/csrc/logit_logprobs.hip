@@ -466,15 +466,39 @@ logprob_join_kernel(LogprobArgs a) {
   }
 }
 
-// dx of a part of a row.
+// A row's sums (no entropy), in every thread.
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS)
+__device__ __forceinline__ Sums row_sums(const Row<T>& row, float c, float* red) {
+  const float rise = kRise / c;
+  Sums sums;
+  each_turn<T, THREADS, kUnroll, false>(row, 0, row.chunks, [&](int, const auto& turn) {
+    constexpr int N = std::decay_t<decltype(turn)>::N;
+    float f[N][kEpc<T>], mx[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      unpack<T>(turn.raw[j], f[j]);
+      mx[j] = max_of<T>(f[j]);
+    }
+    sums.expect(max_all(mx), c, rise);
+    sums.template add<false>(f, c);
+  });
+  return block_join<THREADS>(sums, c, red);
+}
+
+// dx of a part of a row. A log-sum-exp is what the forward call handed over: its float32 value and what that rounding left
+// off. From kFarLse on the latter is as large as log l itself or larger, and further out it swallows log l whole, while the
+// place of the row's logits cannot be told from lse / scale any more: the sums of such a row are formed again.
+constexpr float kFarLse = 0x1p24f;
+
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 8)
 logprob_grad_kernel(LogprobGradArgs a) {
+  __shared__ float red[3 * THREADS / 64];
   int r, s;
   if (!grid_place((long long)a.rows.B * a.rows.N, a.plan.parts, &r, &s)) return;
   r = a.rows.B * a.rows.N - 1 - r;   // the last rows first: the forward pass left them in the cache
   const Row<T> row(a.rows, r);
-  const int c0 = s * a.plan.chunks, c1 = min(row.chunks, c0 + a.plan.chunks);
+  int c0 = s * a.plan.chunks, c1 = min(row.chunks, c0 + a.plan.chunks);
   const int b = r / a.rows.N;
   T* const dx = static_cast<T*>(a.dx) + b * a.dsb + (r - b * a.rows.N) * a.dsn;
   long long tok = -1;
@@ -482,44 +506,52 @@ logprob_grad_kernel(LogprobGradArgs a) {
     tok = a.tokens64 ? static_cast<const long long*>(a.tokens)[r] : static_cast<const int*>(a.tokens)[r];
   const float g = a.dlogp && tok >= 0 ? a.dlogp[r] : 0.f;
   const float h = a.dentropy ? a.dentropy[r] : 0.f, e = a.dlse ? a.dlse[r] : 0.f;
-  const float lse = a.lse[r];
-  float at = 0.f, p1 = 0.f, p2 = 0.f, hit = 0.f;   // dx_j = p_j (p1 + p2 u_j) + (j == tok) hit, p_j = 2^u_j
+  const float lse = a.lse[r], c = a.scale * kLog2e;
   const bool none = (g == 0.f && h == 0.f && e == 0.f) || lse == kNegInf;
-  if (!none) {
-    const Exponent x(lse, a.lse_err ? a.lse_err[r] : 0.f, a.scale);
-    at = x.at;
-    // log p_j = ln 2 u_j + log f
-    const float H = h == 0.f ? 0.f : a.entropy[r];
-    p1 = a.scale * x.f * (e - g - h * (H + logf(x.f)));
-    p2 = -a.scale * x.f * h * kLn2;
-    hit = a.scale * g;
-    if (tok >= row.V) p1 = __builtin_nanf("");
-  }
-  const float c = a.scale * kLog2e;
-  const int tok_at = tok >= 0 && tok < row.V ? (int)tok + row.ph : -1;
-  const int tok_chunk = tok_at >= 0 ? tok_at / kEpc<T> : -1;
   if (none) {
     float z[kEpc<T>] = {};
     for (int ch = c0 + threadIdx.x; ch < c1; ch += THREADS) store<T>(row, dx, ch, z);
     return;
   }
+  float at, f, log_f;   // p_j = 2^u_j f, u_j = (x_j - at) c
+  if (__builtin_fabsf(lse) < kFarLse) {
+    const Exponent x(lse, a.lse_err ? a.lse_err[r] : 0.f, a.scale);
+    at = x.at;
+    f = x.f;
+    log_f = logf(f);
+  } else {   // by the first workgroup alone, the others would write what it reads where dx is x
+    if (s != 0) return;
+    c0 = 0;
+    c1 = row.chunks;
+    const Sums sums = row_sums<T, THREADS>(row, c, red);
+    at = sums.r;
+    f = 1.f / sums.l;
+    log_f = -logf(sums.l);
+  }
+  // dx_j = p_j (p1 + p2 u_j) + (j == tok) hit
+  const float H = h == 0.f ? 0.f : a.entropy[r];
+  float p1 = a.scale * f * (e - g - h * (H + log_f));
+  const float p2 = -a.scale * f * h * kLn2, hit = a.scale * g;
+  if (tok >= row.V) p1 = __builtin_nanf("");
+  const int tok_at = tok >= 0 && tok < row.V ? (int)tok + row.ph : -1;
+  const int tok_chunk = tok_at >= 0 ? tok_at / kEpc<T> : -1;
   each_turn<T, THREADS, kUnroll, false>(row, c0, c1, [&](int first, const auto& turn) {
 #pragma unroll
     for (int j = 0; j < std::decay_t<decltype(turn)>::N; ++j) {
       const int ch = first + j * THREADS;
-      float f[kEpc<T>];
-      unpack<T>(turn.raw[j], f);
+      float d[kEpc<T>];
+      unpack<T>(turn.raw[j], d);
 #pragma unroll
       for (int i = 0; i < kEpc<T>; ++i) {
-        float u = (f[i] - at) * c;
+        float u = (d[i] - at) * c;
         u = u < kFloor ? kFloor : u;
-        f[i] = exp2_fast(u) * __builtin_fmaf(p2, u, p1);
+        d[i] = exp2_fast(u) * __builtin_fmaf(p2, u, p1);
       }
       if (ch == tok_chunk) {
 #pragma unroll
-        for (int i = 0; i < kEpc<T>; ++i) f[i] += i == tok_at % kEpc<T> ? hit : 0.f;
+        for (int i = 0; i < kEpc<T>; ++i) d[i] += i == tok_at % kEpc<T> ? hit : 0.f;
       }
-      if (ch < c1) store<T>(row, dx, ch, f);
+      if (ch < c1) store<T>(row, dx, ch, d);
     }
   });
 }

@@ -301,7 +301,7 @@ __device__ __forceinline__ double log_of(double v) {
 }
 
 // exp(s x - lse) = 2^((x - at) c) f: what a log-sum-exp is for a kernel that forms probabilities, given as its float32
-// value and what the rounding left off.
+// value and what the rounding left off, both moderate (|lse| < 2^24).
 struct Exponent {
   float at, f;
   __device__ __forceinline__ Exponent(float lse, float err, float scale) {

@@ -1,0 +1,50 @@
+"""Rows of logits at the ends of what the operators take: values far from zero, tokens outside the vocabulary, NaN in lists,
+outputs that are edited in place, how exact long sums are."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import logits_oracle as lo
+from test_gpu_token_logprobs import HALF, TINY, logits, near, np64
+
+pytestmark = pytest.mark.gpu
+
+
+def f32(v):
+    """A scale as the kernels hold it."""
+    return float(np.float32(v))
+
+
+def far_rows(V, dtype, seed=0):
+    """Nine rows: of the type's lowest and largest value, of equal values far from zero, of noise around such values (which
+    the type rounds to a few of its numbers), half of the lowest value, and noise."""
+    top = torch.finfo(dtype).max
+    far = (-60000.0, -30000.0, 2.0 ** 14, 2.0 ** 12) if dtype is torch.float16 else (-1e30, -1e12, 2.0 ** 60, 2.0 ** 26)
+    noise = logits(9, V, torch.float32, seed=seed)
+    x = noise.clone()
+    x[0], x[1], x[2], x[3] = -top, top, far[0], far[1]
+    x[4] = far[2]
+    x[4, ::3] = far[2] / 2
+    x[5] += far[3]
+    x[6] -= min(2.0 ** 24, top / 4)
+    x[7, ::2] = -top
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("scale", [1.0, 0.9, 2.0 / 3.0, 0.6, 0.3])
+@pytest.mark.parametrize("V", [5, 1000, 70001])
+def test_gradients_of_rows_far_from_zero(gpu_lib, V, scale, dtype):
+    """The log-sum-exp of such a row does not hold what its probabilities are, nor does any number added to it."""
+    x, scale = far_rows(V, dtype), f32(scale)
+    tokens = torch.tensor([0, 1, V - 1, 2, 0, 3, 4, 2, -1], device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    up = [torch.randn(9, generator=gen, device="cuda") for _ in range(3)]
+    xg = x.clone().requires_grad_(True)
+    y = gpu_lib.token_logprobs(xg, tokens, scale=scale)
+    dx, = torch.autograd.grad((y.logp, y.entropy, y.lse), xg, up)
+    ref, bound = lo.token_logprobs_grad(np64(x), tokens.cpu().numpy(), scale, *(np64(u) for u in up))
+    near(dx, (ref, bound + HALF[dtype] * np.abs(ref) + TINY[dtype]), "dx")
+    z, err = gpu_lib.token_logprobs_fwd(x, tokens, scale, save=True)
+    same = gpu_lib.token_logprobs_bwd(x, tokens, z.lse, err, z.entropy, *up, scale=scale, out=x)   # in place
+    assert same is x and torch.equal(x, dx)
