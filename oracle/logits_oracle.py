@@ -98,8 +98,8 @@ def _row(z, ids, t, s1, rest, reverse):
         p, lp = np.exp(t), t
         pr = max(1.0 - p.sum(), LEAST_REST)
     else:
-        u = s1 * t
-        lp = u - (u.max() + np.log(np.exp(u - u.max()).sum()))
+        u = s1 * (t - t.max())   # an absolute log-sum-exp would swallow what values near the type's lowest one differ by
+        lp = u - np.log(np.exp(u).sum())
         p, pr = np.exp(lp), 0.0
     others = rest and np.isfinite(z[outside]).any()
     qr, lqr, err_r = 0.0, 0.0, 0.0

@@ -110,24 +110,29 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// The teacher's side, by one wave: lp, p, mass and twice.
+// The teacher's side, by one wave: lp, p, mass and twice. Without a rest everything relative to the largest value: an absolute
+// log-sum-exp would swallow log sum of a list near the type's lowest value (which is uniform), in 64 bits too.
 __device__ __forceinline__ void teacher_side(const DistillArgs& a, List& list) {
   const int lane = threadIdx.x & 63;
   bool there[2];
+  float t[2];
   double lp[2];
   double norm = 0.0;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     there[i] = list.id[lane + 64 * i] >= 0;
-    lp[i] = there[i] ? (double)a.s1 * (double)list.t[lane + 64 * i] : 0.0;
+    t[i] = there[i] ? list.t[lane + 64 * i] : kNegInf;
+    lp[i] = (double)t[i];   // with a rest s1 is 1
   }
   if (!a.rest) {
-    const float m = wave_max(fmaxf(there[0] ? (float)lp[0] : kNegInf, there[1] ? (float)lp[1] : kNegInf));
+    const float m = wave_max(fmaxf(t[0], t[1]));
     double sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (there[i]) sum += exp(lp[i] - (double)m);
-    norm = (double)m + log(wave_sum(sum));
+    for (int i = 0; i < 2; ++i) {
+      lp[i] = (double)a.s1 * ((double)t[i] - (double)m);
+      if (there[i]) sum += exp(lp[i]);
+    }
+    norm = log(wave_sum(sum));
   }
   double mass = 0.0;
   bool twice = false;

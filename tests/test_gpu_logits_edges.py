@@ -48,3 +48,33 @@ def test_gradients_of_rows_far_from_zero(gpu_lib, V, scale, dtype):
     z, err = gpu_lib.token_logprobs_fwd(x, tokens, scale, save=True)
     same = gpu_lib.token_logprobs_bwd(x, tokens, z.lse, err, z.entropy, *up, scale=scale, out=x)   # in place
     assert same is x and torch.equal(x, dx)
+
+
+@pytest.mark.parametrize("teacher", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("s1", [1.0, 0.7, 0.3])
+@pytest.mark.parametrize("R", [5, 600])
+def test_teacher_logits_far_from_zero(gpu_lib, R, s1, teacher):
+    """Lists of the type's lowest value are uniform, as rows of it are; lists around a value far from zero."""
+    V, K, s1 = 3001, 7, f32(s1)
+    gen = torch.Generator(device="cuda").manual_seed(R)
+    x = logits(R, V, torch.float32, seed=R)
+    ids = torch.stack([torch.randperm(V, generator=gen, device="cuda")[:K] for _ in range(R)])
+    t = torch.randn(R, K, generator=gen, device="cuda").to(teacher)
+    low = torch.finfo(teacher).min
+    t[0] = low
+    t[1, 2:] = low
+    t[2] = low
+    t[2, 3] = low / 2
+    t[3] = low / 4
+    ids[3, 5:] = -1
+    g = torch.ones(R, device="cuda")
+    xg = x.requires_grad_(True)
+    y = gpu_lib.topk_distill(xg, ids, t, s1=s1, rest=False)
+    dx, = torch.autograd.grad(y, xg, g)
+    loss, lb, ref, db = lo.distill(np64(x), ids.cpu().numpy(), np64(t), s1, 1.0, False, False)
+    near(y, (loss, lb), "loss")
+    near(dx, (ref, db + HALF[torch.float32] * np.abs(ref)), "dx")
+    for bad in (-torch.inf, torch.inf, torch.nan):
+        t[0] = bad   # a list of nothing, or of no numbers, is no distribution
+        y = gpu_lib.topk_distill(x.detach(), ids, t, s1=s1, rest=False)
+        assert torch.isnan(y[0]) and torch.isfinite(y[1:]).all()
