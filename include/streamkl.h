@@ -568,6 +568,7 @@ size_t streamkl_token_logprobs_workspace_bytes(int B, int N, int V, int dtype, i
  *             themselves; entropy is read only with dentropy). A log-sum-exp of 2^24 and more does not hold what the
  *             probabilities are: the sums of such a row are formed again, by one workgroup.
  *   dlogp, dentropy, dlse  float32 [B, N], each may be NULL (zero). dlogp of rows without a token is not read.
+ *             A row with dlogp for a token >= V gets NaN, one without it what the others give.
  *   dx        rows of the element type of x at dx + b dx_sb + n dx_sn that do not overlap, each value rounded once. It may be
  *             x itself, with its strides. Rows whose upstream gradients are all 0 get zeros, whatever x holds.
  */

@@ -532,7 +532,7 @@ logprob_grad_kernel(LogprobGradArgs a) {
   const float H = h == 0.f ? 0.f : a.entropy[r];
   float p1 = a.scale * f * (e - g - h * (H + log_f));
   const float p2 = -a.scale * f * h * kLn2, hit = a.scale * g;
-  if (tok >= row.V) p1 = __builtin_nanf("");
+  if (tok >= row.V && g != 0.f) p1 = __builtin_nanf("");   // entropy and log-sum-exp do not depend on the token
   const int tok_at = tok >= 0 && tok < row.V ? (int)tok + row.ph : -1;
   const int tok_chunk = tok_at >= 0 ? tok_at / kEpc<T> : -1;
   each_turn<T, THREADS, kUnroll, false>(row, c0, c1, [&](int first, const auto& turn) {

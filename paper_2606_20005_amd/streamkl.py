@@ -1087,7 +1087,8 @@ def token_logprobs(logits, tokens=None, *, scale=1.0, top=0, entropy=True):
 
     logits [N, V] or [B, N, V] in bfloat16, float16 or float32, rows anywhere in memory (a vocabulary of any size, a slice
     of a padded one, logits[:, :-1]). tokens: int32 or int64 [N] or [B, N], or None; a negative token is none (padding)
-    and has logp 0, one outside the vocabulary NaN. scale: an inverse temperature. top: 0 to 128.
+    and has logp 0, one outside the vocabulary NaN (and NaN gradients where logp has an upstream gradient). scale: an
+    inverse temperature. top: 0 to 128.
 
     Returns TokenLogprobs: logp, entropy (nats; None unless ``entropy``) and lse = log sum exp(scale logits), float32 of
     the tokens' shape; top_logp (float32) and top_ids (int32) [..., top], descending, the lowest index first among equal

@@ -78,3 +78,24 @@ def test_teacher_logits_far_from_zero(gpu_lib, R, s1, teacher):
         t[0] = bad   # a list of nothing, or of no numbers, is no distribution
         y = gpu_lib.topk_distill(x.detach(), ids, t, s1=s1, rest=False)
         assert torch.isnan(y[0]) and torch.isfinite(y[1:]).all()
+
+
+@pytest.mark.parametrize("which", ["entropy", "lse", "dlogp 0"])
+def test_a_token_outside_the_vocabulary_spoils_its_log_probability_only(gpu_lib, which):
+    """Entropies and log-sum-exps do not depend on the token, nor do their gradients."""
+    V, R = 3001, 6
+    x = logits(R, V, torch.float32, seed=5).requires_grad_(True)
+    tokens = torch.tensor([1, V, V + 7, -1, 1 << 40, 3], device="cuda")
+    out = (1, 2, 4)
+    y = gpu_lib.token_logprobs(x, tokens)
+    one, zero = torch.ones(R, device="cuda"), torch.zeros(R, device="cuda")
+    outputs, up = {"entropy": ((y.entropy,), (one,)), "lse": ((y.lse,), (one,)),
+                   "dlogp 0": ((y.logp, y.entropy), (torch.where(tokens < V, 1.0, 0.0), one))}[which]
+    dx, = torch.autograd.grad(outputs, x, up, retain_graph=True)
+    g = np64(up[0]) if which == "dlogp 0" else None
+    h, e = (None, np.ones(R)) if which == "lse" else (np.ones(R), None)
+    ref, bound = lo.token_logprobs_grad(np64(x), np.where(np64(tokens) < V, np64(tokens), -1).astype(np.int64), 1.0, g, h, e)
+    near(dx, (ref, bound + HALF[torch.float32] * np.abs(ref)), "dx")
+    dx, = torch.autograd.grad((y.logp, y.entropy), x, (one, zero))   # and its own gradient with it
+    bad = torch.isnan(dx).all(-1)
+    assert bad[list(out)].all() and torch.isfinite(dx[[0, 3, 5]]).all()
