@@ -620,7 +620,8 @@ size_t streamkl_topk_distill_workspace_bytes(int B, int N, int V, int dtype, int
  *   dloss     float32 [B, N], or NULL: 1. dfactor: float32 [1] on the device, or NULL: 1.
  *   done_if_one  1: dx already holds the gradient for dfactor[0] = 1 (streamkl_topk_distill_step wrote it), and is left as it
  *             is where dfactor[0] is 1.
- *   dx        as for streamkl_token_logprobs_bwd. Rows with g = 0 get zeros, whatever x holds.
+ *   dx        as for streamkl_token_logprobs_bwd, but not x with done_if_one: it cannot hold the gradient and the logits.
+ *             Rows with g = 0 get zeros, whatever x holds.
  */
 int streamkl_topk_distill_bwd(const streamkl_logits* x, const streamkl_teacher_list* teacher, float scale, int direction,
                               const void* stats, const float* dloss, float factor, const float* dfactor, int done_if_one,

@@ -1162,7 +1162,8 @@ def topk_distill_bwd(logits, ids, teacher, stats, dloss=None, s1=1.0, s2=1.0, re
     """streamkl_topk_distill_bwd: the gradient of the logits, in their type, for the upstream gradients
     dloss (float32 of the rows' shape, None: ones) times factor times dfactor (a float32 tensor of one element, None: 1).
     done_if_one: ``out`` already holds it for dfactor 1 (topk_distill_step) and is left alone then. ``out`` may be a
-    tensor of the logits' shape and type with rows that do not overlap, the logits themselves among them."""
+    tensor of the logits' shape and type with rows that do not overlap, the logits themselves among them (but with
+    done_if_one, where it holds the gradient)."""
     dev, shape, args = _distill_inputs(logits, ids, teacher, s1, s2, rest, direction)
     _distill_stats(stats, shape, dev)
     _row_floats(dloss, shape, dev, "dloss")
@@ -1170,6 +1171,8 @@ def topk_distill_bwd(logits, ids, teacher, stats, dloss=None, s1=1.0, s2=1.0, re
         raise ValueError(f"dfactor must be a float32 tensor of one element on {dev}")
     if done_if_one and (out is None or dfactor is None):
         raise ValueError("done_if_one needs out and dfactor")
+    if done_if_one and out.data_ptr() == logits.data_ptr() and out.numel():
+        raise ValueError("out holds the gradient with done_if_one: the logits must be elsewhere")
     out, sb, sn = _grad_rows(out, logits)
     with _on(dev):
         st = lib.streamkl_topk_distill_bwd(*args, _p(stats), _p(dloss), float(factor), _p(dfactor),

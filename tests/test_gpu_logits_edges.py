@@ -99,3 +99,19 @@ def test_a_token_outside_the_vocabulary_spoils_its_log_probability_only(gpu_lib,
     dx, = torch.autograd.grad((y.logp, y.entropy), x, (one, zero))   # and its own gradient with it
     bad = torch.isnan(dx).all(-1)
     assert bad[list(out)].all() and torch.isfinite(dx[[0, 3, 5]]).all()
+
+
+def test_a_finished_gradient_is_not_in_the_place_of_the_logits(gpu_lib):
+    """An in-place step and then a loss scale: the logits that the second pass would read are gone."""
+    x = logits(4, 300, torch.float32, seed=3)
+    ids = torch.arange(6, dtype=torch.int32, device="cuda").expand(4, 6).contiguous()
+    t = torch.full((4, 6), -2.0, device="cuda")
+    logit = x.clone()
+    loss, stats, dx = gpu_lib.topk_distill_step(logit, ids, t, out=logit)
+    three = torch.full((1,), 3.0, device="cuda")
+    keep = dx.clone()
+    with pytest.raises(ValueError):
+        gpu_lib.topk_distill_bwd(logit, ids, t, stats, dfactor=three, done_if_one=True, out=logit)
+    assert torch.equal(logit, keep)
+    gpu_lib.topk_distill_bwd(x, ids, t, stats, dfactor=three, done_if_one=True, out=logit)   # from the logits it does
+    near(logit, (3.0 * np64(keep), 2.0 ** -20 * np.abs(3.0 * np64(keep))), "dx")
