@@ -115,3 +115,29 @@ def test_a_finished_gradient_is_not_in_the_place_of_the_logits(gpu_lib):
     assert torch.equal(logit, keep)
     gpu_lib.topk_distill_bwd(x, ids, t, stats, dfactor=three, done_if_one=True, out=logit)   # from the logits it does
     near(logit, (3.0 * np64(keep), 2.0 ** -20 * np.abs(3.0 * np64(keep))), "dx")
+
+
+@pytest.mark.parametrize("N", [3, 700])
+def test_outputs_are_edited_in_place(gpu_lib, N):
+    """Outputs of one call are tensors of their own: editing one neither needs nor touches the others."""
+    x = logits(N, 1000, torch.float32, seed=6).requires_grad_(True)
+    tokens = torch.arange(N, device="cuda") % 1000
+    ref = gpu_lib.token_logprobs(x.detach(), tokens)
+    keep = tokens % 2 == 0
+    y = gpu_lib.token_logprobs(x, tokens)
+    y.logp.masked_fill_(~keep, 0.0)
+    y.logp.mul_(2.0)
+    assert torch.equal(y.logp, torch.where(keep, 2.0 * ref.logp, 0.0))
+    assert torch.equal(y.entropy, ref.entropy) and torch.equal(y.lse, ref.lse)
+    dx, = torch.autograd.grad(y.logp.sum() + y.entropy.sum(), x)
+    z = gpu_lib.token_logprobs(x, tokens)
+    same, = torch.autograd.grad((2.0 * z.logp[keep]).sum() + z.entropy.sum(), x)
+    assert torch.equal(dx, same)
+    with torch.no_grad():
+        z = gpu_lib.token_logprobs(x, tokens)
+        z.logp.zero_()
+        assert torch.equal(z.lse, ref.lse)
+    w = torch.ones(N, device="cuda", requires_grad=True)
+    z = gpu_lib.token_logprobs(x.detach(), tokens)
+    z.logp.mul_(w)   # weights that are trained, on scores that are not
+    assert torch.equal(torch.autograd.grad(z.logp.sum(), w)[0], ref.logp)
