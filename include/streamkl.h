@@ -579,7 +579,7 @@ int streamkl_token_logprobs_bwd(const streamkl_logits* x, const void* tokens, in
 /*
  * A teacher's best tokens, K of each row.
  *   ids       int32 (ids64 = 0) or int64 (1), contiguous [B, N, K]. A negative id is no entry (lists of unequal length); one
- *             >= V makes the row's results NaN.
+ *             >= V makes the row's results NaN, an empty row's too.
  *   values    contiguous [B, N, K] of type dtype. With rest = 1 natural log probabilities; with rest = 0 logits or log
  *             probabilities, of which p = softmax(scale values) over the list is taken.
  *   K         1 to 128, else STREAMKL_ERR_UNSUPPORTED.

@@ -224,9 +224,10 @@ __device__ __forceinline__ DistillStats finish_row(const DistillArgs& a, const S
     }
     if (outside) rest /= (double)sums.l;
   }
-  if (list.some && list.bad) loss = rest = total = (double)__builtin_nanf("");
+  if (!list.some || empty) lse = (double)kNegInf;
+  if (list.bad) loss = rest = total = lse = (double)__builtin_nanf("");   // of an empty row too
   *loss_out = (float)loss;
-  return DistillStats{x0, outside ? sums.r : 0.f, list.some && !empty ? lse : (double)kNegInf, rest, total};
+  return DistillStats{x0, outside ? sums.r : 0.f, lse, rest, total};
 }
 
 // Gradients of the listed logits in the units of x, for the upstream gradient g, by one wave after teacher_side.

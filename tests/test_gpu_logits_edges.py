@@ -141,3 +141,22 @@ def test_outputs_are_edited_in_place(gpu_lib, N):
     z = gpu_lib.token_logprobs(x.detach(), tokens)
     z.logp.mul_(w)   # weights that are trained, on scores that are not
     assert torch.equal(torch.autograd.grad(z.logp.sum(), w)[0], ref.logp)
+
+
+@pytest.mark.parametrize("rest,direction", [(True, "fwd"), (True, "rev"), (False, "fwd")])
+@pytest.mark.parametrize("R", [3, 600])
+def test_an_id_outside_the_vocabulary_spoils_an_empty_row_too(gpu_lib, R, rest, direction):
+    """Loss and gradient alike; without it the row has no loss."""
+    V, K = 2003, 4
+    x = logits(R, V, torch.float32, seed=7)
+    x[:2] = -torch.inf
+    ids = torch.arange(K, device="cuda").expand(R, K).contiguous()
+    ids[1, 2] = V
+    t = torch.full((R, K), -2.0, device="cuda")
+    opts = dict(rest=rest, direction=direction)
+    loss, stats, dx = gpu_lib.topk_distill_step(x, ids, t, **opts)
+    back = gpu_lib.topk_distill_bwd(x, ids, t, stats, **opts)
+    for g in (dx, back):
+        assert loss[0] == 0 and not g[0].any()
+        assert torch.isnan(loss[1]) and torch.isnan(g[1]).all()
+        assert torch.isfinite(loss[2:]).all() and torch.isfinite(g[2:]).all()
