@@ -225,7 +225,8 @@ __device__ __forceinline__ DistillStats finish_row(const DistillArgs& a, const S
     if (outside) rest /= (double)sums.l;
   }
   if (!list.some || empty) lse = (double)kNegInf;
-  if (list.bad) loss = rest = total = lse = (double)__builtin_nanf("");   // of an empty row too
+  // of an empty row too; maxima do not see a NaN, which is no sign of an empty row, and entries of probability 0 no infinity
+  if (list.bad || __any(!(x[0] < -kNegInf) || !(x[1] < -kNegInf))) loss = rest = total = lse = (double)__builtin_nanf("");
   *loss_out = (float)loss;
   return DistillStats{x0, outside ? sums.r : 0.f, lse, rest, total};
 }

@@ -160,3 +160,24 @@ def test_an_id_outside_the_vocabulary_spoils_an_empty_row_too(gpu_lib, R, rest, 
         assert loss[0] == 0 and not g[0].any()
         assert torch.isnan(loss[1]) and torch.isnan(g[1]).all()
         assert torch.isfinite(loss[2:]).all() and torch.isfinite(g[2:]).all()
+
+
+@pytest.mark.parametrize("direction", ["fwd", "rev"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("R,V", [(4, 1), (4, 2003), (600, 2003)])
+def test_a_listed_logit_that_is_none_beside_nothing(gpu_lib, R, V, value, direction):
+    """A row of -inf but for a NaN or +inf in its list is spoilt, not empty, whatever its teacher's value."""
+    x = torch.full((R, V), -torch.inf, device="cuda")
+    x[1:, V // 2] = 2.0
+    x[0, V // 2] = value
+    ids = torch.full((R, 2), -1, dtype=torch.int32, device="cuda")
+    ids[:, 1] = V // 2
+    t = torch.full((R, 2), -0.5, device="cuda")
+    for w, v in ((1.0, -0.5), (0.0, -0.5), (1.0, -torch.inf), (0.0, -torch.inf)):
+        g = torch.ones(R, device="cuda")
+        g[0], t[0] = w, v
+        loss, stats, dx = gpu_lib.topk_distill_step(x, ids, t, g, direction=direction)
+        back = gpu_lib.topk_distill_bwd(x, ids, t, stats, g, direction=direction)
+        assert torch.isnan(loss[0]) and torch.isfinite(loss[1:]).all()
+        for d in (dx, back):
+            assert (torch.isnan(d[0]).all() if w else not d[0].any()) and torch.isfinite(d[1:]).all()
