@@ -7,14 +7,23 @@ Rows are [R, V]. Every function also returns how far a computation may be from i
 float32, U = 2^-24 a rounding, and rounds each result once to its type (the caller's part). A probability is
 exp2((x - r) c): the difference, the product and c are each off by U of themselves, which the exponential turns into
 3 U |z - r| of the term, and the exponential by 2 U. A reference r is within 4 ln 2 < 3 of the largest logit it has
-seen. A lane adds at most V / 64 terms one after the other, and some 20 more roundings join them. So a sum of
-exponentials, relative, and with it its logarithm, absolute, is off by at most
-    SUM = U (3 (D + 3) + 22 + V / 64),    D = sum_j p_j |z_j - max z|.
+seen. The sums: at least 64 lanes share a row, so that a lane adds at most V / 64 terms. In long rows it adds far fewer
+one after the other: the terms of a turn (at most 32 logits a lane) come in four chains of up to 8, 9 additions, and are
+added to the lane's sum at once; 256 threads take at least 2048 logits a turn, of parts of at most 16384, and 512
+threads at least 4096, so that there are at most V / 4096 + 9 turns. Three joins (a wave, a workgroup, parts) with 15
+additions and three moves of a reference, 3 U each, come to 24 roundings; 20 of them count everywhere, short rows having
+fewer levels. So a sum of exponentials, relative, and with it its logarithm, absolute, is off by at most
+    SUM = U (3 (D + 3) + 22 + min(V / 64, V / 4096 + 24)),    D = sum_j p_j |z_j - max z|.
 """
 import numpy as np
 
 U = 2.0 ** -24
 LEAST_REST = 2.0 ** -24
+
+
+def _sum_error(d, V):
+    """SUM, for d the distance D."""
+    return U * (3 * (d + 3) + 22 + min(V / 64, V / 4096 + 24))
 
 
 def _softmax(x, scale):
@@ -30,7 +39,7 @@ def _softmax(x, scale):
         p = np.where(total > 0, e / total, 0.0)
         d = np.where(p > 0, p * np.abs(z - safe), 0.0).sum(-1)
         lp = np.where(total > 0, (z - safe) - np.log(total), -np.inf)
-    return lp, p, lse[:, 0], U * (3 * (d + 3) + 22 + x.shape[-1] / 64)
+    return lp, p, lse[:, 0], _sum_error(d, x.shape[-1])
 
 
 def _entropy_terms(p, lp):
@@ -106,7 +115,7 @@ def _row(z, ids, t, s1, rest, reverse):
     if others:
         zr = z[outside]
         er = np.exp(zr - zr.max())
-        err_r = U * (3 * (np.where(er > 0, er * np.where(er > 0, zr.max() - zr, 0.0), 0.0).sum() / er.sum() + 3) + 22 + V / 64)
+        err_r = _sum_error(np.where(er > 0, er * np.where(er > 0, zr.max() - zr, 0.0), 0.0).sum() / er.sum(), V)
         lqr = lz[outside].max() + np.log(er.sum())
         qr = np.exp(lqr)
     else:

@@ -181,3 +181,23 @@ def test_a_listed_logit_that_is_none_beside_nothing(gpu_lib, R, V, value, direct
         assert torch.isnan(loss[0]) and torch.isfinite(loss[1:]).all()
         for d in (dx, back):
             assert (torch.isnan(d[0]).all() if w else not d[0].any()) and torch.isfinite(d[1:]).all()
+
+
+@pytest.mark.parametrize("V", [100003, 131072])
+def test_how_exact_long_sums_are(gpu_lib, V):
+    """Errors in norm over rows of noise. A result near 10 is rounded to 24 bits: 0.3 2^-24 of it. A lane's sum is off by some
+    2^-24 of itself for each of its at most 16 turns, in different directions, and the lanes' average out; one chain of all
+    terms of a lane is off by a dozen of these (1.1e-6 of the entropies)."""
+    R, K = 96, 32
+    x = logits(R, V, torch.float32, seed=V)
+    tokens = torch.arange(R, device="cuda") * 1009
+    y = gpu_lib.token_logprobs(x, tokens)
+    ref = lo.token_logprobs(np64(x), tokens.cpu().numpy(), 1.0, 0)
+    for n in ("logp", "entropy", "lse"):
+        value = ref[n][0]
+        assert np.linalg.norm(np64(getattr(y, n)) - value) <= 3e-7 * np.linalg.norm(value), n
+    best = gpu_lib.token_logprobs(logits(R, V, torch.float32, seed=V + 1), top=K)
+    for rest, direction in ((True, "fwd"), (True, "rev"), (False, "fwd")):
+        loss = gpu_lib.topk_distill(x, best.top_ids, best.top_logp, rest=rest, direction=direction)
+        value = lo.distill(np64(x), best.top_ids.cpu().numpy(), np64(best.top_logp), 1.0, 1.0, rest, direction == "rev")[0]
+        assert np.linalg.norm(np64(loss) - value) <= 3e-7 * np.linalg.norm(value), (rest, direction)
