@@ -1231,18 +1231,22 @@ class _TopkDistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, ids, teacher, weight, factor, opts):
         loss, stats, grad = topk_distill_step(logits, ids, teacher, weight, *opts, factor)
-        ctx.save_for_backward(logits, ids, teacher, weight, stats)
+        # grad, for an upstream gradient of 1, among the tensors that hooks on saved tensors (offloading, checkpoints) see
+        ctx.save_for_backward(logits, ids, teacher, weight, stats, grad)
         ctx.cfg = (factor, opts)
-        ctx.grad = grad   # for an upstream gradient of 1
+        ctx.handed_over = False
         return _distill_total(loss, weight, factor)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, g):
-        logits, ids, teacher, weight, stats = ctx.saved_tensors
+        logits, ids, teacher, weight, stats, grad = ctx.saved_tensors
         factor, opts = ctx.cfg
-        # the first backward pass hands the gradient over; a later one through a retained graph forms it again
-        out, ctx.grad = ctx.grad, None
+        # the first backward pass hands the gradient over; a later one through a retained graph forms it again. As a tensor
+        # of its own (.data): the saved one does not see what becomes of it, and a leaf takes it without a copy
+        out = None if ctx.handed_over else grad.data
+        ctx.handed_over = True
+        del grad
         return (topk_distill_bwd(logits, ids, teacher, stats, weight, *opts, factor, g.to(torch.float32), out is not None,
                                  out), None, None, None, None, None)
 
@@ -1281,8 +1285,9 @@ def topk_distill_loss(logits, ids, teacher, weight=None, *, s1=1.0, s2=1.0, rest
     mean over all rows. Rows of weight 0 (padding) are left out, whatever they hold.
 
     The weights are known before the losses, so the gradient is formed with them, in the forward call where the logits
-    require one (memory of the logits' size from there on). The backward pass hands it over; for an upstream gradient
-    other than 1 (a loss scale) it forms the gradient anew, rounded once. Under torch.no_grad() only the loss is formed.
+    require one (memory of the logits' size from there on, saved as autograd saves tensors: hooks on these see it, and a
+    checkpoint keeps none of it). The backward pass hands it over; for an upstream gradient other than 1 (a loss scale) it
+    forms the gradient anew, rounded once. Under torch.no_grad() only the loss is formed.
     """
     opts = (s1, s2, rest, direction)
     rows = logits.numel() // logits.shape[-1] if isinstance(logits, torch.Tensor) and logits.numel() else 0

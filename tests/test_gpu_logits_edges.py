@@ -216,3 +216,46 @@ def test_how_exact_long_sums_are(gpu_lib, R, V, dtype):
         value = lo.distill(np64(x[:n]), best.top_ids[:n].cpu().numpy(), np64(best.top_logp[:n]), 1.0, 1.0, rest,
                            direction == "rev")[0]
         assert np.linalg.norm(np64(loss) - value) <= 5 * U * np.linalg.norm(value), (rest, direction)
+
+
+def test_the_gradient_of_the_loss_passes_saved_tensor_hooks(gpu_lib):
+    """What topk_distill_loss keeps of the logits' size goes through save_for_backward: an offloading hook sees it, and a
+    checkpointed loss keeps none of it."""
+    R, V, K = 300, 5003, 8
+    x = logits(R, V, torch.float32, seed=8).requires_grad_(True)
+    best = gpu_lib.token_logprobs(logits(R, V, torch.float32, seed=9), top=K)
+    w = torch.rand(R, device="cuda")
+    args = (best.top_ids, best.top_logp, w)
+    ref, = torch.autograd.grad(gpu_lib.topk_distill_loss(x, *args), x)
+    seen = []
+
+    def pack(t):
+        seen.append(t.shape)
+        return t.cpu()
+
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.cuda()):
+        y = gpu_lib.topk_distill_loss(x, *args)
+    assert seen.count((R, V)) == 2   # logits and gradient
+    for up in (1.0, 3.0):   # handed over, and formed anew
+        dx, = torch.autograd.grad(y, x, torch.tensor(up, device="cuda"), retain_graph=True)
+        near(dx, (up * np64(ref), 2.0 ** -20 * np.abs(up * np64(ref))), "dx")
+    before = torch.cuda.memory_allocated()
+    y = torch.utils.checkpoint.checkpoint(gpu_lib.topk_distill_loss, x, *args, use_reentrant=False)
+    assert torch.cuda.memory_allocated() - before < x.numel() * 4 // 2
+    dx, = torch.autograd.grad(y, x)
+    assert torch.equal(dx, ref)
+
+
+def test_a_gradient_that_was_handed_over_is_the_callers(gpu_lib):
+    """Editing it leaves a retained graph alone, and accumulating into a leaf makes no copy of it."""
+    R, V, K = 300, 5003, 8
+    x = logits(R, V, torch.float32, seed=8).requires_grad_(True)
+    best = gpu_lib.token_logprobs(logits(R, V, torch.float32, seed=9), top=K)
+    y = gpu_lib.topk_distill_loss(x, best.top_ids, best.top_logp)
+    before = torch.cuda.memory_allocated()
+    y.backward(retain_graph=True)
+    assert torch.cuda.memory_allocated() - before < x.numel() * 4 // 2   # the gradient was there
+    first = x.grad.clone()
+    x.grad.zero_()
+    y.backward()
+    near(x.grad, (np64(first), 2.0 ** -20 * np.abs(np64(first))), "dx")
