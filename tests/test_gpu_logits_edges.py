@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import logits_oracle as lo
-from test_gpu_token_logprobs import HALF, TINY, logits, near, np64
+from test_gpu_token_logprobs import HALF, TINY, check_fwd, logits, near, np64
 
 pytestmark = pytest.mark.gpu
 
@@ -259,3 +259,24 @@ def test_a_gradient_that_was_handed_over_is_the_callers(gpu_lib):
     x.grad.zero_()
     y.backward()
     near(x.grad, (np64(first), 2.0 ** -20 * np.abs(np64(first))), "dx")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("scale", [0.9, 0.6, 0.3])
+@pytest.mark.parametrize("V", [150, 1000, 70001])
+def test_values_of_rows_far_from_zero(gpu_lib, V, scale, dtype):
+    """Log probabilities, entropies, best tokens; losses on them and their gradients in both directions."""
+    x, scale = far_rows(V, dtype), f32(scale)
+    tokens = torch.tensor([0, 1, V - 1, 2, 0, 3, 4, 2, -1], device="cuda")
+    check_fwd(gpu_lib, x, tokens, scale, 9)
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    ids = torch.stack([torch.randperm(V, generator=gen, device="cuda")[:6] for _ in range(9)])
+    t = torch.log_softmax(torch.randn(9, 8, generator=gen, device="cuda"), -1)[:, :6].contiguous()
+    for rest, direction in ((True, "fwd"), (True, "rev"), (False, "fwd")):
+        opts = dict(s2=scale, rest=rest, direction=direction)
+        loss, stats, dx = gpu_lib.topk_distill_step(x, ids, t, **opts)
+        back = gpu_lib.topk_distill_bwd(x, ids, t, stats, **opts)
+        value, lb, ref, db = lo.distill(np64(x), ids.cpu().numpy(), np64(t), 1.0, scale, rest, direction == "rev")
+        near(loss, (value, lb), "loss")
+        for g in (dx, back):
+            near(g, (ref, db + HALF[dtype] * np.abs(ref) + TINY[dtype]), "dx")
