@@ -22,11 +22,14 @@
 // 16-byte chunk in LDS, and a chunk that holds a listed logit (at most K of
 // thousands) takes another way through the sums.
 //
-// What belongs to a row (K terms) is formed by one wave, in 64 bits: the terms
-// cancel where student and teacher agree (with float32 logarithms and
-// exponentials the losses of 4094 rows were off by 4.5e-7 instead of 6e-8, for
-// half a percent of the time). Probabilities that only go into gradients are
-// float32. What does not depend on the sums over the row is prepared while its
+// What belongs to a row (K terms) is formed by one wave. Log probabilities,
+// their differences and the sums of the terms are held in 64 bits: they cancel
+// where student and teacher agree (with float32 logarithms and exponentials
+// the losses of 4094 rows were off by 4.5e-7 instead of 6e-8, for half a
+// percent of the time). The probabilities that the differences are weighed
+// with, and those of the gradients, are float32: p_k rounded once, q_k and q_r
+// the exponential of a float32 exponent, off by 2^-24 |log2 q| of themselves,
+// in terms of the size q |log q - log p|. What does not depend on the sums over the row is prepared while its
 // logits are on their way.
 #pragma once
 

@@ -10,10 +10,10 @@
 //
 // A CU holds two workgroups of 512 threads, 8192 chunks each, so that one reads
 // while the other finishes its row or writes. At 8192 x 128000 bf16, 64 entries
-// (4.2 GB, 807 us at the rate of a large copy): 828 us; in two passes 1279 us;
-// one workgroup of 1024 threads that holds the whole row 1024 us; four of 256
-// 960 us; 512 threads of 8 chunks 873 us; gradients kept in the caches 932 us;
-// the chunks read again first to last 868 us. At 8192 x 262144 (three quarters
+// (4.2 GB, 807 us at the rate of a large copy): 812 us; in two passes 1279 us.
+// Where it took 828 us: one workgroup of 1024 threads that holds the whole row
+// 1024 us; four of 256 960 us; 512 threads of 8 chunks 873 us; gradients kept
+// in the caches 932 us; the chunks read again first to last 868 us. At 8192 x 262144 (three quarters
 // read again, 1652 us) 1813 us.
 //
 // All loads of a row are issued before its list is read; the teacher's side is

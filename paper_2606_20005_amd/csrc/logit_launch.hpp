@@ -91,7 +91,8 @@ inline size_t distill_workspace(long long rows, const LogitPlan& p) {
 
 // Whether a distillation step runs as one kernel, a workgroup a row, or as a forward and a backward pass in parts: for few
 // long rows parts fill the chip (one kernel and three, us: 4096 logits, 1 row 8.8 and 12.7; 32000, 1 row 15.5 and 19.4;
-// 128000, 16 rows 25 and 21, 64 rows 25.8 both, 128 rows 28 and 34; 262144, 128 rows 61 and 49, 256 rows 68 and 81).
+// 128000, 16 rows 25 and 21, 64 rows 25.8 both, 128 rows 28 and 34; 262144, 128 rows 61 and 49, 256 rows 68 and 81). Rows
+// whose marks, a byte a chunk, are more than LDS is kept for take two passes as well: float32 from some 135000 logits on.
 inline bool distill_step_fits(long long rows, int V, bool f32) {
   const int chunks = chunks_of(V, f32);
   return chunks <= kMostMarks && (chunks <= 8192 || rows * 128 >= chunks);
